@@ -25,7 +25,8 @@
  *   - Random numbers: Philox4x32-10, key = 64-bit seed, counter =
  *     (index low, index high, sub-index, stream); stream 0 = training
  *     negatives (index = global position of the positive sample, sub-index =
- *     k), stream 1 = initial embeddings (index = row, sub-index = column / 4).
+ *     k), stream 1 = initial embeddings (index = row, sub-index = column / 4),
+ *     stream 5 = dropout (index = row, sub-index = column / 8).
  */
 #ifndef GVHOT_H
 #define GVHOT_H
@@ -361,6 +362,73 @@ int gv_auc(const float *host_pos, uint64_t num_pos, const float *host_neg, uint6
 int gv_link_prediction_auc(gv_ctx *ctx, const uint32_t *host_edge_first, const uint32_t *host_edge_second,
                            uint64_t num_edges, const uint32_t *host_other_first, const uint32_t *host_other_second,
                            uint64_t num_others, double *auc);
+
+/* Operators on rows in device memory: what is done with learned rows after training.  They train a head on
+ * the rows (root-mean-square norm of a sum with a learned gain, dropout, their gradients) and answer queries from
+ * them (rows in 8 bits, scored against a table of rows in 4 bits).  They need no context: they run on `stream` (a hipStream_t
+ * of the calling thread's current device, NULL = its default stream), allocate nothing, return after launching,
+ * and can be captured into a graph; gv_last_error(NULL) has the text of a refusal.  The matrices of a context may be
+ * passed (gv_device_embeddings) once gv_sync has waited for their training.
+ * A matrix of `rows` rows is a pointer, aligned to its values, and a stride: the values from one row to the next, at least
+ * cols (the values of a row lie together).  GV_F32 = float, GV_BF16 = bfloat16, GV_F16 = IEEE half, GV_I8 = int8.
+ * rows <= 2^31, 1 <= cols <= GV_MAX_ROW_COLS; rows = 0 is an empty call.  An output may be the very matrix (pointer, stride and
+ * type) of an input of the same call; matrices that overlap otherwise leave undefined values.
+ * Arithmetic is fp32 whatever the types; a result is rounded once, to nearest even, when it is written.          */
+enum { GV_F32 = 0, GV_BF16 = 1, GV_F16 = 2, GV_I8 = 3 };
+#define GV_MAX_ROW_COLS 16384u
+
+/* Dropout: out = keep ? x * 65536 / (65536 - t) : 0, t = floor(65536 drop + 1/2), 0 <= drop, t < 65536.  keep(i, c) holds
+ * when 16-bit number c mod 8 of Philox block (first_row + i, c / 8) of stream 5 of `seed` is not below t (number 2 w is the
+ * low half of word w, 2 w + 1 its high half), so the mask is never stored: the gradient of x is the same call
+ * on the gradient of out, and a batch that is cut differently drops the same values.  A dropped value is 0 whatever it
+ * was, NaN included.                                                                                          */
+int gv_drop_rows(uint64_t rows, uint32_t cols, int type, const void *dev_x, uint64_t x_stride, double drop, uint64_t seed,
+                 uint64_t first_row, void *dev_out, uint64_t out_stride, void *stream);
+
+/* Root-mean-square norm with the residual's addition:
+ *   h = residual + dropout(x) (dropout as gv_drop_rows; drop = 0 leaves x; dev_residual NULL: h = dropout(x))
+ *   out = h * rstd * gain,  rstd = 1 / sqrt(mean(h^2) + eps),  eps >= 0
+ * x, residual and sum are of `type`, gain float[cols].  dev_sum (may be NULL) receives h, dev_rstd (float[rows], may be
+ * NULL) what the backward pass needs.  out_type = type, or GV_I8 with dev_out_scale[rows]: with v = h * gain, a = max |v| of
+ * the row and step = a * (1 / 127) in fp32, out = v * (1 / step) rounded to the nearest whole number (even at ties) and
+ * out_scale = step * rstd; no sum takes part in the codes, which are the same bits wherever they are computed.  A row
+ * with a < 2^-100 has codes 0 and scale 0, a row with a value of v that is not finite codes 0 and scale NaN.      */
+int gv_norm_rows(uint64_t rows, uint32_t cols, int type, const void *dev_x, uint64_t x_stride, const void *dev_residual,
+                 uint64_t residual_stride, const float *dev_gain, float eps, double drop, uint64_t seed, uint64_t first_row,
+                 void *dev_sum, uint64_t sum_stride, int out_type, void *dev_out, uint64_t out_stride, float *dev_out_scale,
+                 float *dev_rstd, void *stream);
+/* Its gradients from grad_out (of out) and, if not NULL, grad_sum (of h, where the sum is used further):
+ *   n = h * rstd, u = grad_out * gain, dh = rstd * (u - n * mean(u * n)) + grad_sum
+ *   grad_residual = dh (may be NULL), grad_x = dropout of dh with the mask of the forward pass (may be NULL),
+ *   grad_gain[cols] = sum over the rows of grad_out * n (may be NULL; summed in an order that depends on rows and cols
+ *   alone, so a call gives the same bits each time).
+ * dev_sum is h as gv_norm_rows kept it (x itself, where nothing was added or dropped), dev_rstd what it gave.
+ * With grad_gain, dev_workspace points to workspace_bytes bytes (at least those of gv_norm_rows_workspace, aligned to 16)
+ * that the call may overwrite.                                                                                */
+int gv_norm_rows_workspace(uint64_t rows, uint32_t cols, uint64_t *bytes);
+int gv_norm_rows_backward(uint64_t rows, uint32_t cols, int type, const void *dev_grad_out, uint64_t grad_out_stride,
+                          const void *dev_sum, uint64_t sum_stride, const float *dev_gain, const float *dev_rstd,
+                          const void *dev_grad_sum, uint64_t grad_sum_stride, double drop, uint64_t seed, uint64_t first_row,
+                          void *dev_grad_x, uint64_t grad_x_stride, void *dev_grad_residual, uint64_t grad_residual_stride,
+                          float *dev_grad_gain, void *dev_workspace, uint64_t workspace_bytes, void *stream);
+
+/* A table of rows in 4 bits.  Columns share a scale in groups of `group` = 32, 64 or 128 (the last of a row may be short):
+ *   scale = bfloat16(max |w| of the group * (1 / 7)),  code = w * (1 / scale) rounded to the nearest whole number, even at
+ * ties, held to -7..7; the value of a code is code * scale.  dev_codes[rows][16 ceil(cols / 32)], aligned to 16: byte
+ * b of a row holds column 2 b in its low half and 2 b + 1 in its high half as two's complement, columns past the
+ * end are 0.  dev_scales[rows][ceil(cols / group)] are the bits of the bfloat16 scales.  A group with max |w| < 2^-100 has
+ * codes 0 and scale 0, a group with a value that is not finite codes 0 and scale NaN.                             */
+int gv_quantize_rows(uint64_t rows, uint32_t cols, int type, const void *dev_x, uint64_t x_stride, uint32_t group,
+                     uint8_t *dev_codes, uint16_t *dev_scales, void *stream);
+/* Scores of `queries` rows x against every row of such a table (any codes -8..7):
+ *   out[b][i] = sum over the groups g of scale[i][g] * sum over c in g of code[i][c] * x[b][c],   float, out_stride >= rows
+ * x is of `type`; GV_I8 rows stand for x * x_scale[b] (gv_norm_rows gives both; dev_x_scale is NULL otherwise).  The
+ * inner sums are whole numbers and exact: x is taken as a 32-bit whole number, in units of 2^-30 of the power of two above the
+ * largest |x| of its query (of 2^-125 at least), and each group is scaled and added in fp32.  A query with a value that is not finite scores NaN
+ * everywhere, and so does a row with a NaN scale.  queries <= 65536; queries = 0 is an empty call.              */
+int gv_score_rows(uint64_t rows, uint32_t cols, uint32_t group, const uint8_t *dev_codes, const uint16_t *dev_scales,
+                  uint64_t queries, int type, const void *dev_x, uint64_t x_stride, const float *dev_x_scale, float *dev_out,
+                  uint64_t out_stride, void *stream);
 
 /* Wait for all queued device work of the context; folds event timings into the
  * statistics; reports samples that named an id >= n (GV_EINVAL, once), and training that has

@@ -20,6 +20,8 @@ GV_MAX_POOL_SLOTS = 16
 GV_STATIC_SCRATCH_WORDS = 1 << 22
 GV_MAX_PARTITIONS = 64
 GV_SHUFFLE_NONE, GV_SHUFFLE_PSEUDO = 0, 1
+GV_F32, GV_BF16, GV_F16, GV_I8 = 0, 1, 2, 3
+GV_MAX_ROW_COLS = 16384
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgvhot.so")
 
@@ -31,6 +33,7 @@ EXPORTS = [
     "gv_set_adjacency", "gv_augment_device", "gv_auc", "gv_link_prediction_auc", "gv_train_device_pool_static",
     "gv_get_partitions", "gv_redistribute_pool", "gv_train_device_blocks", "gv_draw_negatives_partitioned",
     "gv_build_walk_tables", "gv_augment_weighted", "gv_set_weighted_graph",
+    "gv_drop_rows", "gv_norm_rows", "gv_norm_rows_workspace", "gv_norm_rows_backward", "gv_quantize_rows", "gv_score_rows",
 ]
 
 
@@ -119,6 +122,15 @@ def load():
     L.gv_set_adjacency.argtypes = [vp, C.POINTER(C.c_uint64), u32p]
     L.gv_augment_device.argtypes = [vp, C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint64, C.c_uint64, C.c_uint32, vp,
                                     C.POINTER(C.c_uint64)]
+    u64, u32, i32, dbl = C.c_uint64, C.c_uint32, C.c_int, C.c_double
+    L.gv_drop_rows.argtypes = [u64, u32, i32, vp, u64, dbl, u64, u64, vp, u64, vp]
+    L.gv_norm_rows.argtypes = [u64, u32, i32, vp, u64, vp, u64, vp, C.c_float, dbl, u64, u64, vp, u64, i32, vp, u64, vp,
+                               vp, vp]
+    L.gv_norm_rows_workspace.argtypes = [u64, u32, u64p]
+    L.gv_norm_rows_backward.argtypes = [u64, u32, i32, vp, u64, vp, u64, vp, vp, vp, u64, dbl, u64, u64, vp, u64, vp, u64,
+                                        vp, vp, u64, vp]
+    L.gv_quantize_rows.argtypes = [u64, u32, i32, vp, u64, u32, vp, vp, vp]
+    L.gv_score_rows.argtypes = [u64, u32, u32, vp, vp, u64, i32, vp, u64, vp, vp, u64, vp]
     for name in EXPORTS:
         if name not in ("gv_destroy", "gv_last_error"):
             getattr(L, name).restype = C.c_int

@@ -171,16 +171,21 @@ struct gv_ctx {
 
 namespace {
 
-int fail(gv_ctx *ctx, int code, const char *fmt, ...) noexcept {
+int fail_with(gv_ctx *ctx, int code, const char *fmt, va_list ap) noexcept {
     char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
     vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
     try {
         if (ctx) ctx->error = buf; else g_create_error = buf;
     } catch (...) {  // no memory even for the text: the code alone is returned
     }
+    return code;
+}
+
+int fail(gv_ctx *ctx, int code, const char *fmt, ...) noexcept {
+    va_list ap;
+    va_start(ap, fmt);
+    code = fail_with(ctx, code, fmt, ap);
+    va_end(ap);
     return code;
 }
 
@@ -947,6 +952,14 @@ double rank_auc(const float *pos, uint64_t num_pos, const float *neg, uint64_t n
 }
 
 }  // namespace
+
+int gv::fail_call(int code, const char *fmt, ...) noexcept {
+    va_list ap;
+    va_start(ap, fmt);
+    code = fail_with(nullptr, code, fmt, ap);
+    va_end(ap);
+    return code;
+}
 
 extern "C" {
 

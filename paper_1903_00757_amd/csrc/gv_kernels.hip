@@ -8,6 +8,7 @@
 //
 // The file is compiled twice, side by side: plainly, and with GV_TRACK_LOSS=1 into a second object that holds
 // nothing but the training kernels that also sum the running loss, under names ending in _tracked.
+#include "gv_device.hpp"
 #include "gv_internal.hpp"
 
 #include <algorithm>
@@ -29,24 +30,6 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 
 constexpr bool is_atomic(int c) { return c == kAtomicAgent || c == kMixed; }
 constexpr bool is_agent(int c) { return c == kAgent || c == kAtomicAgent || c == kMixed; }
-
-// ---------------------------------------------------------------------------
-// Philox4x32-10 (Salmon et al., SC'11): ten rounds of two 32x32->64 multiplies
-// and a word permutation; the key advances by the Weyl constants between rounds.
-__device__ __forceinline__ uint4 philox4x32_10(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0,
-                                               uint32_t k1) {
-#pragma unroll
-    for (int round = 0; round < 10; ++round) {
-        const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
-        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
-        c1 = (uint32_t)p1;
-        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
-        c3 = (uint32_t)p0;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
-    }
-    return make_uint4(c0, c1, c2, c3);
-}
 
 // Negative k of positive sample g (Alg. 1, NegativeSampling; Sec. 4.3 alias
 // table): bucket = floor(R * n / 2^64) from the first two words, accepted when
@@ -83,11 +66,6 @@ __device__ __forceinline__ float learning_rate(float lr0, float lr_min_ratio, ui
 // Cross-lane sum of a wave64 with DPP moves: quad butterflies, half-row and row
 // mirrors give every lane its 16-lane row sum; two row broadcasts carry the sums
 // to the last row; the result is read from lane 63 as a wave-uniform scalar.
-template <int kCtrl, int kRowMask>
-__device__ __forceinline__ float dpp_take(float x) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), kCtrl, kRowMask, 0xF, false));
-}
-
 __device__ __forceinline__ float wave_sum(float x) {
     x += dpp_take<0xB1, 0xF>(x);   // quad_perm [1,0,3,2]
     x += dpp_take<0x4E, 0xF>(x);   // quad_perm [2,3,0,1]

@@ -1,0 +1,78 @@
+// Internal interface between the checks of the operators on rows (gv_rows_api.cpp) and their kernels
+// (gv_rows.hip, gv_scores.hip).  Not part of the C boundary.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gv {
+
+struct DropArgs {
+    uint32_t threshold;  // a value is kept when its 16-bit number is not below; 0: all are kept
+    float factor;        // of the values that are kept
+    uint64_t seed, first_row;
+};
+
+struct NormArgs {
+    const void *x, *residual;  // residual may be null
+    const float *gain;
+    void *sum, *out;           // sum may be null
+    float *out_scale, *rstd;   // rstd may be null
+    uint64_t rows, x_stride, residual_stride, sum_stride, out_stride;
+    uint32_t cols;
+    int type, out_type;
+    float eps;
+    DropArgs drop;
+};
+
+struct NormGradArgs {
+    const void *grad_out, *sum, *grad_sum;  // grad_sum may be null
+    const float *gain, *rstd;
+    void *grad_x, *grad_residual;           // both may be null
+    float *grad_gain;                       // may be null
+    float *partial;                         // norm_grad_parts x cols, where grad_gain is wanted
+    uint64_t rows, grad_out_stride, sum_stride, grad_sum_stride, grad_x_stride, grad_residual_stride;
+    uint32_t cols;
+    int type;
+    DropArgs drop;
+};
+
+struct DropRowsArgs {
+    const void *x;
+    void *out;
+    uint64_t rows, x_stride, out_stride;
+    uint32_t cols;
+    int type;
+    DropArgs drop;
+};
+
+struct QuantizeArgs {
+    const void *x;
+    uint8_t *codes;
+    uint16_t *scales;
+    uint64_t rows, x_stride;
+    uint32_t cols, group;
+    int type;
+};
+
+struct ScoreArgs {
+    const uint8_t *codes;
+    const uint16_t *scales;
+    const void *x;
+    const float *x_scale;
+    float *out;
+    uint64_t rows, queries, x_stride, out_stride;
+    uint32_t cols, group;
+    int type;
+};
+
+// how many partial sums of the gain's gradient the backward pass leaves
+uint32_t norm_grad_parts(uint64_t rows, uint32_t cols);
+
+hipError_t launch_norm(const NormArgs &a, hipStream_t stream);
+hipError_t launch_norm_grad(const NormGradArgs &a, hipStream_t stream);
+hipError_t launch_drop(const DropRowsArgs &a, hipStream_t stream);
+hipError_t launch_quantize(const QuantizeArgs &a, hipStream_t stream);
+hipError_t launch_score(const ScoreArgs &a, hipStream_t stream);
+
+}  // namespace gv
