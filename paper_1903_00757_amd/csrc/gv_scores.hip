@@ -1,108 +1,600 @@
 // gfx950 kernels of tables of rows in 4 bits: making one, and the scores of queries against all of its rows.
+//
+// A score is sum_g scale_g sum_{c in g} code_c x_c.  The inner sums are taken in whole numbers: x is a 32-bit whole number
+// times a power of two (of its query), split into four signed digits of 8 bits, and the codes are the high halves of
+// bytes (16 code, which costs a mask and a shift for eight of them and no sign extension); products of bytes are what the
+// dot-product and matrix instructions of this machine take, exactly.  A query is read and split once by every workgroup
+// and then stays, in registers or in LDS, while rows of the table pass by.
 #include "gv_device.hpp"
 #include "gv_rows.hpp"
 #include "gvhot.h"
 
+#include <algorithm>
+
+// a product and a sum round by themselves where no fmaf is written: codes are the same bits wherever they are computed
 #pragma clang fp contract(off)
 
 namespace gv {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWaves = 4;
+constexpr uint32_t kSlot = 32;  // columns to 16 bytes of codes
+
+typedef int i4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float scale_of(uint16_t bits) { return __uint_as_float((uint32_t)bits << 16); }
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// One thread to a group.
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp_word(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xF, 0xF, false);
+}
+
+// Joins the values of kLanes lanes (a power of two, aligned); all of them get the result.
+template <int kLanes, class Join>
+__device__ __forceinline__ uint32_t join_lanes(uint32_t x, Join &&join) {
+    if constexpr (kLanes >= 2) x = join(x, dpp_word<0xB1>(x));    // quad_perm [1,0,3,2]
+    if constexpr (kLanes >= 4) x = join(x, dpp_word<0x4E>(x));    // quad_perm [2,3,0,1]
+    if constexpr (kLanes >= 8) x = join(x, dpp_word<0x141>(x));   // row_half_mirror
+    if constexpr (kLanes >= 16) x = join(x, dpp_word<0x140>(x));  // row_mirror
+    if constexpr (kLanes >= 32) x = join(x, (uint32_t)__shfl_xor((int)x, 16));
+    if constexpr (kLanes >= 64) x = join(x, (uint32_t)__shfl_xor((int)x, 32));
+    return x;
+}
+template <int kLanes>
+__device__ __forceinline__ float sum_lanes(float x) {
+    return __uint_as_float(join_lanes<kLanes>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
+template <int kLanes>
+__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t x) {
+    return join_lanes<kLanes>(x, larger);
+}
+
+// Columns k .. k + 7 of a row, 0 past its end.  A whole piece is one load or two of 16 bytes wherever the row starts.
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_quantize(QuantizeArgs a) {
-    const uint32_t groups = (a.cols + a.group - 1) / a.group;
-    const uint64_t pitch = 16ull * ((a.cols + 31) / 32), all = a.rows * groups;
-    for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (uint64_t)gridDim.x * kThreads) {
-        const uint64_t row = i / groups;
-        const uint32_t g = (uint32_t)(i % groups), first = g * a.group;
-        const uint32_t last = first + a.group < a.cols ? first + a.group : a.cols;
-        const T *x = (const T *)a.x + row * a.x_stride;
-        float largest = 0.0f;
-        bool strange = false;
-        for (uint32_t c = first; c < last; ++c) {
-            const float w = fabsf((float)x[c]);
-            if (w < __builtin_inff()) largest = fmaxf(largest, w); else strange = true;
-        }
-        const __bf16 scale = strange ? (__bf16)__builtin_nanf("") : (__bf16)(largest < 0x1p-100f ? 0.0f : largest * (float)(1.0 / 7.0));
-        const float up = strange || largest < 0x1p-100f ? 0.0f : 1.0f / (float)scale;
-        a.scales[i] = __builtin_bit_cast(uint16_t, scale);
-        const uint32_t end = first + a.group < 2 * (uint32_t)pitch ? first + a.group : 2 * (uint32_t)pitch;
-        for (uint32_t c = first; c < end; c += 2) {
-            uint32_t byte = 0;
-            for (uint32_t k = 0; k < 2; ++k) {
-                const float w = up == 0.0f || c + k >= last ? 0.0f : (float)x[c + k] * up;
-                byte |= ((uint32_t)(int)rintf(fminf(fmaxf(w, -7.0f), 7.0f)) & 15u) << (4 * k);
+__device__ __forceinline__ void load_piece(const T *row, uint32_t k, uint32_t cols, float (&v)[8]) {
+    struct Piece { T at[8]; } p;
+    if (k + 8 <= cols) {
+        __builtin_memcpy(&p, row + k, sizeof p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)p.at[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? (float)row[k + i] : 0.0f;
+    }
+}
+__device__ __forceinline__ void load_piece_of(int type, const void *x, uint64_t at, uint32_t k, uint32_t cols, float (&v)[8]) {
+    if (type == GV_F32) load_piece((const float *)x + at, k, cols, v);
+    else if (type == GV_BF16) load_piece((const __bf16 *)x + at, k, cols, v);
+    else load_piece((const _Float16 *)x + at, k, cols, v);
+}
+
+// Whole numbers of a query whose largest |x| has these bits: x = number * 2^(exponent - 156), |number| <= 2^30.
+struct Whole {
+    int exponent;
+    __device__ __forceinline__ explicit Whole(uint32_t top) : exponent((int)larger(top >> 23, 34u)) {}  // units are normal floats
+    // 0 where the query is not finite: its unit is NaN
+    __device__ __forceinline__ float factor() const { return exponent == 255 ? 0.0f : __uint_as_float((uint32_t)(283 - exponent) << 23); }
+    // of a sum of 16 code * number
+    __device__ __forceinline__ float unit() const {
+        return exponent == 255 ? __builtin_nanf("") : __uint_as_float((uint32_t)(exponent - 33) << 23);
+    }
+};
+
+// The digits of eight columns in the order of the codes' halves: digits[p][0] has digit p of columns 0, 2, 4, 6, [1] of 1, 3, 5, 7.
+__device__ __forceinline__ void split(const float (&v)[8], float factor, uint32_t (&digits)[4][2]) {
+    uint32_t z[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)  // number = sum_p digit_p 256^p with digits -128..127
+        z[i] = factor == 0.0f ? 0u : ((uint32_t)__float2int_rn(v[i] * factor) + 0x00808080u) ^ 0x00808080u;
+#pragma unroll
+    for (int odd = 0; odd < 2; ++odd) {
+        const uint32_t a = z[odd], b = z[2 + odd], c = z[4 + odd], d = z[6 + odd];
+        const uint32_t ab = __builtin_amdgcn_perm(b, a, 0x05010400u), ab2 = __builtin_amdgcn_perm(b, a, 0x07030602u);
+        const uint32_t cd = __builtin_amdgcn_perm(d, c, 0x05010400u), cd2 = __builtin_amdgcn_perm(d, c, 0x07030602u);
+        digits[0][odd] = __builtin_amdgcn_perm(cd, ab, 0x05040100u);
+        digits[1][odd] = __builtin_amdgcn_perm(cd, ab, 0x07060302u);
+        digits[2][odd] = __builtin_amdgcn_perm(cd2, ab2, 0x05040100u);
+        digits[3][odd] = __builtin_amdgcn_perm(cd2, ab2, 0x07060302u);
+    }
+}
+// Eight columns of an 8-bit row, in the same order.
+__device__ __forceinline__ void split_bytes(const int8_t *row, uint32_t k, uint32_t cols, uint32_t (&digits)[2]) {
+    uint32_t w[2] = {0, 0};
+    if (k + 8 <= cols) {
+        __builtin_memcpy(w, row + k, 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k + i < cols) w[i / 4] |= (uint32_t)(uint8_t)row[k + i] << (8 * (i % 4));
+    }
+    digits[0] = __builtin_amdgcn_perm(w[1], w[0], 0x06040200u);
+    digits[1] = __builtin_amdgcn_perm(w[1], w[0], 0x07050301u);
+}
+
+// The codes of a word as bytes of 16 code: the low halves (columns 0, 2, 4, 6), the high halves (1, 3, 5, 7).
+__device__ __forceinline__ uint32_t low_codes(uint32_t w) { return (w << 4) & 0xF0F0F0F0u; }
+__device__ __forceinline__ uint32_t high_codes(uint32_t w) { return w & 0xF0F0F0F0u; }
+
+__device__ __forceinline__ long half_of(i4 x, int j) { return (long)(((uint64_t)(uint32_t)x[2 * j + 1] << 32) | (uint32_t)x[2 * j]); }
+
+// sum_p s[p] 256^p; |s[p]| <= 2^21
+__device__ __forceinline__ float join_digits(int s0, int s1, int s2, int s3) {
+    return fmaf((float)((s3 << 8) + s2), 65536.0f, (float)((s1 << 8) + s0));
+}
+
+// ---------------------------------------------------------------------------
+// Few queries: kLanes lanes to a row of the table, each with 16 bytes of it (32 columns) and the digits of those columns
+// in registers; kColumns digit columns (one query of four digits, or 1, 2 or 4 queries in 8 bits).  A wave has kUnroll loads of 64
+// consecutive pieces in flight.  Rows longer than 2048 columns (kLong): the digits lie in LDS, a lane goes along the row.
+template <bool kFloat, int kColumns, int kLanes, int kUnroll, bool kLong>
+__global__ __launch_bounds__(kThreads) void k_score_few(ScoreArgs a) {
+    constexpr int kQueries = kFloat ? 1 : kColumns, kRows = 64 / kLanes;
+    extern __shared__ uint4 shared_digits[];  // kLong: [column][half][slot]
+    const int lane = threadIdx.x % 64, h = lane % kLanes, sub = lane / kLanes;
+    const uint32_t slots = (a.cols + kSlot - 1) / kSlot, groups = (a.cols + a.group - 1) / a.group;
+    const uint32_t shift = a.group == 32 ? 0 : a.group == 64 ? 1 : 2;
+    const bool mine = (uint32_t)h < slots;
+
+    uint32_t digits[kLong ? 1 : kColumns][8];
+    float unit[kQueries];
+    if constexpr (kFloat) {
+        uint32_t top = 0;
+        if constexpr (kLong) {
+            __shared__ uint32_t tops[kWaves];
+            for (uint32_t k = 8 * threadIdx.x; k < a.cols; k += 8 * kThreads) {
+                float v[8];
+                load_piece_of(a.type, a.x, 0, k, a.cols, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = larger(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
             }
-            a.codes[row * pitch + c / 2] = (uint8_t)byte;
+            top = largest_of_lanes<64>(top);
+            if (lane == 0) tops[threadIdx.x / 64] = top;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) top = larger(top, tops[w]);
+            const Whole whole(top);
+            unit[0] = whole.unit();
+            for (uint32_t p = threadIdx.x; p < 4 * slots; p += kThreads) {  // eight columns: word p % 4 of slot p / 4
+                float v[8];
+                uint32_t d[4][2];
+                load_piece_of(a.type, a.x, 0, 8 * p, a.cols, v);
+                split(v, whole.factor(), d);
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    ((uint2 *)shared_digits)[((c * 2 + p % 4 / 2) * (uint64_t)slots + p / 4) * 2 + p % 2] = make_uint2(d[c][0], d[c][1]);
+            }
+            __syncthreads();
+        } else {
+            float v[4][8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                load_piece_of(a.type, a.x, 0, kSlot * h + 8 * j, a.cols, v[j]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = larger(top, __float_as_uint(v[j][i]) & 0x7FFFFFFFu);
+            }
+            const Whole whole(largest_of_lanes<kLanes>(top));
+            unit[0] = whole.unit();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t d[4][2];
+                split(v[j], whole.factor(), d);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) digits[c][2 * j] = d[c][0], digits[c][2 * j + 1] = d[c][1];
+            }
+        }
+    } else {
+        for (int q = 0; q < kQueries; ++q) {
+            const bool there = (uint64_t)q < a.queries;
+            const int8_t *x = (const int8_t *)a.x + (there ? q : 0) * a.x_stride;
+            unit[q] = there ? a.x_scale[q] * 0.0625f : 0.0f;
+            if constexpr (kLong) {
+                for (uint32_t p = threadIdx.x; p < 4 * slots; p += kThreads) {
+                    uint32_t d[2];
+                    split_bytes(x, 8 * p, there ? a.cols : 0, d);
+                    ((uint2 *)shared_digits)[((q * 2 + p % 4 / 2) * (uint64_t)slots + p / 4) * 2 + p % 2] = make_uint2(d[0], d[1]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t d[2];
+                    split_bytes(x, kSlot * h + 8 * j, there ? a.cols : 0, d);
+                    digits[q][2 * j] = d[0], digits[q][2 * j + 1] = d[1];
+                }
+            }
+        }
+        if constexpr (kLong) __syncthreads();
+    }
+
+    const uint64_t tiles = (a.rows + kRows * kUnroll - 1) / (kRows * kUnroll);
+    for (uint64_t tile = (uint64_t)blockIdx.x * kWaves + threadIdx.x / 64; tile < tiles; tile += (uint64_t)gridDim.x * kWaves) {
+        const uint64_t first = tile * (kRows * kUnroll) + sub;
+        float score[kUnroll][kQueries];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int q = 0; q < kQueries; ++q) score[u][q] = 0.0f;
+        for (uint32_t slot = h; kLong ? slot < slots : slot == (uint32_t)h; slot += kLanes) {
+            uint4 codes[kUnroll];
+            float scale[kUnroll];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const uint64_t row = first + u * kRows;
+                const bool there = row < a.rows && (kLong || mine);
+                codes[u] = there ? ((const uint4 *)a.codes)[row * slots + slot] : make_uint4(0, 0, 0, 0);
+                scale[u] = there ? scale_of(a.scales[row * groups + (slot >> shift)]) : 0.0f;
+            }
+            uint32_t d[kColumns][8];
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c) {
+                if constexpr (kLong) {
+                    const uint4 lo = shared_digits[(c * 2) * (uint64_t)slots + slot], hi = shared_digits[(c * 2 + 1) * (uint64_t)slots + slot];
+                    d[c][0] = lo.x, d[c][1] = lo.y, d[c][2] = lo.z, d[c][3] = lo.w;
+                    d[c][4] = hi.x, d[c][5] = hi.y, d[c][6] = hi.z, d[c][7] = hi.w;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d[c][j] = digits[c][j];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const uint32_t word[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w};
+                int sums[kColumns] = {};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int lo = (int)low_codes(word[j]), hi = (int)high_codes(word[j]);
+#pragma unroll
+                    for (int c = 0; c < kColumns; ++c) {
+                        sums[c] = __builtin_amdgcn_sdot4(lo, (int)d[c][2 * j], sums[c], false);
+                        sums[c] = __builtin_amdgcn_sdot4(hi, (int)d[c][2 * j + 1], sums[c], false);
+                    }
+                }
+                if constexpr (kFloat) {
+                    score[u][0] = fmaf(join_digits(sums[0], sums[1], sums[2], sums[3]), scale[u], score[u][0]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < kQueries; ++q) score[u][q] = fmaf((float)sums[q], scale[u], score[u][q]);
+                }
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < kQueries; ++q) {
+            if (!kFloat && (uint64_t)q >= a.queries) break;
+            float *out = a.out + q * a.out_stride;
+            if constexpr (kLanes >= kUnroll) {  // lane u of a row's lanes writes row u: neighbours in memory, one store
+                float all = 0.0f;
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    const float s = sum_lanes<kLanes>(score[u][q]) * unit[q];
+                    all = h == u ? s : all;
+                }
+                const uint64_t row = first + h * kRows;
+                if (h < kUnroll && row < a.rows) out[row] = all;
+            } else {
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    const float s = sum_lanes<kLanes>(score[u][q]) * unit[q];
+                    const uint64_t row = first + u * kRows;
+                    if (h == u % kLanes && row < a.rows) out[row] = s;
+                }
+            }
         }
     }
 }
 
-// Queries one after the other: the workgroup makes whole numbers of the query, then a thread takes a row of the table.
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_score(ScoreArgs a) {
-    __shared__ int whole[GV_MAX_ROW_COLS];
-    __shared__ uint32_t top;
-    const uint32_t groups = (a.cols + a.group - 1) / a.group;
-    const uint64_t pitch = 16ull * ((a.cols + 31) / 32);
-    for (uint64_t b = blockIdx.y; b < a.queries; b += gridDim.y) {
-        const T *x = (const T *)a.x + b * a.x_stride;
-        float unit = 1.0f;
-        if (threadIdx.x == 0) top = 0;
-        __syncthreads();
-        if (sizeof(T) > 1) {
-            for (uint32_t c = threadIdx.x; c < a.cols; c += kThreads) atomicMax(&top, __float_as_uint((float)x[c]) & 0x7FFFFFFFu);
-            __syncthreads();
-            // the largest |x| is below 2^(exponent - 126); the units are normal floats
-            const int exponent = top >> 23 > 31 ? (int)(top >> 23) : 31;
-            unit = exponent == 255 ? __builtin_nanf("") : ldexpf(1.0f, exponent - 126 - 30);
-            for (uint32_t c = threadIdx.x; c < a.cols; c += kThreads)
-                whole[c] = exponent == 255 ? 0 : (int)rintf(ldexpf((float)x[c], 30 + 126 - exponent));
-        } else {
-            for (uint32_t c = threadIdx.x; c < a.cols; c += kThreads) whole[c] = (int)(float)x[c];
-            unit = a.x_scale[b];
-        }
-        __syncthreads();
-        for (uint64_t row = (uint64_t)blockIdx.x * kThreads + threadIdx.x; row < a.rows; row += (uint64_t)gridDim.x * kThreads) {
-            float score = 0.0f;
-            for (uint32_t g = 0; g < groups; ++g) {
-                const uint32_t first = g * a.group, last = first + a.group < a.cols ? first + a.group : a.cols;
-                int64_t sum = 0;
-                for (uint32_t c = first; c < last; ++c) {
-                    const int code = (int)((uint32_t)a.codes[row * pitch + c / 2] << (c % 2 ? 24 : 28)) >> 28;
-                    sum += (int64_t)code * whole[c];
-                }
-                score += scale_of(a.scales[row * groups + g]) * (float)sum;
+constexpr int many_threads(int tiles) { return tiles == 8 ? 512 : 256; }  // 64 KB of digits serve twice the waves
+
+// ---------------------------------------------------------------------------
+// Many queries: the matrix instruction multiplies 16 digit columns by 16 rows of the table over 32 columns of theirs.  A
+// wave loads 16 rows x 128 columns with 16 bytes a lane (lane r + 16 h: slot h of row r), four such tiles at a time; the
+// 4 x 4 words that lanes r, r + 16, r + 32, r + 48 hold are transposed by four lane swaps, so that word j is slot j
+// everywhere, as the instruction wants it.  The digits of kTiles x 16 columns lie in LDS in the order of the lanes.  The digit
+// columns are the rows of the product: its lane r + 16 h then holds four digits of one query (or four queries in 8 bits) for
+// row r alone, whose scale is one value, and the digits join without another lane.
+template <bool kFloat, int kTiles, int kPer, int kRowTiles>
+__global__ __launch_bounds__(many_threads(kTiles), 4) void k_score_many(ScoreArgs a, uint32_t segment, uint32_t passes) {
+    constexpr int kQueries = kFloat ? 4 : 16;  // of a tile
+    constexpr int kOut = kFloat ? 1 : 4;       // queries of a tile that a lane holds
+    constexpr int kThreads = many_threads(kTiles), kWaves = kThreads / 64, kBlockRows = kWaves * kRowTiles * 16;
+    extern __shared__ uint4 shared_digits[];   // uint2 [pair of slots of the segment][tile][lane][slot of the pair]
+    __shared__ uint32_t tops[kQueries * kTiles];
+    uint2 *digits = (uint2 *)shared_digits;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, h = lane / 16;
+    const uint32_t slots = (a.cols + kSlot - 1) / kSlot, groups = (a.cols + a.group - 1) / a.group;
+    // workgroup b runs on die b mod 8: the passes over the same rows are neighbours on one die and share its L2
+    const uint32_t turn = blockIdx.x / 8, blocks_across = gridDim.x / passes;
+    const uint64_t first_query = (uint64_t)(turn % passes) * (kQueries * kTiles);
+    const uint32_t queries = (uint32_t)std::min<uint64_t>(kQueries * kTiles, a.queries - first_query);
+
+    if constexpr (kFloat) {
+        for (uint32_t q = wave; q < (uint32_t)(kQueries * kTiles); q += kWaves) {
+            uint32_t top = 0;
+            for (uint32_t k = 8 * lane; q < queries && k < a.cols; k += 8 * 64) {
+                float v[8];
+                load_piece_of(a.type, a.x, (first_query + q) * a.x_stride, k, a.cols, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = larger(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
             }
-            a.out[b * a.out_stride + row] = score * unit;
+            top = largest_of_lanes<64>(top);
+            if (lane == 0) tops[q] = top;
         }
         __syncthreads();
     }
+    float unit[kTiles][kOut];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < kOut; ++i) {
+            if constexpr (kFloat) {
+                unit[t][i] = Whole(tops[kQueries * t + h]).unit();
+            } else {
+                const uint32_t q = kQueries * t + 4 * h + i;
+                unit[t][i] = q < queries ? a.x_scale[first_query + q] * 0.0625f : 0.0f;
+            }
+        }
+
+    const uint64_t blocks = (a.rows + kBlockRows - 1) / kBlockRows;
+    const uint64_t all_scales = a.rows * groups;
+    bool staged = false;
+    for (uint64_t block = turn / passes * 8 + blockIdx.x % 8; block < blocks; block += blocks_across) {
+        const uint64_t first = block * kBlockRows + wave * (kRowTiles * 16) + r;
+        float score[kRowTiles][kTiles][kOut];
+#pragma unroll
+        for (int n = 0; n < kRowTiles; ++n)
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int i = 0; i < kOut; ++i) score[n][t][i] = 0.0f;
+        for (uint32_t begin = 0; begin < slots; begin += segment) {
+            const uint32_t end = std::min(begin + segment, slots);
+            if (!staged) {
+                __syncthreads();
+                if constexpr (kFloat) {
+                    for (uint32_t p = threadIdx.x; p < (end - begin) * kTiles * 16; p += kThreads) {
+                        const uint32_t word = p % 4, q = p / 4 % (kQueries * kTiles), slot = p / (4 * kQueries * kTiles);
+                        float v[8];
+                        uint32_t d[4][2];
+                        load_piece_of(a.type, a.x, (first_query + (q < queries ? q : 0)) * a.x_stride, kSlot * (begin + slot) + 8 * word,
+                                      q < queries ? a.cols : 0, v);
+                        split(v, Whole(tops[q]).factor(), d);
+                        uint2 *to = digits + 2 * ((slot / 2 * kTiles + q / 4) * 64 + 16 * word + 4 * (q % 4)) + slot % 2;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) to[2 * c] = make_uint2(d[c][0], d[c][1]);
+                    }
+                } else {
+                    for (uint32_t p = threadIdx.x; p < (end - begin) * kTiles * 64; p += kThreads) {
+                        const uint32_t word = p % 4, q = p / 4 % (kQueries * kTiles), slot = p / (4 * kQueries * kTiles);
+                        uint32_t d[2];
+                        split_bytes((const int8_t *)a.x + (first_query + (q < queries ? q : 0)) * a.x_stride,
+                                    kSlot * (begin + slot) + 8 * word, q < queries ? a.cols : 0, d);
+                        digits[2 * ((slot / 2 * kTiles + q / 16) * 64 + 16 * word + q % 16) + slot % 2] = make_uint2(d[0], d[1]);
+                    }
+                }
+                __syncthreads();
+                staged = segment >= slots;
+            }
+            for (uint32_t base = begin; base < end; base += 4) {
+                uint4 codes[kRowTiles];
+                float scale[kRowTiles][4 / kPer];
+#pragma unroll
+                for (int n = 0; n < kRowTiles; ++n) {
+                    const uint64_t row = first + 16 * n;
+                    const bool there = row < a.rows;
+                    codes[n] = there && base + h < end ? ((const uint4 *)a.codes)[row * slots + base + h] : make_uint4(0, 0, 0, 0);
+                    // one load, which may reach into the next row's scales but not past the table's last; those count as 0
+                    uint16_t bits[4 / kPer] = {};
+                    const uint64_t at = row * groups + base / kPer;
+                    if (there && at + 4 / kPer <= all_scales) {
+                        __builtin_memcpy(bits, a.scales + at, sizeof bits);
+                    } else if (there) {
+#pragma unroll
+                        for (int g = 0; g < 4 / kPer; ++g)
+                            if (at + g < all_scales) bits[g] = a.scales[at + g];
+                    }
+#pragma unroll
+                    for (int g = 0; g < 4 / kPer; ++g) scale[n][g] = base / kPer + g < groups ? scale_of(bits[g]) : 0.0f;
+                }
+                uint32_t word[kRowTiles][4];
+#pragma unroll
+                for (int n = 0; n < kRowTiles; ++n) {
+                    const auto p = __builtin_amdgcn_permlane32_swap(codes[n].x, codes[n].z, false, false);
+                    const auto q = __builtin_amdgcn_permlane32_swap(codes[n].y, codes[n].w, false, false);
+                    const auto lo = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false);
+                    const auto hi = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
+                    word[n][0] = lo[0], word[n][1] = lo[1], word[n][2] = hi[0], word[n][3] = hi[1];
+                }
+                i4 sums[kRowTiles][kTiles];
+                auto add = [&](int g) {  // the sums of group g of these 128 columns
+#pragma unroll
+                    for (int n = 0; n < kRowTiles; ++n)
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) {
+                            const i4 d = sums[n][t];
+                            if constexpr (kFloat) {
+                                score[n][t][0] = fmaf(join_digits(d[0], d[1], d[2], d[3]), scale[n][g], score[n][t][0]);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) score[n][t][i] = fmaf((float)d[i], scale[n][g], score[n][t][i]);
+                            }
+                        }
+                    __builtin_amdgcn_sched_barrier(0);  // the sums of one group at a time: registers for more waves
+                };
+#pragma unroll
+                for (int pair = 0; pair < 2; ++pair) {
+                    // past the row's end whatever lies in LDS meets codes of 0
+                    i4 x[kTiles], w[kRowTiles];
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+                        x[t] = __builtin_bit_cast(i4, shared_digits[((base - begin) / 2 + pair) * (kTiles * 64) + t * 64 + lane]);
+#pragma unroll
+                    for (int n = 0; n < kRowTiles; ++n) {
+                        const uint32_t u = word[n][2 * pair], v = word[n][2 * pair + 1];
+                        w[n] = i4{(int)low_codes(u), (int)high_codes(u), (int)low_codes(v), (int)high_codes(v)};
+                    }
+                    if constexpr (kPer == 1) {  // a slot at a time: 32 columns
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                            for (int n = 0; n < kRowTiles; ++n)
+#pragma unroll
+                                for (int t = 0; t < kTiles; ++t)
+                                    sums[n][t] = __builtin_amdgcn_mfma_i32_16x16x32_i8(half_of(x[t], j), half_of(w[n], j), i4{0, 0, 0, 0}, 0, 0, 0);
+                            add(2 * pair + j);
+                        }
+                    } else {  // both
+#pragma unroll
+                        for (int n = 0; n < kRowTiles; ++n)
+#pragma unroll
+                            for (int t = 0; t < kTiles; ++t)
+                                sums[n][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[t], w[n], kPer == 2 || pair == 0 ? i4{0, 0, 0, 0} : sums[n][t], 0, 0, 0);
+                        if (kPer == 2 || pair == 1) add(kPer == 2 ? pair : 0);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < kRowTiles; ++n) {
+            const uint64_t row = first + 16 * n;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int i = 0; i < kOut; ++i) {
+                    const uint32_t q = kFloat ? kQueries * t + h : kQueries * t + 4 * h + i;
+                    if (row < a.rows && q < queries) a.out[(first_query + q) * a.out_stride + row] = score[n][t][i] * unit[t][i];
+                }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// A table from rows: 8 columns a lane, kLanes lanes to a group.
+template <class T, int kLanes>
+__global__ __launch_bounds__(kThreads) void k_quantize(QuantizeArgs a) {
+    const uint32_t groups = (a.cols + 8 * kLanes - 1) / (8 * kLanes), pieces = groups * kLanes;  // of a row
+    const uint32_t slots = (a.cols + kSlot - 1) / kSlot;
+    const uint64_t all = a.rows * pieces, stride = (uint64_t)gridDim.x * kThreads;
+    uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x, row = i / pieces;
+    uint32_t piece = (uint32_t)(i % pieces);
+    const uint64_t rows_on = stride / pieces;
+    const uint32_t pieces_on = (uint32_t)(stride % pieces);
+    for (; i < all; i += stride) {
+        float v[8];
+        load_piece((const T *)a.x + row * a.x_stride, 8 * piece, a.cols, v);
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = larger(top, __float_as_uint(v[k]) & 0x7FFFFFFFu);
+        const float largest = __uint_as_float(largest_of_lanes<kLanes>(top));
+        const bool finite = largest < __builtin_inff(), any = finite && largest >= 0x1p-100f;
+        const __bf16 scale = !finite ? (__bf16)__builtin_nanf("") : any ? (__bf16)(largest * (float)(1.0 / 7.0)) : (__bf16)0.0f;
+        const float up = any ? 1.0f / (float)scale : 0.0f;
+        uint32_t word = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float w = fminf(fmaxf(v[k] * up, -7.0f), 7.0f);
+            word |= (any ? (uint32_t)__float2int_rn(w) & 15u : 0u) << (4 * k);
+        }
+        if (piece < 4 * slots) ((uint32_t *)a.codes)[row * 4 * slots + piece] = word;
+        if (piece % kLanes == 0) a.scales[row * groups + piece / kLanes] = __builtin_bit_cast(uint16_t, scale);
+        row += rows_on;
+        piece += pieces_on;
+        if (piece >= pieces) piece -= pieces, ++row;
+    }
+}
+
+// ---------------------------------------------------------------------------
+
+template <bool kFloat, int kColumns, int kLanes, bool kLong>
+void score_few(const ScoreArgs &a, hipStream_t stream) {
+    const uint32_t slots = (a.cols + kSlot - 1) / kSlot;
+    const uint32_t bytes = kLong ? kColumns * 32 * slots : 0;
+    const uint64_t waves = (a.rows + 64 / kLanes - 1) / (64 / kLanes);  // of one load each
+    if (waves <= 4096) {  // fewer than four loads for each of four waves on every compute unit: spread them
+        k_score_few<kFloat, kColumns, kLanes, 1, kLong><<<(uint32_t)((waves + kWaves - 1) / kWaves), kThreads, bytes, stream>>>(a);
+    } else {
+        const uint32_t blocks = (uint32_t)std::min<uint64_t>((waves + 4 * kWaves - 1) / (4 * kWaves), kLong ? 512 : 2048);
+        k_score_few<kFloat, kColumns, kLanes, 4, kLong><<<blocks, kThreads, bytes, stream>>>(a);
+    }
+}
+
+template <bool kFloat, int kColumns>
+void score_few_by_length(const ScoreArgs &a, hipStream_t stream) {
+    const uint32_t slots = (a.cols + kSlot - 1) / kSlot;
+    if (slots <= 1) score_few<kFloat, kColumns, 1, false>(a, stream);
+    else if (slots <= 2) score_few<kFloat, kColumns, 2, false>(a, stream);
+    else if (slots <= 4) score_few<kFloat, kColumns, 4, false>(a, stream);
+    else if (slots <= 8) score_few<kFloat, kColumns, 8, false>(a, stream);
+    else if (slots <= 16) score_few<kFloat, kColumns, 16, false>(a, stream);
+    else if (slots <= 32) score_few<kFloat, kColumns, 32, false>(a, stream);
+    else if (slots <= 64) score_few<kFloat, kColumns, 64, false>(a, stream);
+    else score_few<kFloat, kColumns, 64, true>(a, stream);
+}
+
+template <bool kFloat, int kTiles, int kPer>
+void score_many(const ScoreArgs &a, hipStream_t stream) {
+    // Two row tiles a wave write whole lines of a query's scores and read its digits once for both (16 queries x 4*10^6
+    // rows of 128: 119 us, 124 with one; 4 queries in floats: 69 and 97); with rows of over 256 columns the tiles' loads wait
+    // for each other longer than that gains (4 queries x 10^6 rows of 512 in groups of 128: 73 us and 63), and more
+    // tiles of 8-bit queries do not fit the registers (64 queries x 10^6 rows of 128: 165 us, 90 with one).
+    constexpr int kRowTiles = kTiles == 1 || (kFloat && kTiles < 8) ? 2 : 1, kAll = many_threads(kTiles), kEach = (kFloat ? 4 : 16) * kTiles;
+    const uint32_t slots = (a.cols + kSlot - 1) / kSlot;
+    const uint32_t segment = std::min((slots + 3) / 4 * 4, 128u / kTiles), bytes = segment * kTiles * 512;
+    const uint32_t passes = (uint32_t)((a.queries + kEach - 1) / kEach);
+    const uint64_t tiles = (a.rows + 15) / 16;
+    // workgroups across the rows, a multiple of the dies; more than are resident gain nothing, each splits its queries first
+    auto across = [&](uint32_t row_tiles) {
+        const uint64_t each = row_tiles * (kAll / 64), all = (tiles + each - 1) / each;
+        const uint64_t most = std::max<uint64_t>(1, (bytes > 32768 ? 512 : 1024) / passes);
+        return (uint32_t)((std::min(all, most) + 7) / 8 * 8);
+    };
+    if (tiles <= 4096 || slots > 8)
+        k_score_many<kFloat, kTiles, kPer, 1><<<across(1) * passes, kAll, bytes, stream>>>(a, segment, passes);
+    else
+        k_score_many<kFloat, kTiles, kPer, kRowTiles><<<across(kRowTiles) * passes, kAll, bytes, stream>>>(a, segment, passes);
+}
+
+template <bool kFloat, int kTiles>
+void score_many_by_group(const ScoreArgs &a, hipStream_t stream) {
+    if (a.group == 32) score_many<kFloat, kTiles, 1>(a, stream);
+    else if (a.group == 64) score_many<kFloat, kTiles, 2>(a, stream);
+    else score_many<kFloat, kTiles, 4>(a, stream);
+}
+
+template <class T>
+void quantize(const QuantizeArgs &a, hipStream_t stream) {
+    const uint64_t pieces = (uint64_t)((a.cols + a.group - 1) / a.group) * (a.group / 8);
+    const uint32_t blocks = (uint32_t)std::min<uint64_t>((a.rows * pieces + kThreads - 1) / kThreads, 8192);
+    if (a.group == 32) k_quantize<T, 4><<<blocks, kThreads, 0, stream>>>(a);
+    else if (a.group == 64) k_quantize<T, 8><<<blocks, kThreads, 0, stream>>>(a);
+    else k_quantize<T, 16><<<blocks, kThreads, 0, stream>>>(a);
 }
 
 }  // namespace
 
 hipError_t launch_quantize(const QuantizeArgs &a, hipStream_t stream) {
-    const uint64_t all = a.rows * ((a.cols + a.group - 1) / a.group), blocks = (all + kThreads - 1) / kThreads;
-    const uint32_t grid = (uint32_t)(blocks < (1u << 16) ? blocks : 1u << 16);
-    if (a.type == GV_F32) k_quantize<float><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.type == GV_BF16) k_quantize<__bf16><<<grid, kThreads, 0, stream>>>(a);
-    else k_quantize<_Float16><<<grid, kThreads, 0, stream>>>(a);
+    if (a.type == GV_F32) quantize<float>(a, stream);
+    else if (a.type == GV_BF16) quantize<__bf16>(a, stream);
+    else quantize<_Float16>(a, stream);
     return hipGetLastError();
 }
 
 hipError_t launch_score(const ScoreArgs &a, hipStream_t stream) {
-    const uint64_t blocks = (a.rows + kThreads - 1) / kThreads;
-    const dim3 grid((uint32_t)(blocks < 4096 ? blocks : 4096), (uint32_t)(a.queries < 64 ? a.queries : 64));
-    if (a.type == GV_F32) k_score<float><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.type == GV_BF16) k_score<__bf16><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.type == GV_F16) k_score<_Float16><<<grid, kThreads, 0, stream>>>(a);
-    else k_score<int8_t><<<grid, kThreads, 0, stream>>>(a);
+    const uint64_t q = a.queries;
+    if (a.type == GV_I8) {
+        if (q == 1) score_few_by_length<false, 1>(a, stream);
+        else if (q == 2) score_few_by_length<false, 2>(a, stream);
+        else if (q <= 4) score_few_by_length<false, 4>(a, stream);
+        else if (q <= 16) score_many_by_group<false, 1>(a, stream);
+        else if (q <= 32) score_many_by_group<false, 2>(a, stream);
+        else score_many_by_group<false, 4>(a, stream);
+    } else {
+        if (q == 1) score_few_by_length<true, 4>(a, stream);
+        else if (q <= 4) score_many_by_group<true, 1>(a, stream);
+        else if (q <= 8) score_many_by_group<true, 2>(a, stream);
+        else if (q <= 16) score_many_by_group<true, 4>(a, stream);
+        else score_many_by_group<true, 8>(a, stream);
+    }
     return hipGetLastError();
 }
 
