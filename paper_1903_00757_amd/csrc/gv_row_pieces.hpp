@@ -1,0 +1,70 @@
+// Device functions of the kernels on rows (gv_rows.hip, gv_scores.hip): pieces of eight columns, and what the lanes of a
+// row share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gv {
+namespace {
+
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp_word(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xF, 0xF, false);
+}
+
+// Joins the values of kLanes lanes (a power of two, aligned); all of them get the result.
+template <int kLanes, class Join>
+__device__ __forceinline__ uint32_t join_lanes(uint32_t x, Join &&join) {
+    if constexpr (kLanes >= 2) x = join(x, dpp_word<0xB1>(x));    // quad_perm [1,0,3,2]
+    if constexpr (kLanes >= 4) x = join(x, dpp_word<0x4E>(x));    // quad_perm [2,3,0,1]
+    if constexpr (kLanes >= 8) x = join(x, dpp_word<0x141>(x));   // row_half_mirror
+    if constexpr (kLanes >= 16) x = join(x, dpp_word<0x140>(x));  // row_mirror
+    if constexpr (kLanes >= 32) x = join(x, (uint32_t)__shfl_xor((int)x, 16));
+    if constexpr (kLanes >= 64) x = join(x, (uint32_t)__shfl_xor((int)x, 32));
+    return x;
+}
+template <int kLanes>
+__device__ __forceinline__ float sum_lanes(float x) {
+    return __uint_as_float(join_lanes<kLanes>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
+template <int kLanes>
+__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t x) {
+    return join_lanes<kLanes>(x, larger);
+}
+
+// Columns k .. k + 7 of a row, 0 past its end.  A whole piece is one load or two of 16 bytes wherever the row starts.
+template <class T>
+__device__ __forceinline__ void load_piece(const T *row, uint32_t k, uint32_t cols, float (&v)[8]) {
+    struct Piece { T at[8]; } p;
+    if (k + 8 <= cols) {
+        __builtin_memcpy(&p, row + k, sizeof p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)p.at[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? (float)row[k + i] : 0.0f;
+    }
+}
+
+// The same columns of a result: each is rounded once.
+template <class T>
+__device__ __forceinline__ void store_piece(T *row, uint32_t k, uint32_t cols, const float (&v)[8]) {
+    struct Piece { T at[8]; } p;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p.at[i] = (T)v[i];
+    if (k + 8 <= cols) {
+        __builtin_memcpy(row + k, &p, sizeof p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k + i < cols) row[k + i] = p.at[i];
+    }
+}
+
+}  // namespace
+}  // namespace gv

@@ -1,136 +1,294 @@
 // gfx950 kernels of rows in device memory: dropout, and the root-mean-square norm of a sum with its gradients.
+//
+// All of them are bound by memory: a value is read once, stays in a register until everything that its row decides is
+// known, and is written once.  A lane takes pieces of eight columns: 16 bytes of a 16-bit type, and one block of the generator
+// (eight numbers of 16 bits: p is met within 2^-17, and with numbers of 32 bits the generator would take twice the time, as
+// much as the memory traffic of a 16-bit type).
 #include "gv_device.hpp"
+#include "gv_row_pieces.hpp"
 #include "gv_rows.hpp"
 #include "gvhot.h"
 
-// each operation rounds by itself: the 8-bit codes of a row are the same bits wherever they are computed
+#include <algorithm>
+#include <type_traits>
+
+// a product and a sum round by themselves where no fmaf is written: codes are the same bits wherever they are computed
 #pragma clang fp contract(off)
 
 namespace gv {
 namespace {
 
-constexpr int kThreads = 256;
+// Drops values of piece k / 8 of a row; numbers 2 w and 2 w + 1 are the halves of word w.
+__device__ __forceinline__ void drop_piece(const DropArgs &d, uint64_t row, uint32_t piece, float (&v)[8]) {
+    const uint64_t r = d.first_row + row;
+    const uint4 w = philox4x32_10((uint32_t)r, (uint32_t)(r >> 32), piece, 5u, (uint32_t)d.seed, (uint32_t)(d.seed >> 32));
+    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t number = i % 2 ? words[i / 2] >> 16 : words[i / 2] & 0xFFFFu;
+        v[i] = number >= d.threshold ? v[i] * d.factor : 0.0f;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Dropout: one piece a lane and turn.
+constexpr int kDropThreads = 256;
 
 template <class T>
-__device__ __forceinline__ float value(const T *at) {
-    return (float)*at;
-}
-
-// the factor on value (row, col): 0 where it is dropped
-__device__ __forceinline__ bool kept(const DropArgs &d, uint64_t row, uint32_t col) {
-    const uint64_t r = d.first_row + row;
-    const uint4 w = philox4x32_10((uint32_t)r, (uint32_t)(r >> 32), col / 8, 5u, (uint32_t)d.seed, (uint32_t)(d.seed >> 32));
-    const uint32_t word = col % 8 < 2 ? w.x : col % 8 < 4 ? w.y : col % 8 < 6 ? w.z : w.w;
-    return (col % 2 ? word >> 16 : word & 0xFFFFu) >= d.threshold;
-}
-
-__device__ __forceinline__ float dropped(const DropArgs &d, uint64_t row, uint32_t col, float x) {
-    return d.threshold == 0 ? x : kept(d, row, col) ? x * d.factor : 0.0f;
-}
-
-template <class F>
-__device__ __forceinline__ float over_block(float x, float *scratch, F &&join) {
-    scratch[threadIdx.x] = x;
-    __syncthreads();
-    for (int step = kThreads / 2; step > 0; step /= 2) {
-        if ((int)threadIdx.x < step) scratch[threadIdx.x] = join(scratch[threadIdx.x], scratch[threadIdx.x + step]);
-        __syncthreads();
+__global__ __launch_bounds__(kDropThreads) void k_drop(DropRowsArgs a) {
+    const uint32_t pieces = (a.cols + 7) / 8;  // of a row
+    const uint64_t all = a.rows * pieces, stride = (uint64_t)gridDim.x * kDropThreads, rows_on = stride / pieces;
+    const uint32_t pieces_on = (uint32_t)(stride % pieces);
+    uint64_t i = (uint64_t)blockIdx.x * kDropThreads + threadIdx.x, row = i / pieces;
+    uint32_t piece = (uint32_t)(i % pieces);
+    for (; i < all; i += stride) {
+        float v[8];
+        load_piece((const T *)a.x + row * a.x_stride, 8 * piece, a.cols, v);
+        drop_piece(a.drop, row, piece, v);
+        store_piece((T *)a.out + row * a.out_stride, 8 * piece, a.cols, v);
+        row += rows_on;
+        piece += pieces_on;
+        if (piece >= pieces) piece -= pieces, ++row;
     }
-    const float all = scratch[0];
+}
+
+// ---------------------------------------------------------------------------
+// Rows over lanes: kLanes lanes (up to 64, or a whole workgroup of 512) hold a row, kPieces pieces each: lane l has pieces
+// l, l + kLanes, ...  A workgroup holds rows_of(kLanes) rows at a time and goes on to others, with the gain in registers.
+constexpr int kMostLanes = 512;
+constexpr int threads_of(int lanes) { return lanes > 64 ? lanes : 256; }
+
+// Sums over the lanes of a row; all of them get the result.  A whole workgroup's: `turn` says which half of the scratch
+// this row takes, so that one barrier a row is enough.
+template <int kLanes>
+__device__ __forceinline__ float row_sum(float x, float (*scratch)[kMostLanes / 64], int turn) {
+    if constexpr (kLanes <= 64) return sum_lanes<kLanes>(x);
+    x = sum_lanes<64>(x);
+    if (threadIdx.x % 64 == 0) scratch[turn][threadIdx.x / 64] = x;
     __syncthreads();
+    float all = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kLanes / 64; ++w) all += scratch[turn][w];
+    return all;
+}
+template <int kLanes>
+__device__ __forceinline__ uint32_t row_largest(uint32_t x, uint32_t (*scratch)[kMostLanes / 64], int turn) {
+    if constexpr (kLanes <= 64) return largest_of_lanes<kLanes>(x);
+    x = largest_of_lanes<64>(x);
+    if (threadIdx.x % 64 == 0) scratch[turn][threadIdx.x / 64] = x;
+    __syncthreads();
+    uint32_t all = 0;
+#pragma unroll
+    for (int w = 0; w < kLanes / 64; ++w) all = larger(all, scratch[turn][w]);
     return all;
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_drop(DropRowsArgs a) {
-    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x)
-        for (uint32_t c = threadIdx.x; c < a.cols; c += kThreads)
-            ((T *)a.out)[row * a.out_stride + c] = (T)dropped(a.drop, row, c, (float)((const T *)a.x)[row * a.x_stride + c]);
+// 1 / sqrt(x), within one unit in the last place; the instruction takes no subnormal x
+__device__ __forceinline__ float inverse_root(float x) {
+    const bool small = x < 0x1p-100f;
+    return __builtin_amdgcn_rsqf(small ? x * 0x1p64f : x) * (small ? 0x1p32f : 1.0f);
 }
 
-// One workgroup to a row at a time; the row waits in LDS.
-template <class T, bool kBytes>
-__global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
-    __shared__ float h[GV_MAX_ROW_COLS];
-    __shared__ float scratch[kThreads];
-    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        float squares = 0.0f, largest = 0.0f, strange = 0.0f;
-        for (uint32_t c = threadIdx.x; c < a.cols; c += kThreads) {
-            float v = dropped(a.drop, row, c, (float)((const T *)a.x)[row * a.x_stride + c]);
-            if (a.residual) v = (float)((const T *)a.residual)[row * a.residual_stride + c] + v;
-            h[c] = v;
-            squares += v * v;
-            const float w = fabsf(v * a.gain[c]);
-            if (w < __builtin_inff()) largest = fmaxf(largest, w); else strange = 1.0f;
+template <class T, int kLanes, int kPieces, bool kBytes>
+__global__ __launch_bounds__(threads_of(kLanes)) void k_norm(NormArgs a) {
+    constexpr int kRows = threads_of(kLanes) / kLanes;
+    __shared__ float sums[2][kMostLanes / 64];
+    __shared__ uint32_t tops[2][kMostLanes / 64];
+    const uint32_t lane = threadIdx.x % kLanes;
+    float gain[kPieces][8];
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) load_piece(a.gain, 8 * (lane + p * kLanes), a.cols, gain[p]);
+    int turn = 0;
+    for (uint64_t row = (uint64_t)blockIdx.x * kRows + threadIdx.x / kLanes; row < a.rows; row += (uint64_t)gridDim.x * kRows) {
+        float h[kPieces][8], squares = 0.0f;
+        uint32_t top = 0;
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) load_piece((const T *)a.x + row * a.x_stride, 8 * (lane + p * kLanes), a.cols, h[p]);
+        if (a.drop.threshold != 0) {
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) drop_piece(a.drop, row, lane + p * kLanes, h[p]);
         }
-        squares = over_block(squares, scratch, [](float p, float q) { return p + q; });
-        const float rstd = 1.0f / sqrtf(squares / (float)a.cols + a.eps);
-        if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
-        float step = 0.0f, up = 0.0f;
-        if (kBytes) {
-            largest = over_block(largest, scratch, [](float p, float q) { return fmaxf(p, q); });
-            strange = over_block(strange, scratch, [](float p, float q) { return fmaxf(p, q); });
-            if (strange == 0.0f && largest >= 0x1p-100f) {
-                step = largest * (float)(1.0 / 127.0);
-                up = 1.0f / step;
+        if (a.residual) {
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                float r[8];
+                load_piece((const T *)a.residual + row * a.residual_stride, 8 * (lane + p * kLanes), a.cols, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[p][i] = r[i] + h[p][i];
             }
-            if (threadIdx.x == 0) a.out_scale[row] = strange != 0.0f ? __builtin_nanf("") : up == 0.0f ? 0.0f : step * rstd;
         }
-        for (uint32_t c = threadIdx.x; c < a.cols; c += kThreads) {
-            if (a.sum) ((T *)a.sum)[row * a.sum_stride + c] = (T)h[c];
-            if (kBytes)
-                ((int8_t *)a.out)[row * a.out_stride + c] = up == 0.0f ? 0 : (int8_t)(int)rintf(h[c] * a.gain[c] * up);
-            else
-                ((T *)a.out)[row * a.out_stride + c] = (T)(h[c] * rstd * a.gain[c]);
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                squares = fmaf(h[p][i], h[p][i], squares);
+                if (kBytes) top = larger(top, __float_as_uint(h[p][i] * gain[p][i]) & 0x7FFFFFFFu);
+            }
+        squares = row_sum<kLanes>(squares, sums, turn);
+        const float rstd = inverse_root(squares / (float)a.cols + a.eps);
+        if (a.rstd && lane == 0) a.rstd[row] = rstd;
+        if (a.sum) {
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) store_piece((T *)a.sum + row * a.sum_stride, 8 * (lane + p * kLanes), a.cols, h[p]);
         }
-        __syncthreads();
+        if constexpr (kBytes) {
+            const float largest = __uint_as_float(row_largest<kLanes>(top, tops, turn));
+            const bool finite = largest < __builtin_inff(), any = finite && largest >= 0x1p-100f;
+            const float step = largest * (float)(1.0 / 127.0), up = any ? 1.0f / step : 0.0f;
+            if (lane == 0) a.out_scale[row] = !finite ? __builtin_nanf("") : any ? step * rstd : 0.0f;
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = any ? rintf(h[p][i] * gain[p][i] * up) : 0.0f;
+                store_piece((int8_t *)a.out + row * a.out_stride, 8 * (lane + p * kLanes), a.cols, v);
+            }
+        } else {
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = h[p][i] * rstd * gain[p][i];
+                store_piece((T *)a.out + row * a.out_stride, 8 * (lane + p * kLanes), a.cols, v);
+            }
+        }
+        turn ^= 1;
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_norm_grad(NormGradArgs a) {
-    __shared__ float scratch[kThreads];
-    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+// ---------------------------------------------------------------------------
+// Gradients.  A lane adds up its columns of the gain's gradient over the rows that its workgroup takes; rows side by side in
+// a wave are joined by lane exchanges, waves one after the other in LDS, workgroups by k_gain_join: an order that rows and
+// cols decide.
+constexpr int kGradThreads = 512;
+constexpr uint32_t kMostParts = 512;
+
+template <class T, int kLanes, int kPieces>
+__global__ __launch_bounds__(kGradThreads) void k_norm_grad(NormGradArgs a) {
+    constexpr int kRows = kGradThreads / kLanes;
+    __shared__ float sums[2][kMostLanes / 64];
+    __shared__ float joined[kLanes <= 64 ? kLanes * kPieces * 8 : 1];
+    const uint32_t lane = threadIdx.x % kLanes;
+    float gain[kPieces][8], grad_gain[kPieces][8];
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+        if (a.rows > 0) load_piece(a.gain, 8 * (lane + p * kLanes), a.cols, gain[p]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) grad_gain[p][i] = 0.0f;
+    }
+    int turn = 0;
+    for (uint64_t row = (uint64_t)blockIdx.x * kRows + threadIdx.x / kLanes; row < a.rows; row += (uint64_t)gridDim.x * kRows) {
         const float rstd = a.rstd[row];
-        float inner = 0.0f;
-        for (uint32_t c = threadIdx.x; c < a.cols; c += kThreads) {
-            const float n = (float)((const T *)a.sum)[row * a.sum_stride + c] * rstd;
-            inner += (float)((const T *)a.grad_out)[row * a.grad_out_stride + c] * a.gain[c] * n;
+        float n[kPieces][8], u[kPieces][8], inner = 0.0f;
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            load_piece((const T *)a.sum + row * a.sum_stride, 8 * (lane + p * kLanes), a.cols, n[p]);
+            load_piece((const T *)a.grad_out + row * a.grad_out_stride, 8 * (lane + p * kLanes), a.cols, u[p]);
         }
-        inner = over_block(inner, scratch, [](float p, float q) { return p + q; }) / (float)a.cols;
-        for (uint32_t c = threadIdx.x; c < a.cols; c += kThreads) {
-            const float n = (float)((const T *)a.sum)[row * a.sum_stride + c] * rstd;
-            const float u = (float)((const T *)a.grad_out)[row * a.grad_out_stride + c] * a.gain[c];
-            float dh = rstd * (u - n * inner);
-            if (a.grad_sum) dh += (float)((const T *)a.grad_sum)[row * a.grad_sum_stride + c];
-            if (a.grad_residual) ((T *)a.grad_residual)[row * a.grad_residual_stride + c] = (T)dh;
-            if (a.grad_x) ((T *)a.grad_x)[row * a.grad_x_stride + c] = (T)dropped(a.drop, row, c, dh);
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[p][i] *= rstd;
+                grad_gain[p][i] = fmaf(u[p][i], n[p][i], grad_gain[p][i]);
+                u[p][i] *= gain[p][i];
+                inner = fmaf(u[p][i], n[p][i], inner);
+            }
+        inner = row_sum<kLanes>(inner, sums, turn) / (float)a.cols;
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = rstd * (u[p][i] - n[p][i] * inner);
+            if (a.grad_sum) {
+                float g[8];
+                load_piece((const T *)a.grad_sum + row * a.grad_sum_stride, 8 * (lane + p * kLanes), a.cols, g);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += g[i];
+            }
+            if (a.grad_residual) store_piece((T *)a.grad_residual + row * a.grad_residual_stride, 8 * (lane + p * kLanes), a.cols, v);
+            if (a.grad_x) {
+                if (a.drop.threshold != 0) drop_piece(a.drop, row, lane + p * kLanes, v);
+                store_piece((T *)a.grad_x + row * a.grad_x_stride, 8 * (lane + p * kLanes), a.cols, v);
+            }
         }
+        turn ^= 1;
+    }
+    if (!a.grad_gain) return;
+    float *to = a.partial + (uint64_t)blockIdx.x * a.cols;
+    if constexpr (kLanes <= 64) {
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int side = kLanes; side < 64; side *= 2) grad_gain[p][i] += __shfl_xor(grad_gain[p][i], side);
+        for (uint32_t wave = 0; wave < kGradThreads / 64; ++wave) {
+            if (threadIdx.x / 64 == wave && threadIdx.x % 64 < kLanes) {
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float &at = joined[(lane + p * kLanes) * 8 + i];
+                        at = wave == 0 ? grad_gain[p][i] : at + grad_gain[p][i];
+                    }
+            }
+            __syncthreads();
+        }
+        for (uint32_t c = threadIdx.x; c < a.cols; c += kGradThreads) to[c] = joined[c];
+    } else {
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) store_piece(to, 8 * (lane + p * kLanes), a.cols, grad_gain[p]);
     }
 }
 
-// Part p of the gain's gradient: its share of the rows, one thread to a column.
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_gain_parts(NormGradArgs a, uint32_t parts) {
-    const uint32_t c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= a.cols) return;
-    const uint64_t each = (a.rows + parts - 1) / parts, lo = blockIdx.y * each;
-    const uint64_t hi = lo + each < a.rows ? lo + each : a.rows;
+// 32 columns a workgroup, 32 threads to a column.
+__global__ __launch_bounds__(1024) void k_gain_join(const float *partial, float *grad_gain, uint32_t parts, uint32_t cols) {
+    __shared__ float scratch[32][33];
+    const uint32_t c = blockIdx.x * 32 + threadIdx.x % 32, first = threadIdx.x / 32;
     float sum = 0.0f;
-    for (uint64_t row = lo; row < hi; ++row)
-        sum += (float)((const T *)a.grad_out)[row * a.grad_out_stride + c] * ((float)((const T *)a.sum)[row * a.sum_stride + c] * a.rstd[row]);
-    a.partial[(uint64_t)blockIdx.y * a.cols + c] = sum;
+    if (c < cols)
+        for (uint32_t p = first; p < parts; p += 32) sum += partial[(uint64_t)p * cols + c];
+    scratch[first][threadIdx.x % 32] = sum;
+    __syncthreads();
+    sum = scratch[threadIdx.x % 32][first];  // column `first`, part threadIdx.x % 32
+    sum = sum_lanes<32>(sum);
+    if (threadIdx.x % 32 == 0 && blockIdx.x * 32 + first < cols) grad_gain[blockIdx.x * 32 + first] = sum;
 }
 
-__global__ __launch_bounds__(kThreads) void k_gain_join(const float *partial, float *grad_gain, uint32_t parts, uint32_t cols) {
-    const uint32_t c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= cols) return;
-    float sum = 0.0f;
-    for (uint32_t p = 0; p < parts; ++p) sum += partial[(uint64_t)p * cols + c];
-    grad_gain[c] = sum;
+// ---------------------------------------------------------------------------
+
+// Lanes and pieces of a row of `cols` columns: at least eight lanes (a line of a 16-bit type) where the row has that many
+// pieces, two to four pieces a lane.
+struct Shape {
+    int lanes, pieces;
+};
+Shape shape_of(uint32_t cols) {
+    const int pieces = (int)((cols + 7) / 8);
+    if (pieces > 256) return {kMostLanes, (pieces + kMostLanes - 1) / kMostLanes};
+    if (pieces <= 8) return {pieces <= 1 ? 1 : pieces <= 2 ? 2 : pieces <= 4 ? 4 : 8, 1};
+    const int lanes = pieces <= 32 ? 8 : pieces <= 64 ? 16 : pieces <= 128 ? 32 : 64;
+    return {lanes, (pieces + lanes - 1) / lanes};
 }
 
-uint32_t blocks_for(uint64_t rows) { return (uint32_t)(rows < (1u << 16) ? rows : 1u << 16); }
+template <class Run>
+void by_shape(uint32_t cols, Run &&run) {
+    const Shape s = shape_of(cols);
+    auto with = [&](auto lanes) {
+        if (s.pieces == 1) run(lanes, std::integral_constant<int, 1>());
+        else if (s.pieces == 2) run(lanes, std::integral_constant<int, 2>());
+        else if (s.pieces == 3) run(lanes, std::integral_constant<int, 3>());
+        else run(lanes, std::integral_constant<int, 4>());
+    };
+    if (s.lanes == 1) run(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+    else if (s.lanes == 2) run(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
+    else if (s.lanes == 4) run(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
+    else if (s.lanes == 8) with(std::integral_constant<int, 8>());
+    else if (s.lanes == 16) with(std::integral_constant<int, 16>());
+    else if (s.lanes == 32) with(std::integral_constant<int, 32>());
+    else if (s.lanes == 64) with(std::integral_constant<int, 64>());
+    else with(std::integral_constant<int, kMostLanes>());
+}
 
 template <class Run>
 hipError_t by_type(int type, Run &&run) {
@@ -142,32 +300,43 @@ hipError_t by_type(int type, Run &&run) {
 
 }  // namespace
 
-uint32_t norm_grad_parts(uint64_t rows, uint32_t) { return (uint32_t)(rows < 1024 ? rows : 1024); }
+uint32_t norm_grad_parts(uint64_t rows, uint32_t cols) {
+    const uint64_t each = kGradThreads / shape_of(cols).lanes;
+    return (uint32_t)std::min<uint64_t>((rows + each - 1) / each, kMostParts);
+}
 
 hipError_t launch_drop(const DropRowsArgs &a, hipStream_t stream) {
+    const uint64_t blocks = (a.rows * ((a.cols + 7) / 8) + kDropThreads - 1) / kDropThreads;
     return by_type(a.type, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        k_drop<T><<<blocks_for(a.rows), kThreads, 0, stream>>>(a);
+        k_drop<T><<<(uint32_t)std::min<uint64_t>(blocks, 4096), kDropThreads, 0, stream>>>(a);
     });
 }
 
 hipError_t launch_norm(const NormArgs &a, hipStream_t stream) {
     return by_type(a.type, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        if (a.out_type == GV_I8) k_norm<T, true><<<blocks_for(a.rows), kThreads, 0, stream>>>(a);
-        else k_norm<T, false><<<blocks_for(a.rows), kThreads, 0, stream>>>(a);
+        by_shape(a.cols, [&](auto lanes, auto pieces) {
+            constexpr int kLanes = decltype(lanes)::value, kPieces = decltype(pieces)::value, kThreads = threads_of(kLanes);
+            constexpr uint64_t kRows = kThreads / kLanes;
+            const uint32_t blocks = (uint32_t)std::min<uint64_t>((a.rows + kRows - 1) / kRows, 2048 * 256 / kThreads);
+            if (a.out_type == GV_I8) k_norm<T, kLanes, kPieces, true><<<blocks, kThreads, 0, stream>>>(a);
+            else k_norm<T, kLanes, kPieces, false><<<blocks, kThreads, 0, stream>>>(a);
+        });
     });
 }
 
-hipError_t launch_norm_grad(const NormGradArgs &a, hipStream_t stream) {
-    return by_type(a.type, [&](auto *t) {
+hipError_t launch_norm_grad(const NormGradArgs &args, hipStream_t stream) {
+    return by_type(args.type, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        const uint32_t parts = norm_grad_parts(a.rows, a.cols), across = (a.cols + kThreads - 1) / kThreads;
-        if (a.grad_gain) {  // first: grad_x may take the place of grad_out
-            if (parts) k_gain_parts<T><<<dim3(across, parts), kThreads, 0, stream>>>(a, parts);
-            k_gain_join<<<across, kThreads, 0, stream>>>(a.partial, a.grad_gain, parts, a.cols);
-        }
-        if (a.rows && (a.grad_x || a.grad_residual)) k_norm_grad<T><<<blocks_for(a.rows), kThreads, 0, stream>>>(a);
+        NormGradArgs a = args;
+        const uint32_t parts = norm_grad_parts(a.rows, a.cols);
+        if (parts <= 1) a.partial = a.grad_gain;
+        by_shape(a.cols, [&](auto lanes, auto pieces) {
+            constexpr int kLanes = decltype(lanes)::value, kPieces = decltype(pieces)::value;
+            k_norm_grad<T, kLanes, kPieces><<<std::max(parts, 1u), kGradThreads, 0, stream>>>(a);
+        });
+        if (a.grad_gain && parts > 1) k_gain_join<<<(a.cols + 31) / 32, 1024, 0, stream>>>(a.partial, a.grad_gain, parts, a.cols);
     });
 }
 

@@ -5,7 +5,7 @@
 // bytes (16 code, which costs a mask and a shift for eight of them and no sign extension); products of bytes are what the
 // dot-product and matrix instructions of this machine take, exactly.  A query is read and split once by every workgroup
 // and then stays, in registers or in LDS, while rows of the table pass by.
-#include "gv_device.hpp"
+#include "gv_row_pieces.hpp"
 #include "gv_rows.hpp"
 #include "gvhot.h"
 
@@ -23,48 +23,7 @@ constexpr uint32_t kSlot = 32;  // columns to 16 bytes of codes
 typedef int i4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float scale_of(uint16_t bits) { return __uint_as_float((uint32_t)bits << 16); }
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-template <int kCtrl>
-__device__ __forceinline__ uint32_t dpp_word(uint32_t x) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xF, 0xF, false);
-}
-
-// Joins the values of kLanes lanes (a power of two, aligned); all of them get the result.
-template <int kLanes, class Join>
-__device__ __forceinline__ uint32_t join_lanes(uint32_t x, Join &&join) {
-    if constexpr (kLanes >= 2) x = join(x, dpp_word<0xB1>(x));    // quad_perm [1,0,3,2]
-    if constexpr (kLanes >= 4) x = join(x, dpp_word<0x4E>(x));    // quad_perm [2,3,0,1]
-    if constexpr (kLanes >= 8) x = join(x, dpp_word<0x141>(x));   // row_half_mirror
-    if constexpr (kLanes >= 16) x = join(x, dpp_word<0x140>(x));  // row_mirror
-    if constexpr (kLanes >= 32) x = join(x, (uint32_t)__shfl_xor((int)x, 16));
-    if constexpr (kLanes >= 64) x = join(x, (uint32_t)__shfl_xor((int)x, 32));
-    return x;
-}
-template <int kLanes>
-__device__ __forceinline__ float sum_lanes(float x) {
-    return __uint_as_float(join_lanes<kLanes>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
-        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
-    }));
-}
-template <int kLanes>
-__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t x) {
-    return join_lanes<kLanes>(x, larger);
-}
-
-// Columns k .. k + 7 of a row, 0 past its end.  A whole piece is one load or two of 16 bytes wherever the row starts.
-template <class T>
-__device__ __forceinline__ void load_piece(const T *row, uint32_t k, uint32_t cols, float (&v)[8]) {
-    struct Piece { T at[8]; } p;
-    if (k + 8 <= cols) {
-        __builtin_memcpy(&p, row + k, sizeof p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)p.at[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? (float)row[k + i] : 0.0f;
-    }
-}
 __device__ __forceinline__ void load_piece_of(int type, const void *x, uint64_t at, uint32_t k, uint32_t cols, float (&v)[8]) {
     if (type == GV_F32) load_piece((const float *)x + at, k, cols, v);
     else if (type == GV_BF16) load_piece((const __bf16 *)x + at, k, cols, v);
