@@ -37,24 +37,35 @@ __device__ __forceinline__ uint32_t largest_of_lanes(uint32_t x) {
     return join_lanes<kLanes>(x, larger);
 }
 
-// Columns k .. k + 7 of a row, 0 past its end.  A whole piece is one load or two of 16 bytes wherever the row starts.
+// Columns k .. k + 7 of a row as they lie there, 0 past its end: one load or two of 16 bytes wherever the row starts, for
+// a whole piece.  Several are asked for before the first is used.
+template <class T>
+struct Piece {
+    T at[8];
+    __device__ __forceinline__ void load(const T *row, uint32_t k, uint32_t cols) {
+        if (k + 8 <= cols) {
+            __builtin_memcpy(this, row + k, sizeof *this);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) at[i] = k + i < cols ? row[k + i] : (T)0.0f;
+        }
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)at[i];
+    }
+};
 template <class T>
 __device__ __forceinline__ void load_piece(const T *row, uint32_t k, uint32_t cols, float (&v)[8]) {
-    struct Piece { T at[8]; } p;
-    if (k + 8 <= cols) {
-        __builtin_memcpy(&p, row + k, sizeof p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)p.at[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? (float)row[k + i] : 0.0f;
-    }
+    Piece<T> p;
+    p.load(row, k, cols);
+    p.values(v);
 }
 
 // The same columns of a result: each is rounded once.
 template <class T>
 __device__ __forceinline__ void store_piece(T *row, uint32_t k, uint32_t cols, const float (&v)[8]) {
-    struct Piece { T at[8]; } p;
+    Piece<T> p;
 #pragma unroll
     for (int i = 0; i < 8; ++i) p.at[i] = (T)v[i];
     if (k + 8 <= cols) {

@@ -158,7 +158,7 @@ __global__ __launch_bounds__(threads_of(kLanes)) void k_norm(NormArgs a) {
 
 // ---------------------------------------------------------------------------
 // Gradients.  A lane adds up its columns of the gain's gradient over the rows that its workgroup takes; rows side by side in
-// a wave are joined by lane exchanges, waves one after the other in LDS, workgroups by k_gain_join: an order that rows and
+// a wave are joined by lane exchanges, waves in LDS, workgroups by k_gain_join: an order that rows and
 // cols decide.
 constexpr int kGradThreads = 512;
 constexpr uint32_t kMostParts = 512;
@@ -167,7 +167,7 @@ template <class T, int kLanes, int kPieces>
 __global__ __launch_bounds__(kGradThreads) void k_norm_grad(NormGradArgs a) {
     constexpr int kRows = kGradThreads / kLanes;
     __shared__ float sums[2][kMostLanes / 64];
-    __shared__ float joined[kLanes <= 64 ? kLanes * kPieces * 8 : 1];
+    __shared__ float joined[kGradThreads / 64][kLanes <= 64 ? kLanes * kPieces * 8 : 1];
     const uint32_t lane = threadIdx.x % kLanes;
     float gain[kPieces][8], grad_gain[kPieces][8];
 #pragma unroll
@@ -223,19 +223,18 @@ __global__ __launch_bounds__(kGradThreads) void k_norm_grad(NormGradArgs a) {
             for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int side = kLanes; side < 64; side *= 2) grad_gain[p][i] += __shfl_xor(grad_gain[p][i], side);
-        for (uint32_t wave = 0; wave < kGradThreads / 64; ++wave) {
-            if (threadIdx.x / 64 == wave && threadIdx.x % 64 < kLanes) {
+        if (threadIdx.x % 64 < kLanes) {
 #pragma unroll
-                for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float &at = joined[(lane + p * kLanes) * 8 + i];
-                        at = wave == 0 ? grad_gain[p][i] : at + grad_gain[p][i];
-                    }
-            }
-            __syncthreads();
+            for (int p = 0; p < kPieces; ++p)
+                __builtin_memcpy(&joined[threadIdx.x / 64][(lane + p * kLanes) * 8], grad_gain[p], sizeof grad_gain[p]);
         }
-        for (uint32_t c = threadIdx.x; c < a.cols; c += kGradThreads) to[c] = joined[c];
+        __syncthreads();
+        for (uint32_t c = threadIdx.x; c < a.cols; c += kGradThreads) {
+            float all = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kGradThreads / 64; ++w) all += joined[w][c];
+            to[c] = all;
+        }
     } else {
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) store_piece(to, 8 * (lane + p * kLanes), a.cols, grad_gain[p]);
@@ -247,8 +246,13 @@ __global__ __launch_bounds__(1024) void k_gain_join(const float *partial, float 
     __shared__ float scratch[32][33];
     const uint32_t c = blockIdx.x * 32 + threadIdx.x % 32, first = threadIdx.x / 32;
     float sum = 0.0f;
-    if (c < cols)
-        for (uint32_t p = first; p < parts; p += 32) sum += partial[(uint64_t)p * cols + c];
+    for (uint32_t p = first; p < parts && c < cols; p += 32 * 8) {
+        float v[8];  // asked for together: the launch is as long as its loads wait for each other
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p + 32 * i < parts ? partial[(uint64_t)(p + 32 * i) * cols + c] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += v[i];
+    }
     scratch[first][threadIdx.x % 32] = sum;
     __syncthreads();
     sum = scratch[threadIdx.x % 32][first];  // column `first`, part threadIdx.x % 32

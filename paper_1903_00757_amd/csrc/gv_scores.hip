@@ -243,6 +243,105 @@ __global__ __launch_bounds__(kThreads) void k_score_few(ScoreArgs a) {
     }
 }
 
+// A workgroup's work on the kQueries queries of its pass.  A thread keeps to one query and one word of eight columns and goes
+// along the slots, four at a time.
+template <int kQueries, int kThreads>
+struct Queries {
+    static constexpr uint32_t kStep = kThreads / (4 * kQueries);  // slots that the workgroup takes at a time
+    static_assert(kStep >= 1, "a slot of every query fits a workgroup");
+    const ScoreArgs &a;
+    const uint64_t first;
+    const uint32_t count, word, q, slot;
+    __device__ __forceinline__ Queries(const ScoreArgs &args, uint64_t first_query, uint32_t queries, uint32_t thread)
+        : a(args), first(first_query), count(queries), word(thread % 4), q(thread / 4 % kQueries), slot(thread / (4 * kQueries)) {}
+    __device__ __forceinline__ uint32_t cols() const { return q < count ? a.cols : 0; }
+    template <class T>
+    __device__ __forceinline__ const T *row() const {
+        return (const T *)a.x + (first + (q < count ? q : 0)) * a.x_stride;
+    }
+    // the bits of the largest |x| of every query
+    template <class T>
+    __device__ __forceinline__ void tops_of(uint32_t slots, uint32_t *tops) const {
+        uint32_t top = 0;
+        for (uint32_t s = slot; s < slots; s += 4 * kStep) {
+            Piece<T> p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i].load(row<T>(), kSlot * (s + i * kStep) + 8 * word, cols());
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[8];
+                p[i].values(v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) top = larger(top, __float_as_uint(v[k]) & 0x7FFFFFFFu);
+            }
+        }
+        top = largest_of_lanes<4>(top);
+        if (word == 0) atomicMax(tops + q, top);
+    }
+    __device__ __forceinline__ void tops(uint32_t slots, uint32_t *to) const {
+        if (threadIdx.x < kQueries) to[threadIdx.x] = 0;
+        __syncthreads();
+        if (a.type == GV_F32) tops_of<float>(slots, to);
+        else if (a.type == GV_BF16) tops_of<__bf16>(slots, to);
+        else tops_of<_Float16>(slots, to);
+        __syncthreads();
+    }
+    // the digits of slots begin .. end - 1: uint2 [pair of slots][tile][lane][slot of the pair]
+    template <class T>
+    __device__ __forceinline__ void split_of(uint32_t begin, uint32_t end, float factor, uint2 *digits) const {
+        constexpr uint32_t kTiles = kQueries / 4;
+        for (uint32_t s = slot; s < end - begin; s += 4 * kStep) {
+            Piece<T> p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i].load(row<T>(), kSlot * (begin + s + i * kStep) + 8 * word, cols());
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t at = s + i * kStep;
+                float v[8];
+                uint32_t d[4][2];
+                p[i].values(v);
+                split(v, factor, d);
+                if (at < end - begin) {
+                    uint2 *to = digits + 2 * ((at / 2 * kTiles + q / 4) * 64 + 16 * word + 4 * (q % 4)) + at % 2;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) to[2 * c] = make_uint2(d[c][0], d[c][1]);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void split_floats(uint32_t begin, uint32_t end, float factor, uint2 *digits) const {
+        if (a.type == GV_F32) split_of<float>(begin, end, factor, digits);
+        else if (a.type == GV_BF16) split_of<__bf16>(begin, end, factor, digits);
+        else split_of<_Float16>(begin, end, factor, digits);
+    }
+    __device__ __forceinline__ void split_8_bits(uint32_t begin, uint32_t end, uint2 *digits) const {
+        constexpr uint32_t kTiles = kQueries / 16;
+        for (uint32_t s = slot; s < end - begin; s += 4 * kStep) {
+            uint32_t d[4][2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) split_bytes(row<int8_t>(), kSlot * (begin + s + i * kStep) + 8 * word, cols(), d[i]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t at = s + i * kStep;
+                if (at < end - begin) digits[2 * ((at / 2 * kTiles + q / 16) * 64 + 16 * word + q % 16) + at % 2] = make_uint2(d[i][0], d[i][1]);
+            }
+        }
+    }
+};
+
+// Words j of lanes r, r + 16, r + 32, r + 48 transposed: word j of lane r + 16 h becomes word h of lane r + 16 j.
+__device__ __forceinline__ void transpose(const uint4 &codes, uint32_t (&word)[4]) {
+    const auto p = __builtin_amdgcn_permlane32_swap(codes.x, codes.z, false, false);
+    const auto q = __builtin_amdgcn_permlane32_swap(codes.y, codes.w, false, false);
+    const auto lo = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
+    word[0] = lo[0], word[1] = lo[1], word[2] = hi[0], word[3] = hi[1];
+}
+// the codes of two words, as the matrix instruction takes them
+__device__ __forceinline__ i4 code_bytes(uint32_t u, uint32_t v) {
+    return i4{(int)low_codes(u), (int)high_codes(u), (int)low_codes(v), (int)high_codes(v)};
+}
+
 constexpr int many_threads(int tiles) { return tiles == 8 ? 512 : 256; }  // 64 KB of digits serve twice the waves
 
 // ---------------------------------------------------------------------------
@@ -267,20 +366,7 @@ __global__ __launch_bounds__(many_threads(kTiles), 4) void k_score_many(ScoreArg
     const uint64_t first_query = (uint64_t)(turn % passes) * (kQueries * kTiles);
     const uint32_t queries = (uint32_t)std::min<uint64_t>(kQueries * kTiles, a.queries - first_query);
 
-    if constexpr (kFloat) {
-        for (uint32_t q = wave; q < (uint32_t)(kQueries * kTiles); q += kWaves) {
-            uint32_t top = 0;
-            for (uint32_t k = 8 * lane; q < queries && k < a.cols; k += 8 * 64) {
-                float v[8];
-                load_piece_of(a.type, a.x, (first_query + q) * a.x_stride, k, a.cols, v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = larger(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-            }
-            top = largest_of_lanes<64>(top);
-            if (lane == 0) tops[q] = top;
-        }
-        __syncthreads();
-    }
+    if constexpr (kFloat) Queries<kQueries * kTiles, kThreads>(a, first_query, queries, threadIdx.x).tops(slots, tops);
     float unit[kTiles][kOut];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
@@ -310,27 +396,11 @@ __global__ __launch_bounds__(many_threads(kTiles), 4) void k_score_many(ScoreArg
             const uint32_t end = std::min(begin + segment, slots);
             if (!staged) {
                 __syncthreads();
-                if constexpr (kFloat) {
-                    for (uint32_t p = threadIdx.x; p < (end - begin) * kTiles * 16; p += kThreads) {
-                        const uint32_t word = p % 4, q = p / 4 % (kQueries * kTiles), slot = p / (4 * kQueries * kTiles);
-                        float v[8];
-                        uint32_t d[4][2];
-                        load_piece_of(a.type, a.x, (first_query + (q < queries ? q : 0)) * a.x_stride, kSlot * (begin + slot) + 8 * word,
-                                      q < queries ? a.cols : 0, v);
-                        split(v, Whole(tops[q]).factor(), d);
-                        uint2 *to = digits + 2 * ((slot / 2 * kTiles + q / 4) * 64 + 16 * word + 4 * (q % 4)) + slot % 2;
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) to[2 * c] = make_uint2(d[c][0], d[c][1]);
-                    }
-                } else {
-                    for (uint32_t p = threadIdx.x; p < (end - begin) * kTiles * 64; p += kThreads) {
-                        const uint32_t word = p % 4, q = p / 4 % (kQueries * kTiles), slot = p / (4 * kQueries * kTiles);
-                        uint32_t d[2];
-                        split_bytes((const int8_t *)a.x + (first_query + (q < queries ? q : 0)) * a.x_stride,
-                                    kSlot * (begin + slot) + 8 * word, q < queries ? a.cols : 0, d);
-                        digits[2 * ((slot / 2 * kTiles + q / 16) * 64 + 16 * word + q % 16) + slot % 2] = make_uint2(d[0], d[1]);
-                    }
-                }
+                uint32_t thread = threadIdx.x;
+                asm volatile("" : "+v"(thread));  // nothing of this waits in registers through the loops
+                const Queries<kQueries * kTiles, kThreads> stage(a, first_query, queries, thread);
+                if constexpr (kFloat) stage.split_floats(begin, end, Whole(tops[stage.q]).factor(), digits);
+                else stage.split_8_bits(begin, end, digits);
                 __syncthreads();
                 staged = segment >= slots;
             }
@@ -357,13 +427,7 @@ __global__ __launch_bounds__(many_threads(kTiles), 4) void k_score_many(ScoreArg
                 }
                 uint32_t word[kRowTiles][4];
 #pragma unroll
-                for (int n = 0; n < kRowTiles; ++n) {
-                    const auto p = __builtin_amdgcn_permlane32_swap(codes[n].x, codes[n].z, false, false);
-                    const auto q = __builtin_amdgcn_permlane32_swap(codes[n].y, codes[n].w, false, false);
-                    const auto lo = __builtin_amdgcn_permlane16_swap(p[0], q[0], false, false);
-                    const auto hi = __builtin_amdgcn_permlane16_swap(p[1], q[1], false, false);
-                    word[n][0] = lo[0], word[n][1] = lo[1], word[n][2] = hi[0], word[n][3] = hi[1];
-                }
+                for (int n = 0; n < kRowTiles; ++n) transpose(codes[n], word[n]);
                 i4 sums[kRowTiles][kTiles];
                 auto add = [&](int g) {  // the sums of group g of these 128 columns
 #pragma unroll
@@ -388,10 +452,7 @@ __global__ __launch_bounds__(many_threads(kTiles), 4) void k_score_many(ScoreArg
                     for (int t = 0; t < kTiles; ++t)
                         x[t] = __builtin_bit_cast(i4, shared_digits[((base - begin) / 2 + pair) * (kTiles * 64) + t * 64 + lane]);
 #pragma unroll
-                    for (int n = 0; n < kRowTiles; ++n) {
-                        const uint32_t u = word[n][2 * pair], v = word[n][2 * pair + 1];
-                        w[n] = i4{(int)low_codes(u), (int)high_codes(u), (int)low_codes(v), (int)high_codes(v)};
-                    }
+                    for (int n = 0; n < kRowTiles; ++n) w[n] = code_bytes(word[n][2 * pair], word[n][2 * pair + 1]);
                     if constexpr (kPer == 1) {  // a slot at a time: 32 columns
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
@@ -423,6 +484,83 @@ __global__ __launch_bounds__(many_threads(kTiles), 4) void k_score_many(ScoreArg
                     const uint32_t q = kFloat ? kQueries * t + h : kQueries * t + 4 * h + i;
                     if (row < a.rows && q < queries) a.out[(first_query + q) * a.out_stride + row] = score[n][t][i] * unit[t][i];
                 }
+        }
+    }
+}
+
+// Many queries and rows of up to 64 columns: a load holds 64 / kSlots rows of kSlots slots (lane r + 16 h: slot h mod kSlots
+// of row 16 (h / kSlots) + r), so that after the transposition word j is slot j mod kSlots of tile j / kSlots.
+// One group: of the row (kPer = kSlots), or of each slot.
+template <bool kFloat, int kTiles, int kPer, int kSlots>
+__global__ __launch_bounds__(many_threads(kTiles), 4) void k_score_narrow(ScoreArgs a, uint32_t passes) {
+    constexpr int kQueries = kFloat ? 4 : 16, kOut = kFloat ? 1 : 4, kGroups = kSlots / kPer;
+    constexpr int kThreads = many_threads(kTiles), kLoadRows = 64 / kSlots, kBlockRows = kThreads / 64 * kLoadRows;
+    __shared__ uint4 shared_digits[kTiles * 64];
+    __shared__ uint32_t tops[kQueries * kTiles];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, h = lane / 16;
+    const uint32_t slots = (a.cols + kSlot - 1) / kSlot;  // kSlots
+    const uint32_t turn = blockIdx.x / 8, blocks_across = gridDim.x / passes;
+    const uint64_t first_query = (uint64_t)(turn % passes) * (kQueries * kTiles);
+    const uint32_t queries = (uint32_t)std::min<uint64_t>(kQueries * kTiles, a.queries - first_query);
+    const Queries<kQueries * kTiles, kThreads> stage(a, first_query, queries, threadIdx.x);
+    if constexpr (kFloat) {
+        stage.tops(slots, tops);
+        stage.split_floats(0, slots, Whole(tops[stage.q]).factor(), (uint2 *)shared_digits);
+    } else {
+        stage.split_8_bits(0, slots, (uint2 *)shared_digits);
+    }
+    __syncthreads();
+    float unit[kTiles][kOut];
+    i4 x[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        x[t] = __builtin_bit_cast(i4, shared_digits[t * 64 + lane]);  // of one slot: the second half is not used
+#pragma unroll
+        for (int i = 0; i < kOut; ++i) {
+            const uint32_t q = kFloat ? kQueries * t + h : kQueries * t + 4 * h + i;
+            if constexpr (kFloat) unit[t][i] = Whole(tops[q]).unit();
+            else unit[t][i] = q < queries ? a.x_scale[first_query + q] * 0.0625f : 0.0f;
+        }
+    }
+    const uint64_t blocks = (a.rows + kBlockRows - 1) / kBlockRows;
+    for (uint64_t block = turn / passes * 8 + blockIdx.x % 8; block < blocks; block += blocks_across) {
+        const uint64_t first = block * kBlockRows + wave * kLoadRows;
+        const uint64_t mine = first + 16 * (h / kSlots) + r;
+        const uint4 codes = mine < a.rows ? ((const uint4 *)a.codes)[mine * kSlots + h % kSlots] : make_uint4(0, 0, 0, 0);
+        float scale[4 / kSlots][kGroups];
+#pragma unroll
+        for (int n = 0; n < 4 / kSlots; ++n) {
+            const uint64_t row = first + 16 * n + r;
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) scale[n][g] = row < a.rows ? scale_of(a.scales[row * kGroups + g]) : 0.0f;
+        }
+        uint32_t word[4];
+        transpose(codes, word);
+#pragma unroll
+        for (int n = 0; n < 4 / kSlots; ++n) {
+            const uint64_t row = first + 16 * n + r;
+            const i4 w = kSlots == 2 ? code_bytes(word[2 * n], word[2 * n + 1]) : code_bytes(word[n], 0);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                float score[kOut] = {};
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    i4 d = {0, 0, 0, 0};
+                    if constexpr (kPer == 2) d = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[t], w, d, 0, 0, 0);
+                    else d = __builtin_amdgcn_mfma_i32_16x16x32_i8(half_of(x[t], g), half_of(w, g), d, 0, 0, 0);
+                    if constexpr (kFloat) {
+                        score[0] = fmaf(join_digits(d[0], d[1], d[2], d[3]), scale[n][g], score[0]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) score[i] = fmaf((float)d[i], scale[n][g], score[i]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kOut; ++i) {
+                    const uint32_t q = kFloat ? kQueries * t + h : kQueries * t + 4 * h + i;
+                    if (row < a.rows && q < queries) a.out[(first_query + q) * a.out_stride + row] = score[i] * unit[t][i];
+                }
+            }
         }
     }
 }
@@ -493,9 +631,10 @@ void score_few_by_length(const ScoreArgs &a, hipStream_t stream) {
 template <bool kFloat, int kTiles, int kPer>
 void score_many(const ScoreArgs &a, hipStream_t stream) {
     // Two row tiles a wave write whole lines of a query's scores and read its digits once for both (16 queries x 4*10^6
-    // rows of 128: 119 us, 124 with one; 4 queries in floats: 69 and 97); with rows of over 256 columns the tiles' loads wait
-    // for each other longer than that gains (4 queries x 10^6 rows of 512 in groups of 128: 73 us and 63), and more
-    // tiles of 8-bit queries do not fit the registers (64 queries x 10^6 rows of 128: 165 us, 90 with one).
+    // rows of 128: 119 us, 124 with one; 4 queries in floats: 69 and 97; 16 bfloat16 queries x 5*10^5 rows of 1024 in groups
+    // of 32: 139 and 173).  Rows of over 256 columns in larger groups, whose sums are joined more seldom, gain more from more
+    // waves (4 queries x 10^6 rows of 512 in groups of 128: 73 us and 63), and more tiles of 8-bit queries do not fit the
+    // registers twice (64 queries x 10^6 rows of 128: 165 us, 90 with one).
     constexpr int kRowTiles = kTiles == 1 || (kFloat && kTiles < 8) ? 2 : 1, kAll = many_threads(kTiles), kEach = (kFloat ? 4 : 16) * kTiles;
     const uint32_t slots = (a.cols + kSlot - 1) / kSlot;
     const uint32_t segment = std::min((slots + 3) / 4 * 4, 128u / kTiles), bytes = segment * kTiles * 512;
@@ -504,18 +643,29 @@ void score_many(const ScoreArgs &a, hipStream_t stream) {
     // workgroups across the rows, a multiple of the dies; more than are resident gain nothing, each splits its queries first
     auto across = [&](uint32_t row_tiles) {
         const uint64_t each = row_tiles * (kAll / 64), all = (tiles + each - 1) / each;
-        const uint64_t most = std::max<uint64_t>(1, (bytes > 32768 ? 512 : 1024) / passes);
+        const uint64_t most = std::max<uint64_t>(1, (bytes > 32768 || kAll > 256 ? 512 : 1024) / passes);
         return (uint32_t)((std::min(all, most) + 7) / 8 * 8);
     };
-    if (tiles <= 4096 || slots > 8)
+    if (tiles <= 4096 || (slots > 8 && kPer > 1))
         k_score_many<kFloat, kTiles, kPer, 1><<<across(1) * passes, kAll, bytes, stream>>>(a, segment, passes);
     else
         k_score_many<kFloat, kTiles, kPer, kRowTiles><<<across(kRowTiles) * passes, kAll, bytes, stream>>>(a, segment, passes);
 }
 
+template <bool kFloat, int kTiles, int kPer, int kSlots>
+void score_narrow(const ScoreArgs &a, hipStream_t stream) {
+    constexpr int kAll = many_threads(kTiles), kEach = (kFloat ? 4 : 16) * kTiles, kRows = kAll / kSlots;
+    const uint32_t passes = (uint32_t)((a.queries + kEach - 1) / kEach);
+    const uint64_t across = std::min<uint64_t>((a.rows + kRows - 1) / kRows, std::max<uint64_t>(1, (kAll > 256 ? 512 : 1024) / passes));
+    k_score_narrow<kFloat, kTiles, kPer, kSlots><<<(uint32_t)((across + 7) / 8 * 8) * passes, kAll, 0, stream>>>(a, passes);
+}
+
 template <bool kFloat, int kTiles>
 void score_many_by_group(const ScoreArgs &a, hipStream_t stream) {
-    if (a.group == 32) score_many<kFloat, kTiles, 1>(a, stream);
+    if (a.cols <= kSlot) score_narrow<kFloat, kTiles, 1, 1>(a, stream);
+    else if (a.cols <= 2 * kSlot && a.group == 32) score_narrow<kFloat, kTiles, 1, 2>(a, stream);
+    else if (a.cols <= 2 * kSlot) score_narrow<kFloat, kTiles, 2, 2>(a, stream);
+    else if (a.group == 32) score_many<kFloat, kTiles, 1>(a, stream);
     else if (a.group == 64) score_many<kFloat, kTiles, 2>(a, stream);
     else score_many<kFloat, kTiles, 4>(a, stream);
 }

@@ -39,52 +39,74 @@ def _refuse(text):
     raise ValueError(text)
 
 
-def _rows(name, t, like=None, dtype=None):
-    """(address, stride) of a matrix of rows, which has to be like another."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        _refuse(f"{name}: a 2-D tensor whose rows are contiguous")
-    if like is not None and (t.shape != like.shape or t.device != like.device or t.dtype is not (dtype or like.dtype)):
-        _refuse(f"{name}: shape, type or device does not fit")
-    rows, cols = t.shape
-    return t.data_ptr(), (t.stride(0) if rows > 1 else cols)
+def _stream_call():
+    """torch's current stream of a GPU by its number, as an address.  The public way makes a Stream object first, which
+    takes 1.9 us, as long as the launch of a short kernel."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _kind(t, kinds, name):
-    if not t.is_cuda:
-        _refuse(f"{name}: not in device memory")
+_stream_of = _stream_call()
+_current_device = torch.cuda.current_device
+_f32, _int8, _uint8, _bf16 = torch.float32, torch.int8, torch.uint8, torch.bfloat16
+
+
+def _first(name, t, kinds=_TYPES):
+    """(address, stride, rows, cols, type, GPU) of the matrix of rows that the others of a call have to be like."""
     kind = kinds.get(t.dtype)
-    if kind is None:
-        _refuse(f"{name}: type {t.dtype} is not supported")
-    return kind
+    if kind is None or not t.is_cuda:
+        _refuse(f"{name}: rows of {', '.join(map(str, kinds))} in device memory are asked for")
+    shape = t.shape
+    if len(shape) != 2:
+        _refuse(f"{name}: a 2-D tensor")
+    rows, cols = shape
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
+        _refuse(f"{name}: the values of a row lie together")
+    return t.data_ptr(), (stride if rows > 1 else cols), rows, cols, kind, t.get_device()
 
 
-def _array(name, t, size, dtype, like):
+def _rows(name, t, rows, cols, dtype, gpu):
+    """(address, stride) of another matrix of rows."""
+    if t.shape != (rows, cols) or t.dtype is not dtype or t.get_device() != gpu:
+        _refuse(f"{name}: {rows} rows of {cols} {dtype} on the same GPU are asked for")
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
+        _refuse(f"{name}: the values of a row lie together")
+    return t.data_ptr(), (stride if rows > 1 else cols)
+
+
+def _array(name, t, size, dtype, gpu):
     """Address of a contiguous array of `size` values."""
-    if t.dtype is not dtype or t.numel() != size or not t.is_contiguous() or t.device != like.device:
-        _refuse(f"{name}: {size} contiguous values of {dtype} on {like.device}")
+    if t.dtype is not dtype or t.numel() != size or not t.is_contiguous() or t.get_device() != gpu:
+        _refuse(f"{name}: {size} contiguous values of {dtype} on the same GPU are asked for")
     return t.data_ptr()
 
 
-def _call(entry, device, *args):
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if device.index == torch.cuda.current_device():
-        rc = entry(*args, stream)
+def _call(entry, gpu, *args):
+    if gpu == _current_device():
+        rc = entry(*args, _stream_of(gpu))
     else:
-        with torch.cuda.device(device):
-            rc = entry(*args, stream)
+        with torch.cuda.device(gpu):
+            rc = entry(*args, _stream_of(gpu))
     if rc != GV_OK:
         raise GvError(rc, load().gv_last_error(None).decode())
 
 
+def _like(x, rows, cols):
+    """A new matrix of x's shape and type; the call that reads them from x takes two thirds of the other's time."""
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+
+
 def gv_drop_rows(x, drop, seed, *, first_row=0, out=None):
     """Dropout of rows.  The gradient of x is the same call, with the same drop, seed and first_row, on out's gradient."""
-    kind = _kind(x, _TYPES, "x")
-    rows, cols = x.shape if x.dim() == 2 else _refuse("x: a 2-D tensor")
-    at, stride = _rows("x", x)
+    at, stride, rows, cols, kind, gpu = _first("x", x)
     if out is None:
-        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    out_at, out_stride = _rows("out", out, x)
-    _call(load().gv_drop_rows, x.device, rows, cols, kind, at, stride, drop, seed, first_row, out_at, out_stride)
+        out = _like(x, rows, cols)
+        out_at, out_stride = out.data_ptr(), cols
+    else:
+        out_at, out_stride = _rows("out", out, rows, cols, x.dtype, gpu)
+    _call(load().gv_drop_rows, gpu, rows, cols, kind, at, stride, drop, seed, first_row, out_at, out_stride)
     return out
 
 
@@ -92,31 +114,40 @@ def gv_norm_rows(x, gain, residual=None, *, eps=1e-6, drop=0.0, seed=0, first_ro
                  keep_rstd=False, out=None, scale=None, sum=None):
     """Root-mean-square norm of residual + dropout(x).  out_type torch.int8 gives 8-bit rows and their scales.  The sum is
     kept (unless keep_sum is false) where it is another than x.  out, scale and sum may be passed; sum may be residual."""
-    kind = _kind(x, _TYPES, "x")
-    rows, cols = x.shape if x.dim() == 2 else _refuse("x: a 2-D tensor")
-    device = x.device
-    at, stride = _rows("x", x)
-    res_at, res_stride = (None, 0) if residual is None else _rows("residual", residual, x)
-    gain_at = _array("gain", gain, cols, torch.float32, x)
+    at, stride, rows, cols, kind, gpu = _first("x", x)
+    dtype, device = x.dtype, x.device
+    gain_at = _array("gain", gain, cols, _f32, gpu)
+    res_at, res_stride = (None, 0) if residual is None else _rows("residual", residual, rows, cols, dtype, gpu)
     if out is None:
-        out = torch.empty((rows, cols), dtype=out_type or x.dtype, device=device)
-    if out_type is not None and out.dtype is not out_type:
-        _refuse("out is not of out_type")
-    bytes_out = out.dtype is torch.int8
-    out_at, out_stride = _rows("out", out, x, out.dtype if bytes_out else None)
-    scale_at = None
-    if bytes_out:
+        out_type = out_type or dtype
+        out = _like(x, rows, cols) if out_type is dtype else torch.empty((rows, cols), dtype=out_type, device=device)
+        out_at, out_stride = out.data_ptr(), cols
+    else:
+        out_type = out_type or out.dtype
+        out_at, out_stride = _rows("out", out, rows, cols, out_type, gpu)
+    if out_type is not dtype and out_type is not _int8:
+        _refuse("out: the type of x, or torch.int8")
+    scale_at = sum_at = rstd = rstd_at = None
+    sum_stride, out_kind = 0, kind
+    if out_type is _int8:
+        out_kind = GV_I8
         if scale is None:
-            scale = torch.empty(rows, dtype=torch.float32, device=device)
-        scale_at = _array("scale", scale, rows, torch.float32, x)
+            scale = torch.empty(rows, dtype=_f32, device=device)
+            scale_at = scale.data_ptr()
+        else:
+            scale_at = _array("scale", scale, rows, _f32, gpu)
     elif scale is not None:
         _refuse("scale belongs to an 8-bit out")
-    if sum is None and keep_sum and (residual is not None or drop != 0.0):
-        sum = torch.empty((rows, cols), dtype=x.dtype, device=device)
-    sum_at, sum_stride = (None, 0) if sum is None else _rows("sum", sum, x)
-    rstd = torch.empty(rows, dtype=torch.float32, device=device) if keep_rstd else None
-    _call(load().gv_norm_rows, device, rows, cols, kind, at, stride, res_at, res_stride, gain_at, eps, drop, seed, first_row,
-          sum_at, sum_stride, GV_I8 if bytes_out else kind, out_at, out_stride, scale_at, rstd.data_ptr() if keep_rstd else None)
+    if sum is not None:
+        sum_at, sum_stride = _rows("sum", sum, rows, cols, dtype, gpu)
+    elif keep_sum and (residual is not None or drop != 0.0):
+        sum = _like(x, rows, cols)
+        sum_at, sum_stride = sum.data_ptr(), cols
+    if keep_rstd:
+        rstd = torch.empty(rows, dtype=_f32, device=device)
+        rstd_at = rstd.data_ptr()
+    _call(load().gv_norm_rows, gpu, rows, cols, kind, at, stride, res_at, res_stride, gain_at, eps, drop, seed, first_row,
+          sum_at, sum_stride, out_kind, out_at, out_stride, scale_at, rstd_at)
     return NormRows(out, scale, sum, rstd)
 
 
@@ -134,56 +165,57 @@ def gv_norm_rows_backward(grad_out, sum, gain, rstd, *, grad_sum=None, drop=0.0,
                           keep_gain=True):
     """Gradients of gv_norm_rows for x, residual and gain.  The residual's is made where keep_residual asks for it (by
     default: where grad_sum is passed); without dropout it is x's, the same tensor."""
-    kind = _kind(grad_out, _TYPES, "grad_out")
-    rows, cols = grad_out.shape if grad_out.dim() == 2 else _refuse("grad_out: a 2-D tensor")
-    device = grad_out.device
-    go_at, go_stride = _rows("grad_out", grad_out)
-    sum_at, sum_stride = _rows("sum", sum, grad_out)
-    gs_at, gs_stride = (None, 0) if grad_sum is None else _rows("grad_sum", grad_sum, grad_out)
-    gain_at = _array("gain", gain, cols, torch.float32, grad_out)
-    rstd_at = _array("rstd", rstd, rows, torch.float32, grad_out)
-    grad_x = torch.empty((rows, cols), dtype=grad_out.dtype, device=device)
-    grad_residual = None
+    go_at, go_stride, rows, cols, kind, gpu = _first("grad_out", grad_out)
+    dtype, device = grad_out.dtype, grad_out.device
+    sum_at, sum_stride = _rows("sum", sum, rows, cols, dtype, gpu)
+    gs_at, gs_stride = (None, 0) if grad_sum is None else _rows("grad_sum", grad_sum, rows, cols, dtype, gpu)
+    gain_at = _array("gain", gain, cols, _f32, gpu)
+    rstd_at = _array("rstd", rstd, rows, _f32, gpu)
+    grad_x = _like(grad_out, rows, cols)
+    grad_residual = res_at = grad_gain = gain_to = space_at = None
+    size = 0
     if grad_sum is not None if keep_residual is None else keep_residual:
-        grad_residual = grad_x if drop == 0.0 else torch.empty_like(grad_x)
-    apart = grad_residual is not None and grad_residual is not grad_x
-    grad_gain, space, size = None, None, 0
+        if drop == 0.0:
+            grad_residual = grad_x
+        else:
+            grad_residual = _like(grad_out, rows, cols)
+            res_at = grad_residual.data_ptr()
     if keep_gain:
-        grad_gain = torch.empty(cols, dtype=torch.float32, device=device)
         size = gv_norm_rows_workspace(rows, cols)
-        space = torch.empty(size, dtype=torch.uint8, device=device)
-    _call(load().gv_norm_rows_backward, device, rows, cols, kind, go_at, go_stride, sum_at, sum_stride, gain_at, rstd_at, gs_at,
-          gs_stride, drop, seed, first_row, grad_x.data_ptr(), cols, grad_residual.data_ptr() if apart else None, cols,
-          grad_gain.data_ptr() if keep_gain else None, space.data_ptr() if keep_gain else None, size)
+        grad_gain = torch.empty(cols, dtype=_f32, device=device)
+        space = torch.empty(size, dtype=_uint8, device=device)
+        gain_to, space_at = grad_gain.data_ptr(), space.data_ptr()
+    _call(load().gv_norm_rows_backward, gpu, rows, cols, kind, go_at, go_stride, sum_at, sum_stride, gain_at, rstd_at, gs_at,
+          gs_stride, drop, seed, first_row, grad_x.data_ptr(), cols, res_at, cols, gain_to, space_at, size)
     return NormGrads(grad_x, grad_residual, grad_gain)
+
+
+def _parts(cols, size):
+    return -(-cols // size) if size > 0 else 0
 
 
 def gv_quantize_rows(x, *, group=32):
     """(codes uint8[rows][16 ceil(cols / 32)], scales bfloat16[rows][ceil(cols / group)]): the table of x in 4 bits."""
-    kind = _kind(x, _TYPES, "x")
-    rows, cols = x.shape if x.dim() == 2 else _refuse("x: a 2-D tensor")
-    at, stride = _rows("x", x)
-    codes = torch.empty((rows, 16 * (-(-cols // 32))), dtype=torch.uint8, device=x.device)
-    scales = torch.empty((rows, -(-cols // group) if group > 0 else 0), dtype=torch.bfloat16, device=x.device)
-    _call(load().gv_quantize_rows, x.device, rows, cols, kind, at, stride, group, codes.data_ptr(), scales.data_ptr())
+    at, stride, rows, cols, kind, gpu = _first("x", x)
+    codes = torch.empty((rows, 16 * _parts(cols, 32)), dtype=_uint8, device=x.device)
+    scales = torch.empty((rows, _parts(cols, group)), dtype=_bf16, device=x.device)
+    _call(load().gv_quantize_rows, gpu, rows, cols, kind, at, stride, group, codes.data_ptr(), scales.data_ptr())
     return codes, scales
 
 
 def gv_score_rows(codes, scales, x, *, group=32, scale=None, out=None):
     """float32[queries][rows]: the scores of the query rows x (8-bit rows with their `scale`) against every row of the
     table that gv_quantize_rows made."""
-    kind = _kind(x, _TYPES_AND_BYTES, "x")
-    queries, cols = x.shape if x.dim() == 2 else _refuse("x: a 2-D tensor")
+    at, stride, queries, cols, kind, gpu = _first("x", x, _TYPES_AND_BYTES)
     rows = codes.shape[0]
-    at, stride = _rows("x", x)
-    codes_at = _array("codes", codes, rows * 16 * (-(-cols // 32)), torch.uint8, x)
-    scales_at = _array("scales", scales, rows * (-(-cols // group)) if group > 0 else 0, torch.bfloat16, x)
+    codes_at = _array("codes", codes, rows * 16 * _parts(cols, 32), _uint8, gpu)
+    scales_at = _array("scales", scales, rows * _parts(cols, group), _bf16, gpu)
     if out is None:
-        out = torch.empty((queries, rows), dtype=torch.float32, device=x.device)
-    elif out.shape != (queries, rows) or out.dtype is not torch.float32 or out.device != x.device:
-        _refuse("out: float32[queries][rows]")
-    out_at, out_stride = _rows("out", out)
-    scale_at = None if scale is None else _array("scale", scale, queries, torch.float32, x)
-    _call(load().gv_score_rows, x.device, rows, cols, group, codes_at, scales_at, queries, kind, at, stride, scale_at, out_at,
+        out = torch.empty((queries, rows), dtype=_f32, device=x.device)
+        out_at, out_stride = out.data_ptr(), rows
+    else:
+        out_at, out_stride = _rows("out", out, queries, rows, _f32, gpu)
+    scale_at = None if scale is None else _array("scale", scale, queries, _f32, gpu)
+    _call(load().gv_score_rows, gpu, rows, cols, group, codes_at, scales_at, queries, kind, at, stride, scale_at, out_at,
           out_stride)
     return out
