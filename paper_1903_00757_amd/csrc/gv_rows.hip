@@ -53,8 +53,8 @@ __global__ __launch_bounds__(kDropThreads) void k_drop(DropRowsArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Rows over lanes: kLanes lanes (up to 64, or a whole workgroup of 512) hold a row, kPieces pieces each: lane l has pieces
-// l, l + kLanes, ...  A workgroup holds rows_of(kLanes) rows at a time and goes on to others, with the gain in registers.
+// Rows over lanes: kLanes lanes (up to 64, or a whole workgroup of 256 or 512) hold a row, kPieces pieces each: lane l has
+// pieces l, l + kLanes, ...
 constexpr int kMostLanes = 512;
 constexpr int threads_of(int lanes) { return lanes > 64 ? lanes : 256; }
 
@@ -160,12 +160,12 @@ __global__ __launch_bounds__(threads_of(kLanes)) void k_norm(NormArgs a) {
 // Gradients.  A lane adds up its columns of the gain's gradient over the rows that its workgroup takes; rows side by side in
 // a wave are joined by lane exchanges, waves in LDS, workgroups by k_gain_join: an order that rows and
 // cols decide.
-constexpr int kGradThreads = 512;
-constexpr uint32_t kMostParts = 512;
+constexpr int grad_threads_of(int lanes) { return lanes > 64 ? lanes : 512; }
+constexpr uint32_t kGradLanes = 1 << 18;  // of the whole launch at most: four waves to each of the chip's 1024 SIMDs
 
 template <class T, int kLanes, int kPieces>
-__global__ __launch_bounds__(kGradThreads) void k_norm_grad(NormGradArgs a) {
-    constexpr int kRows = kGradThreads / kLanes;
+__global__ __launch_bounds__(grad_threads_of(kLanes)) void k_norm_grad(NormGradArgs a) {
+    constexpr int kGradThreads = grad_threads_of(kLanes), kRows = kGradThreads / kLanes;
     __shared__ float sums[2][kMostLanes / 64];
     __shared__ float joined[kGradThreads / 64][kLanes <= 64 ? kLanes * kPieces * 8 : 1];
     const uint32_t lane = threadIdx.x % kLanes;
@@ -263,35 +263,39 @@ __global__ __launch_bounds__(1024) void k_gain_join(const float *partial, float 
 // ---------------------------------------------------------------------------
 
 // Lanes and pieces of a row of `cols` columns: at least eight lanes (a line of a 16-bit type) where the row has that many
-// pieces, two to four pieces a lane.
+// pieces, and two pieces a lane as far as that goes.  With up to four, a row takes fewer exchanges, but the gradients take 200
+// registers instead of 125 and two waves a SIMD do not keep the memory busy (10^5 rows of 1024 in bfloat16, forward and
+// backward: 371 us, 291 with two; 2*10^5 of 160: 141 and 116).
 struct Shape {
     int lanes, pieces;
 };
 Shape shape_of(uint32_t cols) {
     const int pieces = (int)((cols + 7) / 8);
-    if (pieces > 256) return {kMostLanes, (pieces + kMostLanes - 1) / kMostLanes};
-    if (pieces <= 8) return {pieces <= 1 ? 1 : pieces <= 2 ? 2 : pieces <= 4 ? 4 : 8, 1};
-    const int lanes = pieces <= 32 ? 8 : pieces <= 64 ? 16 : pieces <= 128 ? 32 : 64;
+    const int lanes = pieces <= 1 ? 1 : pieces <= 2 ? 2 : pieces <= 4 ? 4 : pieces <= 16 ? 8 : pieces <= 32 ? 16 : pieces <= 64 ? 32
+                      : pieces <= 128 ? 64 : pieces <= 256 ? 256 : kMostLanes;
     return {lanes, (pieces + lanes - 1) / lanes};
 }
 
+template <int kLanes, int kPieces, class Run>
+void with_shape(Run &&run) {
+    run(std::integral_constant<int, kLanes>(), std::integral_constant<int, kPieces>());
+}
 template <class Run>
 void by_shape(uint32_t cols, Run &&run) {
     const Shape s = shape_of(cols);
-    auto with = [&](auto lanes) {
-        if (s.pieces == 1) run(lanes, std::integral_constant<int, 1>());
-        else if (s.pieces == 2) run(lanes, std::integral_constant<int, 2>());
-        else if (s.pieces == 3) run(lanes, std::integral_constant<int, 3>());
-        else run(lanes, std::integral_constant<int, 4>());
-    };
-    if (s.lanes == 1) run(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-    else if (s.lanes == 2) run(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
-    else if (s.lanes == 4) run(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
-    else if (s.lanes == 8) with(std::integral_constant<int, 8>());
-    else if (s.lanes == 16) with(std::integral_constant<int, 16>());
-    else if (s.lanes == 32) with(std::integral_constant<int, 32>());
-    else if (s.lanes == 64) with(std::integral_constant<int, 64>());
-    else with(std::integral_constant<int, kMostLanes>());
+    if (s.lanes == 1) with_shape<1, 1>(run);
+    else if (s.lanes == 2) with_shape<2, 1>(run);
+    else if (s.lanes == 4) with_shape<4, 1>(run);
+    else if (s.lanes == 8 && s.pieces == 1) with_shape<8, 1>(run);
+    else if (s.lanes == 8) with_shape<8, 2>(run);
+    else if (s.lanes == 16) with_shape<16, 2>(run);
+    else if (s.lanes == 32) with_shape<32, 2>(run);
+    else if (s.lanes == 64) with_shape<64, 2>(run);
+    else if (s.lanes == 256) with_shape<256, 1>(run);
+    else if (s.pieces == 1) with_shape<kMostLanes, 1>(run);
+    else if (s.pieces == 2) with_shape<kMostLanes, 2>(run);
+    else if (s.pieces == 3) with_shape<kMostLanes, 3>(run);
+    else with_shape<kMostLanes, 4>(run);
 }
 
 template <class Run>
@@ -305,15 +309,21 @@ hipError_t by_type(int type, Run &&run) {
 }  // namespace
 
 uint32_t norm_grad_parts(uint64_t rows, uint32_t cols) {
-    const uint64_t each = kGradThreads / shape_of(cols).lanes;
-    return (uint32_t)std::min<uint64_t>((rows + each - 1) / each, kMostParts);
+    const int lanes = shape_of(cols).lanes, threads = grad_threads_of(lanes);
+    const uint64_t each = threads / lanes;
+    return (uint32_t)std::min<uint64_t>((rows + each - 1) / each, kGradLanes / threads);
 }
+
+// Workgroups that come and go pass through memory side by side; a grid that loops drifts apart (dropout of
+// 2^20 rows of 512 in bfloat16, there and back: 755 us, 901 with 4096 workgroups; 2^20 rows of 128 through the norm
+// and back: 435 and 462 us).  They loop past the largest grid of 2^32 threads alone.
+constexpr uint64_t kMostBlocks = 1 << 22;
 
 hipError_t launch_drop(const DropRowsArgs &a, hipStream_t stream) {
     const uint64_t blocks = (a.rows * ((a.cols + 7) / 8) + kDropThreads - 1) / kDropThreads;
     return by_type(a.type, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        k_drop<T><<<(uint32_t)std::min<uint64_t>(blocks, 4096), kDropThreads, 0, stream>>>(a);
+        k_drop<T><<<(uint32_t)std::min<uint64_t>(blocks, kMostBlocks), kDropThreads, 0, stream>>>(a);
     });
 }
 
@@ -323,7 +333,7 @@ hipError_t launch_norm(const NormArgs &a, hipStream_t stream) {
         by_shape(a.cols, [&](auto lanes, auto pieces) {
             constexpr int kLanes = decltype(lanes)::value, kPieces = decltype(pieces)::value, kThreads = threads_of(kLanes);
             constexpr uint64_t kRows = kThreads / kLanes;
-            const uint32_t blocks = (uint32_t)std::min<uint64_t>((a.rows + kRows - 1) / kRows, 2048 * 256 / kThreads);
+            const uint32_t blocks = (uint32_t)std::min<uint64_t>((a.rows + kRows - 1) / kRows, kMostBlocks);
             if (a.out_type == GV_I8) k_norm<T, kLanes, kPieces, true><<<blocks, kThreads, 0, stream>>>(a);
             else k_norm<T, kLanes, kPieces, false><<<blocks, kThreads, 0, stream>>>(a);
         });
@@ -338,7 +348,7 @@ hipError_t launch_norm_grad(const NormGradArgs &args, hipStream_t stream) {
         if (parts <= 1) a.partial = a.grad_gain;
         by_shape(a.cols, [&](auto lanes, auto pieces) {
             constexpr int kLanes = decltype(lanes)::value, kPieces = decltype(pieces)::value;
-            k_norm_grad<T, kLanes, kPieces><<<std::max(parts, 1u), kGradThreads, 0, stream>>>(a);
+            k_norm_grad<T, kLanes, kPieces><<<std::max(parts, 1u), grad_threads_of(kLanes), 0, stream>>>(a);
         });
         if (a.grad_gain && parts > 1) k_gain_join<<<(a.cols + 31) / 32, 1024, 0, stream>>>(a.partial, a.grad_gain, parts, a.cols);
     });
