@@ -87,85 +87,68 @@ __device__ __forceinline__ float join_digits(int s0, int s1, int s2, int s3) {
 // ---------------------------------------------------------------------------
 // Few queries: kLanes lanes to a row of the table, each with 16 bytes of it (32 columns) and the digits of those columns
 // in registers; kColumns digit columns (one query of four digits, or 1, 2 or 4 queries in 8 bits).  A wave has kUnroll loads of 64
-// consecutive pieces in flight.  Rows longer than 2048 columns (kLong): the digits lie in LDS, a lane goes along the row.
+// consecutive pieces in flight.  Rows longer than 2048 columns (kLong): the digits stay in LDS, a lane goes along the row.
 template <bool kFloat, int kColumns, int kLanes, int kUnroll, bool kLong>
 __global__ __launch_bounds__(kThreads) void k_score_few(ScoreArgs a) {
     constexpr int kQueries = kFloat ? 1 : kColumns, kRows = 64 / kLanes;
-    extern __shared__ uint4 shared_digits[];  // kLong: [column][half][slot]
+    extern __shared__ uint4 shared_digits[];  // [digit column][half][slot]
     const int lane = threadIdx.x % 64, h = lane % kLanes, sub = lane / kLanes;
     const uint32_t slots = (a.cols + kSlot - 1) / kSlot, groups = (a.cols + a.group - 1) / a.group;
     const uint32_t shift = a.group == 32 ? 0 : a.group == 64 ? 1 : 2;
     const bool mine = (uint32_t)h < slots;
 
-    uint32_t digits[kLong ? 1 : kColumns][8];
+    // The queries are split once by the workgroup: eight columns a thread, word p % 4 of slot p / 4.
+    auto keep = [&](int column, uint32_t p, uint32_t even, uint32_t odd) {
+        ((uint2 *)shared_digits)[((column * 2 + p % 4 / 2) * (uint64_t)slots + p / 4) * 2 + p % 2] = make_uint2(even, odd);
+    };
     float unit[kQueries];
     if constexpr (kFloat) {
+        __shared__ uint32_t tops[kWaves];
         uint32_t top = 0;
-        if constexpr (kLong) {
-            __shared__ uint32_t tops[kWaves];
-            for (uint32_t k = 8 * threadIdx.x; k < a.cols; k += 8 * kThreads) {
-                float v[8];
-                load_piece_of(a.type, a.x, 0, k, a.cols, v);
+        float v[8];
+        for (uint32_t p = threadIdx.x; p < 4 * slots; p += kThreads) {
+            load_piece_of(a.type, a.x, 0, 8 * p, a.cols, v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) top = larger(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-            }
-            top = largest_of_lanes<64>(top);
-            if (lane == 0) tops[threadIdx.x / 64] = top;
-            __syncthreads();
+            for (int i = 0; i < 8; ++i) top = larger(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+        }
+        top = largest_of_lanes<64>(top);
+        if (lane == 0) tops[threadIdx.x / 64] = top;
+        __syncthreads();
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) top = larger(top, tops[w]);
-            const Whole whole(top);
-            unit[0] = whole.unit();
-            for (uint32_t p = threadIdx.x; p < 4 * slots; p += kThreads) {  // eight columns: word p % 4 of slot p / 4
-                float v[8];
-                uint32_t d[4][2];
-                load_piece_of(a.type, a.x, 0, 8 * p, a.cols, v);
-                split(v, whole.factor(), d);
+        for (int w = 0; w < kWaves; ++w) top = larger(top, tops[w]);
+        const Whole whole(top);
+        unit[0] = whole.unit();
+        for (uint32_t p = threadIdx.x; p < 4 * slots; p += kThreads) {
+            uint32_t d[4][2];
+            if constexpr (kLong) load_piece_of(a.type, a.x, 0, 8 * p, a.cols, v);  // otherwise it is the one piece of above
+            split(v, whole.factor(), d);
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    ((uint2 *)shared_digits)[((c * 2 + p % 4 / 2) * (uint64_t)slots + p / 4) * 2 + p % 2] = make_uint2(d[c][0], d[c][1]);
-            }
-            __syncthreads();
-        } else {
-            float v[4][8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                load_piece_of(a.type, a.x, 0, kSlot * h + 8 * j, a.cols, v[j]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = larger(top, __float_as_uint(v[j][i]) & 0x7FFFFFFFu);
-            }
-            const Whole whole(largest_of_lanes<kLanes>(top));
-            unit[0] = whole.unit();
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t d[4][2];
-                split(v[j], whole.factor(), d);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) digits[c][2 * j] = d[c][0], digits[c][2 * j + 1] = d[c][1];
-            }
+            for (int c = 0; c < 4; ++c) keep(c, p, d[c][0], d[c][1]);
         }
     } else {
+#pragma unroll
         for (int q = 0; q < kQueries; ++q) {
             const bool there = (uint64_t)q < a.queries;
             const int8_t *x = (const int8_t *)a.x + (there ? q : 0) * a.x_stride;
             unit[q] = there ? a.x_scale[q] * 0.0625f : 0.0f;
-            if constexpr (kLong) {
-                for (uint32_t p = threadIdx.x; p < 4 * slots; p += kThreads) {
-                    uint32_t d[2];
-                    split_bytes(x, 8 * p, there ? a.cols : 0, d);
-                    ((uint2 *)shared_digits)[((q * 2 + p % 4 / 2) * (uint64_t)slots + p / 4) * 2 + p % 2] = make_uint2(d[0], d[1]);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t d[2];
-                    split_bytes(x, kSlot * h + 8 * j, there ? a.cols : 0, d);
-                    digits[q][2 * j] = d[0], digits[q][2 * j + 1] = d[1];
-                }
+            for (uint32_t p = threadIdx.x; p < 4 * slots; p += kThreads) {
+                uint32_t d[2];
+                split_bytes(x, 8 * p, there ? a.cols : 0, d);
+                keep(q, p, d[0], d[1]);
             }
         }
-        if constexpr (kLong) __syncthreads();
     }
+    __syncthreads();
+    auto digits_of = [&](uint32_t slot, uint32_t (&d)[kColumns][8]) {
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) {
+            const uint4 lo = shared_digits[(c * 2) * (uint64_t)slots + slot], hi = shared_digits[(c * 2 + 1) * (uint64_t)slots + slot];
+            d[c][0] = lo.x, d[c][1] = lo.y, d[c][2] = lo.z, d[c][3] = lo.w;
+            d[c][4] = hi.x, d[c][5] = hi.y, d[c][6] = hi.z, d[c][7] = hi.w;
+        }
+    };
+    uint32_t d[kColumns][8];
+    if constexpr (!kLong) digits_of(mine ? h : 0, d);
 
     const uint64_t tiles = (a.rows + kRows * kUnroll - 1) / (kRows * kUnroll);
     for (uint64_t tile = (uint64_t)blockIdx.x * kWaves + threadIdx.x / 64; tile < tiles; tile += (uint64_t)gridDim.x * kWaves) {
@@ -185,18 +168,7 @@ __global__ __launch_bounds__(kThreads) void k_score_few(ScoreArgs a) {
                 codes[u] = there ? ((const uint4 *)a.codes)[row * slots + slot] : make_uint4(0, 0, 0, 0);
                 scale[u] = there ? scale_of(a.scales[row * groups + (slot >> shift)]) : 0.0f;
             }
-            uint32_t d[kColumns][8];
-#pragma unroll
-            for (int c = 0; c < kColumns; ++c) {
-                if constexpr (kLong) {
-                    const uint4 lo = shared_digits[(c * 2) * (uint64_t)slots + slot], hi = shared_digits[(c * 2 + 1) * (uint64_t)slots + slot];
-                    d[c][0] = lo.x, d[c][1] = lo.y, d[c][2] = lo.z, d[c][3] = lo.w;
-                    d[c][4] = hi.x, d[c][5] = hi.y, d[c][6] = hi.z, d[c][7] = hi.w;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d[c][j] = digits[c][j];
-                }
-            }
+            if constexpr (kLong) digits_of(slot, d);
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
                 const uint32_t word[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w};
@@ -605,13 +577,14 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantizeArgs a) {
 template <bool kFloat, int kColumns, int kLanes, bool kLong>
 void score_few(const ScoreArgs &a, hipStream_t stream) {
     const uint32_t slots = (a.cols + kSlot - 1) / kSlot;
-    const uint32_t bytes = kLong ? kColumns * 32 * slots : 0;
+    const uint32_t bytes = kColumns * 32 * slots;
     const uint64_t waves = (a.rows + 64 / kLanes - 1) / (64 / kLanes);  // of one load each
     if (waves <= 4096) {  // fewer than four loads for each of four waves on every compute unit: spread them
         k_score_few<kFloat, kColumns, kLanes, 1, kLong><<<(uint32_t)((waves + kWaves - 1) / kWaves), kThreads, bytes, stream>>>(a);
     } else {
-        const uint32_t blocks = (uint32_t)std::min<uint64_t>((waves + 4 * kWaves - 1) / (4 * kWaves), kLong ? 512 : 2048);
-        k_score_few<kFloat, kColumns, kLanes, 4, kLong><<<blocks, kThreads, bytes, stream>>>(a);
+        const uint64_t tiles = (waves + 3) / 4, all = (tiles + kWaves - 1) / kWaves;
+        const uint64_t turns = (all + (kLong ? 1024 : 2048) - 1) / (kLong ? 1024 : 2048);  // of every workgroup, as many of each
+        k_score_few<kFloat, kColumns, kLanes, 4, kLong><<<(uint32_t)((all + turns - 1) / turns), kThreads, bytes, stream>>>(a);
     }
 }
 
