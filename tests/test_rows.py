@@ -559,3 +559,18 @@ def test_on_another_stream_and_in_a_graph(gv):
         assert all(torch.equal(a, b) for a, b in zip(held, want))
         x.mul_(1.5)  # new inputs for the same graph
         want = [t.clone() for t in work()]
+
+
+@gpu
+def test_example_answers_queries(gv):
+    """examples/answer_queries.py on the small community graph: the head learns, and a shortlist of a hundred from the 4-bit
+    table holds nearly all of the best ten (a table of random codes would hold 2 % of them)."""
+    import importlib.util
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "answer_queries.py")
+    spec = importlib.util.spec_from_file_location("answer_queries", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    r = example.run("c4-small", samples=4_000_000, steps=40, queries=4)
+    assert r["last_loss"] < 0.9 * r["first_loss"]
+    assert r["recall"] > 0.9 and r["table_mb"] * 7 < r["rows_mb"] * 1.01
