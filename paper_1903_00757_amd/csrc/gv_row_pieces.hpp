@@ -37,6 +37,26 @@ __device__ __forceinline__ uint32_t largest_of_lanes(uint32_t x) {
     return join_lanes<kLanes>(x, larger);
 }
 
+// Calls take(row, item) for the items of this thread (see Walk).
+template <class Walk, class Take>
+__device__ __forceinline__ void walk_items(const Walk &w, Take &&take) {
+    uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x, row;
+    uint32_t item;
+    if (w.all >> 32 == 0) {
+        row = (uint32_t)i / w.each;
+        item = (uint32_t)i % w.each;
+    } else {
+        row = i / w.each;
+        item = (uint32_t)(i % w.each);
+    }
+    for (; i < w.all; i += w.stride) {
+        take(row, item);
+        row += w.rows_on;
+        item += w.items_on;
+        if (item >= w.each) item -= w.each, ++row;
+    }
+}
+
 // Columns k .. k + 7 of a row as they lie there, 0 past its end: one load or two of 16 bytes wherever the row starts, for
 // a whole piece.  Several are asked for before the first is used.
 template <class T>
@@ -66,8 +86,18 @@ __device__ __forceinline__ void load_piece(const T *row, uint32_t k, uint32_t co
 template <class T>
 __device__ __forceinline__ void store_piece(T *row, uint32_t k, uint32_t cols, const float (&v)[8]) {
     Piece<T> p;
+    if constexpr (sizeof(T) == 2) {  // two at a time: the machine rounds pairs
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        typedef T t2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p.at[i] = (T)v[i];
+        for (int i = 0; i < 8; i += 2) {
+            const t2 pair = __builtin_convertvector((f2{v[i], v[i + 1]}), t2);
+            p.at[i] = pair[0], p.at[i + 1] = pair[1];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p.at[i] = (T)v[i];
+    }
     if (k + 8 <= cols) {
         __builtin_memcpy(row + k, &p, sizeof p);
     } else {

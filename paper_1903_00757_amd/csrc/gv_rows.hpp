@@ -7,6 +7,16 @@
 
 namespace gv {
 
+// Items i = 0, 1, ... of rows of `each` items, taken by threads in turn: a thread goes on by the grid's threads, which are
+// rows_on rows and items_on items (divided on the host).
+struct Walk {
+    uint64_t all, stride, rows_on;
+    uint32_t each, items_on;
+};
+inline Walk walk_of(uint64_t rows, uint32_t each, uint64_t threads) {
+    return {rows * each, threads, threads / each, each, (uint32_t)(threads % each)};
+}
+
 struct DropArgs {
     uint32_t threshold;  // a value is kept when its 16-bit number is not below; 0: all are kept
     float factor;        // of the values that are kept

@@ -203,6 +203,22 @@ def test_refusals_of_tensors(gv):
             call()
 
 
+def test_row_kernels_keep_everything_in_registers(gv):
+    from test_kernel_registers import code_objects, kernels_of
+
+    with open(gv.LIB_PATH, "rb") as f:
+        data = f.read()
+    names = ("k_drop", "k_norm", "k_gain_join", "k_score_few", "k_score_many", "k_score_narrow", "k_quantize")
+    found = {n: 0 for n in names}
+    for elf in code_objects(data):
+        for k in kernels_of(elf):
+            for n in names:
+                if n in k[".name"]:
+                    found[n] += 1
+                    assert k[".vgpr_spill_count"] == 0 and k[".private_segment_fixed_size"] == 0, k[".name"]
+    assert all(found.values()), found
+
+
 # ------------------------------------------------------------------------------------------------ on the GPU
 
 SHAPES = [(1, 1), (1, 128), (3, 7), (5, 8), (257, 31), (64, 32), (100, 64), (33, 96), (1001, 128), (17, 129), (50, 160), (9, 257),
