@@ -403,8 +403,8 @@ int gv_norm_rows(uint64_t rows, uint32_t cols, int type, const void *dev_x, uint
  *   grad_gain[cols] = sum over the rows of grad_out * n (may be NULL; summed in an order that depends on rows and cols
  *   alone, so a call gives the same bits each time).
  * dev_sum is h as gv_norm_rows kept it (x itself, where nothing was added or dropped), dev_rstd what it gave.
- * With grad_gain, dev_workspace points to workspace_bytes bytes (at least those of gv_norm_rows_workspace, aligned to 16)
- * that the call may overwrite.                                                                                */
+ * With grad_gain, dev_workspace points to workspace_bytes bytes (at least those of gv_norm_rows_workspace, which may be
+ * none; aligned to 16) that the call may overwrite.                                                                                */
 int gv_norm_rows_workspace(uint64_t rows, uint32_t cols, uint64_t *bytes);
 int gv_norm_rows_backward(uint64_t rows, uint32_t cols, int type, const void *dev_grad_out, uint64_t grad_out_stride,
                           const void *dev_sum, uint64_t sum_stride, const float *dev_gain, const float *dev_rstd,

@@ -310,6 +310,10 @@ hipError_t by_type(int type, Run &&run) {
 uint32_t norm_grad_parts(uint64_t rows, uint32_t cols) {
     const int lanes = shape_of(cols).lanes, threads = grad_threads_of(lanes);
     const uint64_t each = threads / lanes;
+    // A few turns of one workgroup take less than a launch that joins several (200 rows of 128 through the norm and back: 21 us
+    // among others, 27 with the launch, 37 alone either way; 30 rows of 1000 22 and 27, alone 42 and 38; twice as many turns
+    // 31 and 27 at 128 rows of 357).
+    if (rows <= 4 * each) return 1;
     return (uint32_t)std::min<uint64_t>((rows + each - 1) / each, kGradLanes / threads);
 }
 
@@ -345,10 +349,10 @@ hipError_t launch_norm_grad(const NormGradArgs &args, hipStream_t stream) {
         using T = std::remove_pointer_t<decltype(t)>;
         NormGradArgs a = args;
         const uint32_t parts = norm_grad_parts(a.rows, a.cols);
-        if (parts <= 1) a.partial = a.grad_gain;
+        if (parts == 1) a.partial = a.grad_gain;
         by_shape(a.cols, [&](auto lanes, auto pieces) {
             constexpr int kLanes = decltype(lanes)::value, kPieces = decltype(pieces)::value;
-            k_norm_grad<T, kLanes, kPieces><<<std::max(parts, 1u), grad_threads_of(kLanes), 0, stream>>>(a);
+            k_norm_grad<T, kLanes, kPieces><<<parts, grad_threads_of(kLanes), 0, stream>>>(a);
         });
         if (a.grad_gain && parts > 1) k_gain_join<<<(a.cols + 31) / 32, 1024, 0, stream>>>(a.partial, a.grad_gain, parts, a.cols);
     });

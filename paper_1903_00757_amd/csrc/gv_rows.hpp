@@ -76,7 +76,7 @@ struct ScoreArgs {
     int type;
 };
 
-// how many partial sums of the gain's gradient the backward pass leaves
+// how many partial sums of the gain's gradient the backward pass leaves; one goes to its place at once
 uint32_t norm_grad_parts(uint64_t rows, uint32_t cols);
 
 hipError_t launch_norm(const NormArgs &a, hipStream_t stream);

@@ -55,6 +55,11 @@ int drop_args(const char *call, double drop, uint64_t seed, uint64_t first_row, 
     return GV_OK;
 }
 
+uint64_t workspace_of(uint64_t rows, uint32_t cols) {
+    const uint32_t parts = gv::norm_grad_parts(rows, cols);
+    return parts > 1 ? 4ull * parts * cols : 0;
+}
+
 int launched(const char *call, hipError_t e) {
     return e == hipSuccess ? GV_OK : fail_call(GV_EHIP, "%s: %s", call, hipGetErrorString(e));
 }
@@ -101,7 +106,7 @@ int gv_norm_rows_workspace(uint64_t rows, uint32_t cols, uint64_t *bytes) {
     const char *call = "gv_norm_rows_workspace";
     GV_TRY(check_shape(call, rows, cols, GV_F32, false));
     if (!bytes) return fail_call(GV_EINVAL, "%s: null output", call);
-    *bytes = 4ull * gv::norm_grad_parts(rows, cols) * cols;
+    *bytes = workspace_of(rows, cols);
     return GV_OK;
 }
 
@@ -118,7 +123,7 @@ int gv_norm_rows_backward(uint64_t rows, uint32_t cols, int type, const void *de
     GV_TRY(drop_args(call, drop, seed, first_row, &a.drop));
     if (dev_grad_gain) {
         GV_TRY(check_array(call, "grad_gain", dev_grad_gain, 4));
-        const uint64_t need = 4ull * gv::norm_grad_parts(rows, cols) * cols;
+        const uint64_t need = workspace_of(rows, cols);
         if (need > 0) GV_TRY(check_array(call, "workspace", dev_workspace, 16));
         if (workspace_bytes < need)
             return fail_call(GV_EINVAL, "%s: workspace of %llu bytes: %llu are needed", call, (unsigned long long)workspace_bytes,

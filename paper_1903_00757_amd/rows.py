@@ -179,8 +179,10 @@ def gv_norm_rows_backward(grad_out, sum, gain, rstd, *, grad_sum=None, drop=0.0,
     if keep_gain:
         size = gv_norm_rows_workspace(rows, cols)
         grad_gain = torch.empty_like(gain)
-        space = gain.new_empty(size // 4)
-        gain_to, space_at = grad_gain.data_ptr(), space.data_ptr()
+        gain_to = grad_gain.data_ptr()
+        if size:
+            space = gain.new_empty(size // 4)
+            space_at = space.data_ptr()
     _call(load().gv_norm_rows_backward, gpu, rows, cols, kind, go_at, go_stride, sum_at, sum_stride, gain_at, rstd_at, gs_at,
           gs_stride, drop, seed, first_row, grad_x.data_ptr(), cols, res_at, cols, gain_to, space_at, size)
     return NormGrads(grad_x, grad_residual, grad_gain)

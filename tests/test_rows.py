@@ -172,8 +172,8 @@ def test_refusals(gv):
                                dict(ot=1), dict(ot=3, scale=None), dict(ot=3, scale=a + 2), dict(eps=-1.0), dict(rstd=a + 1),
                                dict(eps=float("nan")), dict(eps=float("inf")), dict(gain=a + 2), dict(type=1, x=a + 1, ot=1)]),
         (back, shapes + odd + [dict(type=3), dict(g=None), dict(s=None), dict(gain=None), dict(rstd=None), dict(gs=7), dict(ds=7),
-                               dict(xs=7), dict(rs=7), dict(w=None), dict(w=a + 4), dict(size=0), dict(gg=a + 2),
-                               dict(rows=0, gg=a + 2)]),
+                               dict(xs=7), dict(rs=7), dict(gg=a + 2), dict(rows=0, gg=a + 2), dict(rows=5000, w=None),
+                               dict(rows=5000, w=a + 4), dict(rows=5000, size=64)]),
         (quantize, shapes + [dict(type=3), dict(group=0), dict(group=16), dict(group=96), dict(x=None), dict(codes=None),
                              dict(scales=None), dict(codes=a + 8), dict(scales=a + 1), dict(xs=7)]),
         (score, shapes + [dict(group=0), dict(group=48), dict(codes=None), dict(codes=a + 4), dict(scales=None), dict(x=None),
@@ -189,7 +189,8 @@ def test_refusals(gv):
     assert score(rows=0, codes=None, outs=0) == score(q=0, x=None) == gv.GV_OK
     assert lib.gv_norm_rows_workspace(10, 0, ctypes.byref(u64)) == gv.GV_EINVAL
     assert lib.gv_norm_rows_workspace(10, 8, None) == gv.GV_EINVAL
-    assert lib.gv_norm_rows_workspace(10, 8, ctypes.byref(u64)) == gv.GV_OK
+    assert lib.gv_norm_rows_workspace(10, 8, ctypes.byref(u64)) == gv.GV_OK and u64.value == 0  # one workgroup: no parts
+    assert lib.gv_norm_rows_workspace(5000, 8, ctypes.byref(u64)) == gv.GV_OK and u64.value > 64
 
 
 def test_refusals_of_tensors(gv):
