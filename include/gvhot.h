@@ -404,7 +404,7 @@ int gv_norm_rows(uint64_t rows, uint32_t cols, int type, const void *dev_x, uint
  *   alone, so a call gives the same bits each time).
  * dev_sum is h as gv_norm_rows kept it (x itself, where nothing was added or dropped), dev_rstd what it gave.
  * With grad_gain, dev_workspace points to workspace_bytes bytes (at least those of gv_norm_rows_workspace, which may be
- * none; aligned to 16) that the call may overwrite.                                                                                */
+ * none; aligned to 16) that the call may overwrite.                                                            */
 int gv_norm_rows_workspace(uint64_t rows, uint32_t cols, uint64_t *bytes);
 int gv_norm_rows_backward(uint64_t rows, uint32_t cols, int type, const void *dev_grad_out, uint64_t grad_out_stride,
                           const void *dev_sum, uint64_t sum_stride, const float *dev_gain, const float *dev_rstd,
@@ -423,9 +423,10 @@ int gv_quantize_rows(uint64_t rows, uint32_t cols, int type, const void *dev_x, 
 /* Scores of `queries` rows x against every row of such a table (any codes -8..7):
  *   out[b][i] = sum over the groups g of scale[i][g] * sum over c in g of code[i][c] * x[b][c],   float, out_stride >= rows
  * x is of `type`; GV_I8 rows stand for x * x_scale[b] (gv_norm_rows gives both; dev_x_scale is NULL otherwise).  The
- * inner sums are whole numbers and exact: x is taken as a 32-bit whole number, in units of 2^-30 of the power of two above the
- * largest |x| of its query (2^-92 at least), and each group is scaled and added in fp32.  A query with a value that is not finite scores NaN
- * everywhere, and so does a row with a NaN scale.  queries <= 65536; queries = 0 is an empty call.              */
+ * inner sums are whole numbers and exact: x is taken as a 32-bit whole number, in units of 2^-30 of the power of two above
+ * the largest |x| of its query (2^-92 at least), and each group is scaled and added in fp32.  A query with a value that
+ * is not finite scores NaN everywhere, and so does a row with a NaN scale.  queries <= 65536; queries = 0 is an empty
+ * call.                                                                                                       */
 int gv_score_rows(uint64_t rows, uint32_t cols, uint32_t group, const uint8_t *dev_codes, const uint16_t *dev_scales,
                   uint64_t queries, int type, const void *dev_x, uint64_t x_stride, const float *dev_x_scale, float *dev_out,
                   uint64_t out_stride, void *stream);
