@@ -424,9 +424,9 @@ int gv_quantize_rows(uint64_t rows, uint32_t cols, int type, const void *dev_x, 
  *   out[b][i] = sum over the groups g of scale[i][g] * sum over c in g of code[i][c] * x[b][c],   float, out_stride >= rows
  * x is of `type`; GV_I8 rows stand for x * x_scale[b] (gv_norm_rows gives both; dev_x_scale is NULL otherwise).  The
  * inner sums are whole numbers and exact: x is taken as a 32-bit whole number, in units of 2^-30 of the power of two above
- * the largest |x| of its query (2^-92 at least), and each group is scaled and added in fp32.  A query with a value that
- * is not finite scores NaN everywhere, and so does a row with a NaN scale.  queries <= 65536; queries = 0 is an empty
- * call.                                                                                                       */
+ * the largest |x| of its query (2^-92 at least), and each group is scaled and added in fp32: a score of finite values
+ * is finite where the sums of its groups' parts are, whatever lies between.  A query with a value that is not finite
+ * scores NaN everywhere, and so does a row with a NaN scale.  queries <= 65536; queries = 0 is an empty call.     */
 int gv_score_rows(uint64_t rows, uint32_t cols, uint32_t group, const uint8_t *dev_codes, const uint16_t *dev_scales,
                   uint64_t queries, int type, const void *dev_x, uint64_t x_stride, const float *dev_x_scale, float *dev_out,
                   uint64_t out_stride, void *stream);

@@ -1,0 +1,97 @@
+"""The operators on rows at the ends of their ranges: values near the ends of fp32, rows without values, tables and batches past
+the sizes at which the kernels change their layout, and what a program around the calls has a right to.
+
+Tolerances (u = 2^-24) are derived as those of test_rows.py are; powers of two that are taken out and put back round nothing."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from test_rows import (U, check, grads_in_64_bits, gv, in_8_bits, keep_mask, make_rows, norm_in_64_bits,  # noqa: F401
+                       norm_tolerance, packed, rounding, scores_in_64_bits)
+
+gpu = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ scores near fp32's ends
+
+# powers of two of the table's scales and of the queries (8-bit queries: of their scales); every score stays inside fp32
+REACHES = {"f32": [(88, 0), (105, -10), (124, -60), (126, -85), (-100, 60), (-132, 80), (-20, 115), (-60, 123), (0, 100)],
+           "f16": [(88, 0), (110, -8), (120, -12), (-100, 8), (-132, 8)],
+           "i8": [(88, 0), (112, -20), (126, -60), (126, -140), (40, -140), (-100, 100), (-132, 126), (0, 98)]}
+REACHES["bf16"] = REACHES["f32"]
+
+
+@gpu
+@pytest.mark.parametrize("rows, cols, group", [(300, 32, 32), (300, 60, 32), (300, 64, 64), (300, 128, 32), (301, 200, 64),
+                                               (200, 544, 128), (40, 2100, 64)])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16", "i8"])
+def test_scores_reach_as_far_as_their_results(gv, rows, cols, group, kind):
+    import torch
+
+    rng = np.random.default_rng(rows + cols + group)
+    dtype = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16, "i8": torch.int8}[kind]
+    codes = rng.integers(-8, 8, (rows, cols))
+    codes_t = torch.from_numpy(packed(codes)).cuda()
+    for of_table, of_query in REACHES[kind]:
+        scale_t = torch.from_numpy(np.ldexp(rng.uniform(1, 2, (rows, -(-cols // group))), of_table).astype(np.float32)).to(torch.bfloat16)
+        scales = scale_t.double().numpy()
+        for queries in (1, 2, 4, 7, 20, 40):
+            if kind == "i8":
+                t = torch.from_numpy(rng.integers(-127, 128, (queries, cols)).astype(np.int8))
+                x_scale = torch.from_numpy(np.ldexp(rng.uniform(1, 2, queries), of_query).astype(np.float32))
+                x = t.double().numpy() * x_scale.double().numpy()[:, None]
+                x_scale = x_scale.cuda()
+            else:
+                t = torch.from_numpy(np.ldexp(rng.standard_normal((queries, cols)), of_query)).to(dtype)
+                x, x_scale = t.double().numpy(), None
+            want, sums, weights = scores_in_64_bits(codes, scales, group, x)
+            tolerance = (scales.shape[1] + 8) * U * sums + 2.0 ** -28 * np.abs(x).max(1, keepdims=True) * weights[None, :]
+            # no sum leaves fp32, and terms that are subnormal (off by 2^-150) stay inside one of the roundings of the tolerance
+            assert sums.max() < 2.0 ** 127 and scales.shape[1] * 2.0 ** -150 < U * sums.min()
+            got = gv.gv_score_rows(codes_t, scale_t.cuda(), t.cuda(), group=group, scale=x_scale)
+            check(got, want, tolerance, (of_table, of_query, queries))
+
+
+@gpu
+def test_scores_of_a_table_of_large_rows(gv):
+    import torch
+
+    codes = torch.full((50, 16), 0x77, dtype=torch.uint8, device="cuda")
+    scales = torch.full((50, 1), 2.0 ** 88, dtype=torch.bfloat16, device="cuda")
+    for queries in (1, 3, 20):
+        got = gv.gv_score_rows(codes, scales, torch.ones(queries, 32, device="cuda"))
+        assert (got == 7.0 * 32 * 2.0 ** 88).all()
+    rows = torch.from_numpy(np.random.default_rng(4).standard_normal((400, 512)).astype(np.float32)).cuda()
+    x = torch.from_numpy(np.random.default_rng(5).standard_normal((9, 512)).astype(np.float32)).cuda()
+    small, large = gv.gv_quantize_rows(rows), gv.gv_quantize_rows(rows * 2.0 ** 93)  # up to 3e28
+    assert torch.equal(small[0], large[0])
+    for queries in (1, 9):
+        got = gv.gv_score_rows(*large, x[:queries])
+        assert torch.isfinite(got).all() and torch.equal(got * 2.0 ** -93, gv.gv_score_rows(*small, x[:queries]))
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["f32", "i8"])
+def test_scores_of_large_rows_beside_rows_that_are_not_finite(gv, kind):
+    """A row that is not finite, an ordinary one and one whose joined groups leave fp32 do not change each other's scores."""
+    import torch
+
+    rng = np.random.default_rng(12)
+    rows, cols, group = 150, 200, 32
+    codes = torch.from_numpy(packed(rng.integers(-8, 8, (rows, cols)))).cuda()
+    scales = torch.from_numpy(np.exp(rng.standard_normal((rows, 7))).astype(np.float32)).to(torch.bfloat16).cuda()
+    for queries in (1, 4, 16, 20, 40):
+        x = torch.from_numpy(rng.integers(-127, 128, (queries, cols)).astype(np.int8 if kind == "i8" else np.float32)).cuda()
+        x_scale = torch.from_numpy(np.exp(rng.standard_normal(queries) - 20).astype(np.float32)).cuda() if kind == "i8" else None
+        x = x if kind == "i8" else x * 2.0 ** -30
+        plain = gv.gv_score_rows(codes, scales, x, group=group, scale=x_scale)
+        mixed = scales.clone()
+        mixed[3::7] *= 2.0 ** 110
+        mixed[5::7, 4] = float("nan")
+        mixed[6::14, 2] = float("inf")
+        got = gv.gv_score_rows(codes, mixed, x, group=group, scale=x_scale)
+        assert torch.isfinite(plain).all() and torch.isnan(got[:, 5::7]).all() and not torch.isfinite(got[:, 6::14]).any()
+        assert torch.equal(got[:, 3::7] * 2.0 ** -110, plain[:, 3::7])
+        for lo in (0, 1, 2, 4):
+            assert torch.equal(got[:, lo::7], plain[:, lo::7])
