@@ -77,10 +77,12 @@ __device__ __forceinline__ uint32_t row_largest(uint32_t x, uint32_t (*scratch)[
     return all;
 }
 
-// 1 / sqrt(x), within one unit in the last place; the instruction takes no subnormal x
+// 1 / sqrt(x), within one unit in the last place; the instruction takes no subnormal x.  0 for 0: the norm of a row without
+// values is such a row, with any eps, and its gradients pass nothing on.
 __device__ __forceinline__ float inverse_root(float x) {
     const bool small = x < 0x1p-100f;
-    return __builtin_amdgcn_rsqf(small ? x * 0x1p64f : x) * (small ? 0x1p32f : 1.0f);
+    const float root = __builtin_amdgcn_rsqf(small ? x * 0x1p64f : x) * (small ? 0x1p32f : 1.0f);
+    return x == 0.0f ? 0.0f : root;
 }
 
 // The norm.  The sum of squares and the largest |h gain| of a row are joined over its lanes by register exchanges (a

@@ -95,3 +95,50 @@ def test_scores_of_large_rows_beside_rows_that_are_not_finite(gv, kind):
         assert torch.equal(got[:, 3::7] * 2.0 ** -110, plain[:, 3::7])
         for lo in (0, 1, 2, 4):
             assert torch.equal(got[:, lo::7], plain[:, lo::7])
+
+
+# ------------------------------------------------------------------------------------------------ rows without values
+
+
+@gpu
+@pytest.mark.parametrize("cols", [8, 31, 130, 700, 1500, 3000, 9000])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_empty_rows_without_eps(gv, cols, kind):
+    """A row whose values are all 0 (where dropout left none, too) gives 0 with any eps, and does not spoil the gain's gradient."""
+    import torch
+
+    rng = np.random.default_rng(cols)
+    rows, p = (1500, 0.6) if cols == 8 else (9, 0.25)
+    t, x = make_rows(torch, rng, rows, cols, kind)
+    grad_t, grad = make_rows(torch, rng, rows, cols, kind)
+    more_t, more = make_rows(torch, rng, rows, cols, kind)
+    t[[0, rows - 2]] = 0
+    x[[0, rows - 2]] = 0
+    gain = torch.from_numpy(rng.standard_normal(cols).astype(np.float32)).cuda()
+    g = gain.double().cpu().numpy()
+    kept = keep_mask(rows, cols, p, 31, 7)
+    h = np.where(kept[0], x * kept[1], 0.0)
+    empty = ~h.any(1)
+    assert empty.sum() >= (10 if cols == 8 else 2) and not empty.all()
+    args = dict(drop=p, seed=31, first_row=7)
+    got = gv.gv_norm_rows(t, gain, eps=0.0, keep_rstd=True, **args)
+    rstd = got.rstd.double().cpu().numpy()
+    assert (rstd[empty] == 0).all() and (got.out[torch.from_numpy(empty).cuda()] == 0).all() and torch.isfinite(got.out).all()
+    some = h[~empty]
+    want = 1 / np.sqrt((some * some).mean(1))
+    assert np.all(np.abs(rstd[~empty] - want) <= 48 * U * want)
+    rel, least = rounding(kind)
+    kept_h = got.sum.double().cpu().numpy()
+    rs = rstd[:, None]
+    dx, dh, dg = grads_in_64_bits(grad, kept_h, g, rs, more, kept)
+    grads = gv.gv_norm_rows_backward(grad_t, got.sum, gain, got.rstd, grad_sum=more_t, **args)
+    n, u = kept_h * rs, grad * g
+    off = rs * (4 * U * np.abs(u) + 88 * U * np.abs(n) * np.abs(u * n).mean(1, keepdims=True)) + 3 * U * np.abs(dh)
+    off += 1.01 * rel * (np.abs(dh) + off) + least
+    if kind == "f16":  # the gradient of a row of one small value may pass half's largest
+        off[np.abs(dh) > 65000] = np.inf
+    check(grads.residual, dh, off, "residual")
+    check(grads.gain, dg, (min(rows, 1100) + 4) * U * np.abs(grad * n).sum(0), "gain")
+    assert torch.equal(grads.residual[0], more_t[0])
+    codes = gv.gv_norm_rows(t, gain, eps=0.0, out_type=torch.int8, **args)
+    assert (codes.out[torch.from_numpy(empty).cuda()] == 0).all() and (codes.scale[torch.from_numpy(empty).cuda()] == 0).all()
