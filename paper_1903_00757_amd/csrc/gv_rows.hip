@@ -52,8 +52,8 @@ __global__ __launch_bounds__(kDropThreads) void k_drop(DropRowsArgs a, Walk walk
 constexpr int kMostLanes = 512;
 constexpr int threads_of(int lanes) { return lanes > 64 ? lanes : 256; }
 
-// Sums over the lanes of a row; all of them get the result.  A whole workgroup's: `turn` says which half of the scratch
-// this row takes, so that one barrier a row is enough.
+// Sums over the lanes of a row; all of them get the result.  A whole workgroup's: `turn` says which part of the scratch
+// this row takes, 0 and 1 in turn, so that one barrier a row is enough (2: a second sum of the same row).
 template <int kLanes>
 __device__ __forceinline__ float row_sum(float x, float (*scratch)[kMostLanes / 64], int turn) {
     if constexpr (kLanes <= 64) return sum_lanes<kLanes>(x);
@@ -91,7 +91,7 @@ __device__ __forceinline__ float inverse_root(float x) {
 template <class T, int kLanes, int kPieces, bool kBytes>
 __global__ __launch_bounds__(threads_of(kLanes)) void k_norm(NormArgs a) {
     constexpr int kRows = threads_of(kLanes) / kLanes;
-    __shared__ float sums[2][kMostLanes / 64];
+    __shared__ float sums[3][kMostLanes / 64];
     __shared__ uint32_t tops[2][kMostLanes / 64];
     const uint32_t lane = threadIdx.x % kLanes;
     float gain[kPieces][8];
@@ -124,7 +124,21 @@ __global__ __launch_bounds__(threads_of(kLanes)) void k_norm(NormArgs a) {
                 if (kBytes) top = larger(top, __float_as_uint(h[p][i] * gain[p][i]) & 0x7FFFFFFFu);
             }
         squares = row_sum<kLanes>(squares, sums, turn);
-        const float rstd = inverse_root(squares / (float)a.cols + a.eps);
+        const float power = squares / (float)a.cols + a.eps;
+        float rstd = inverse_root(power);
+        if (!(power < __builtin_inff()) || power < 0x1p-100f) {
+            // Squares that left the range of fp32 are taken again, of values times a power of two: values below 2^56, of which
+            // 16384 squares are below 2^126, or values below 2^53 whose least square is normal.  A row's lanes come here together.
+            const float scale = power < 0x1p-100f ? 0x1p96f : 0x1p-72f;
+            squares = 0.0f;
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) squares = fmaf(h[p][i] * scale, h[p][i] * scale, squares);
+            squares = row_sum<kLanes>(squares, sums, 2);
+            rstd = inverse_root(squares / (float)a.cols + a.eps * scale * scale) * scale;
+            if (rstd == __builtin_inff()) rstd = 0.0f;
+        }
         if (a.rstd && lane == 0) a.rstd[row] = rstd;
         if (a.sum) {
 #pragma unroll

@@ -142,3 +142,58 @@ def test_empty_rows_without_eps(gv, cols, kind):
     assert torch.equal(grads.residual[0], more_t[0])
     codes = gv.gv_norm_rows(t, gain, eps=0.0, out_type=torch.int8, **args)
     assert (codes.out[torch.from_numpy(empty).cuda()] == 0).all() and (codes.scale[torch.from_numpy(empty).cuda()] == 0).all()
+
+
+# ------------------------------------------------------------------------------------------------ rows whose squares leave fp32
+
+
+@gpu
+@pytest.mark.parametrize("cols", [1, 8, 31, 130, 700, 1500, 3000, 9000, 16384])
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_norm_of_rows_whose_squares_leave_the_range(gv, cols, kind):
+    import torch
+
+    rng = np.random.default_rng(cols + 1)
+    exponents = [70, 0, 122, 63, -40, -75, -110, -60, 90, 55]
+    rows = len(exponents)
+    t, x = make_rows(torch, rng, rows, cols, kind)
+    x = np.ldexp(np.clip(x, -8, 8) + 2.0 ** -6, np.array(exponents)[:, None])
+    t.copy_(torch.from_numpy(x))
+    grad_t, grad = make_rows(torch, rng, rows, cols, kind)
+    x = t.double().cpu().numpy()
+    gain = torch.from_numpy(rng.uniform(0.5, 1, cols).astype(np.float32)).cuda()
+    g = gain.double().cpu().numpy()
+    for eps in (0.0, 1e-6):
+        _, rstd, y = norm_in_64_bits(x, None, g, float(np.float32(eps)), None)
+        got = gv.gv_norm_rows(t, gain, eps=eps, keep_rstd=True)
+        check(got.rstd, rstd[:, 0], 48 * U * rstd[:, 0], "rstd")
+        check(got.out, y, norm_tolerance(kind, y, x, g, rstd, None) + 2.0 ** -126, "out")
+        codes, step = in_8_bits(x, None, gain.cpu().numpy())
+        eighth = gv.gv_norm_rows(t, gain, eps=eps, out_type=torch.int8)
+        assert np.array_equal(eighth.out.cpu().numpy(), codes)
+        check(eighth.scale, step * rstd[:, 0], 50 * U * step * rstd[:, 0] + 2.0 ** -126, "scale")
+    # back through the rows whose gradients are inside fp32
+    some = [i for i, e in enumerate(exponents) if -80 < e]
+    rs = rstd[some].astype(np.float32).astype(np.float64)
+    _, dh, dg = grads_in_64_bits(grad[some], x[some], g, rs, None, None)
+    back = gv.gv_norm_rows_backward(grad_t[some], t[some], gain, torch.from_numpy(rs[:, 0].astype(np.float32)).cuda())
+    n, u = x[some] * rs, grad[some] * g
+    off = rs * (4 * U * np.abs(u) + 88 * U * np.abs(n) * np.abs(u * n).mean(1, keepdims=True)) + 3 * U * np.abs(dh)
+    check(back.x, dh, off + 1.01 * rounding(kind)[0] * (np.abs(dh) + off) + 2.0 ** -126, "x")
+    check(back.gain, dg, (rows + 4) * U * np.abs(grad[some] * n).sum(0), "gain")
+
+
+@gpu
+def test_norm_of_rows_that_are_too_small_for_their_inverse(gv):
+    """1 / sqrt(mean(h^2)) has no float below 2^-128: such a row counts as empty."""
+    import torch
+
+    for cols in (8, 700, 3000):
+        x = torch.full((3, cols), 2.0 ** -140, device="cuda")
+        x[1] = 1.0
+        got = gv.gv_norm_rows(x, torch.ones(cols, device="cuda"), eps=0.0, keep_rstd=True)
+        assert (got.out[[0, 2]] == 0).all() and (got.rstd[[0, 2]] == 0).all() and (got.out[1] == 1).all()
+        x[2] = float("nan")
+        x[0, 0] = float("inf")
+        got = gv.gv_norm_rows(x, torch.ones(cols, device="cuda"), eps=0.0, keep_rstd=True)
+        assert torch.isnan(got.rstd[2]) and torch.isnan(got.out[2]).all() and torch.isnan(got.out[0, 0]) and (got.out[1] == 1).all()
