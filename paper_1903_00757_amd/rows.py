@@ -2,6 +2,10 @@
 from the tensors, results that the caller does not pass are allocated, and the kernels go to torch's current stream
 of the tensors' GPU.  Rows are 2-D tensors whose last dimension is contiguous; their rows may lie further apart.
 No arithmetic happens here.
+
+The calls record no graph for autograd: gradients are calls of their own (gv_norm_rows_backward; dropout's is dropout).  So
+where gradients are enabled and a tensor of a floating result asks for one, a call refuses: it belongs under torch.no_grad(), or
+takes detached tensors.  Codes, of 8-bit rows and of tables, are constants.
 """
 from __future__ import annotations
 
@@ -39,11 +43,18 @@ def _refuse(text):
     raise ValueError(text)
 
 
+def _without_graph(*tensors):
+    if any(t is not None and t.requires_grad for t in tensors):
+        _refuse("no graph is recorded here, and a tensor asks for gradients: call under torch.no_grad() or pass it detached "
+                "(gradients are calls of their own: gv_norm_rows_backward, gv_drop_rows)")
+
+
 # A call that finds its kernel's launch waiting for nothing is as long as the host takes for it, 3.5 us of which are the launch:
 # so torch is asked in the ways that take it least.  The current stream of a GPU as an address, and the current GPU:
 # the public ways make a Stream object and look whether torch is initialised first (1.9 and 0.25 us instead of 0.1 each).
 _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda gpu: torch.cuda.current_stream(gpu).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_recording = torch.is_grad_enabled
 _f32, _int8, _uint8, _bf16 = torch.float32, torch.int8, torch.uint8, torch.bfloat16
 
 
@@ -97,11 +108,14 @@ def _like(x, rows, cols):
 def gv_drop_rows(x, drop, seed, *, first_row=0, out=None):
     """Dropout of rows.  The gradient of x is the same call, with the same drop, seed and first_row, on out's gradient."""
     at, stride, rows, cols, kind, gpu = _first("x", x)
-    if out is None:
+    passed = out is not None
+    if _recording() and (x.requires_grad or passed):
+        _without_graph(x, out)
+    if passed:
+        out_at, out_stride = _rows("out", out, rows, cols, x.dtype, gpu)
+    else:
         out = _like(x, rows, cols)
         out_at, out_stride = out.data_ptr(), cols
-    else:
-        out_at, out_stride = _rows("out", out, rows, cols, x.dtype, gpu)
     _call(load().gv_drop_rows, gpu, rows, cols, kind, at, stride, drop, seed, first_row, out_at, out_stride)
     return out
 
@@ -114,6 +128,7 @@ def gv_norm_rows(x, gain, residual=None, *, eps=1e-6, drop=0.0, seed=0, first_ro
     dtype = x.dtype
     gain_at = _array("gain", gain, cols, _f32, gpu)
     res_at, res_stride = (None, 0) if residual is None else _rows("residual", residual, rows, cols, dtype, gpu)
+    passed = (out, scale, sum) if out is not None or scale is not None or sum is not None else ()
     if out is None:
         out_type = out_type or dtype
         out = _like(x, rows, cols) if out_type is dtype else x.new_empty((rows, cols), dtype=out_type)
@@ -142,6 +157,12 @@ def gv_norm_rows(x, gain, residual=None, *, eps=1e-6, drop=0.0, seed=0, first_ro
     if keep_rstd:
         rstd = gain.new_empty(rows)
         rstd_at = rstd.data_ptr()
+    if _recording() and (passed or x.requires_grad or gain.requires_grad or (residual is not None and residual.requires_grad)):
+        _without_graph(*passed)
+        if out_type is not _int8:
+            _without_graph(x, residual, gain)
+        elif sum is not None:
+            _without_graph(x, residual)
     _call(load().gv_norm_rows, gpu, rows, cols, kind, at, stride, res_at, res_stride, gain_at, eps, drop, seed, first_row,
           sum_at, sum_stride, out_kind, out_at, out_stride, scale_at, rstd_at)
     return NormRows(out, scale, sum, rstd)
@@ -167,6 +188,9 @@ def gv_norm_rows_backward(grad_out, sum, gain, rstd, *, grad_sum=None, drop=0.0,
     gs_at, gs_stride = (None, 0) if grad_sum is None else _rows("grad_sum", grad_sum, rows, cols, dtype, gpu)
     gain_at = _array("gain", gain, cols, _f32, gpu)
     rstd_at = _array("rstd", rstd, rows, _f32, gpu)
+    if _recording() and (grad_out.requires_grad or sum.requires_grad or gain.requires_grad or rstd.requires_grad
+                         or (grad_sum is not None and grad_sum.requires_grad)):
+        _without_graph(grad_out, sum, gain, rstd, grad_sum)
     grad_x = _like(grad_out, rows, cols)
     grad_residual = res_at = grad_gain = gain_to = space_at = None
     size = 0
@@ -208,12 +232,15 @@ def gv_score_rows(codes, scales, x, *, group=32, scale=None, out=None):
     rows = codes.shape[0]
     codes_at = _array("codes", codes, rows * 16 * _parts(cols, 32), _uint8, gpu)
     scales_at = _array("scales", scales, rows * _parts(cols, group), _bf16, gpu)
-    if out is None:
+    passed = out is not None
+    if passed:
+        out_at, out_stride = _rows("out", out, queries, rows, _f32, gpu)
+    else:
         out = (x if scale is None else scale).new_empty((queries, rows), dtype=_f32)
         out_at, out_stride = out.data_ptr(), rows
-    else:
-        out_at, out_stride = _rows("out", out, queries, rows, _f32, gpu)
     scale_at = None if scale is None else _array("scale", scale, queries, _f32, gpu)
+    if _recording() and (passed or x.requires_grad or scales.requires_grad or (scale is not None and scale.requires_grad)):
+        _without_graph(x, scales, scale, out)
     _call(load().gv_score_rows, gpu, rows, cols, group, codes_at, scales_at, queries, kind, at, stride, scale_at, out_at,
           out_stride)
     return out

@@ -197,3 +197,36 @@ def test_norm_of_rows_that_are_too_small_for_their_inverse(gv):
         x[0, 0] = float("inf")
         got = gv.gv_norm_rows(x, torch.ones(cols, device="cuda"), eps=0.0, keep_rstd=True)
         assert torch.isnan(got.rstd[2]) and torch.isnan(got.out[2]).all() and torch.isnan(got.out[0, 0]) and (got.out[1] == 1).all()
+
+
+# ------------------------------------------------------------------------------------------------ in a program with autograd
+
+
+@gpu
+def test_inputs_that_ask_for_gradients_are_refused(gv):
+    """The calls record no graph: where torch would have to, they refuse instead of dropping the gradient."""
+    import torch
+
+    x, r = torch.randn(6, 32, device="cuda"), torch.randn(6, 32, device="cuda")
+    gain = torch.nn.Parameter(torch.ones(32, device="cuda"))
+    plain = gain.detach()
+    wants = torch.randn(6, 32, device="cuda", requires_grad=True)
+    later = wants * 2
+    codes, scales = gv.gv_quantize_rows(torch.randn(40, 32, device="cuda"))
+    y = gv.gv_norm_rows(x, plain, r, keep_rstd=True)
+    for call in (lambda: gv.gv_norm_rows(x, gain), lambda: gv.gv_norm_rows(wants, plain), lambda: gv.gv_norm_rows(x, plain, later),
+                 lambda: gv.gv_norm_rows(x, plain, out=wants), lambda: gv.gv_norm_rows(x, plain, r, sum=wants),
+                 lambda: gv.gv_drop_rows(later, 0.1, 1), lambda: gv.gv_drop_rows(x, 0.1, 1, out=wants),
+                 lambda: gv.gv_norm_rows_backward(later, y.sum, plain, y.rstd), lambda: gv.gv_norm_rows_backward(x, y.sum, gain, y.rstd),
+                 lambda: gv.gv_norm_rows_backward(x, wants, plain, y.rstd),
+                 lambda: gv.gv_norm_rows_backward(x, y.sum, plain, y.rstd, grad_sum=later),
+                 lambda: gv.gv_score_rows(codes, scales, later)):
+        with pytest.raises(ValueError, match="no_grad"):
+            call()
+    with torch.no_grad():
+        assert torch.equal(gv.gv_norm_rows(x, gain, r).out, y.out) and gv.gv_drop_rows(later, 0.1, 1).shape == x.shape
+        assert gv.gv_score_rows(codes, scales, later).shape == (6, 40)
+        assert gv.gv_norm_rows_backward(x, y.sum, gain, y.rstd).gain.shape == (32,)
+    # codes are constants, as every whole number of torch is
+    assert not gv.gv_norm_rows(x, gain, out_type=torch.int8).scale.requires_grad
+    assert torch.equal(gv.gv_quantize_rows(later)[0], gv.gv_quantize_rows(later.detach())[0])
