@@ -55,6 +55,8 @@ def _without_graph(*tensors):
 _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda gpu: torch.cuda.current_stream(gpu).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _recording = torch.is_grad_enabled
+# a passed tensor that was written to: autograd raises where it had kept what was there
+_written = torch.autograd.graph.increment_version
 _f32, _int8, _uint8, _bf16 = torch.float32, torch.int8, torch.uint8, torch.bfloat16
 
 
@@ -117,6 +119,8 @@ def gv_drop_rows(x, drop, seed, *, first_row=0, out=None):
         out = _like(x, rows, cols)
         out_at, out_stride = out.data_ptr(), cols
     _call(load().gv_drop_rows, gpu, rows, cols, kind, at, stride, drop, seed, first_row, out_at, out_stride)
+    if passed:
+        _written(out)
     return out
 
 
@@ -165,6 +169,8 @@ def gv_norm_rows(x, gain, residual=None, *, eps=1e-6, drop=0.0, seed=0, first_ro
             _without_graph(x, residual)
     _call(load().gv_norm_rows, gpu, rows, cols, kind, at, stride, res_at, res_stride, gain_at, eps, drop, seed, first_row,
           sum_at, sum_stride, out_kind, out_at, out_stride, scale_at, rstd_at)
+    if passed:
+        _written([t for t in passed if t is not None])
     return NormRows(out, scale, sum, rstd)
 
 
@@ -243,4 +249,6 @@ def gv_score_rows(codes, scales, x, *, group=32, scale=None, out=None):
         _without_graph(x, scales, scale, out)
     _call(load().gv_score_rows, gpu, rows, cols, group, codes_at, scales_at, queries, kind, at, stride, scale_at, out_at,
           out_stride)
+    if passed:
+        _written(out)
     return out

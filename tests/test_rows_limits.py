@@ -230,3 +230,28 @@ def test_inputs_that_ask_for_gradients_are_refused(gv):
     # codes are constants, as every whole number of torch is
     assert not gv.gv_norm_rows(x, gain, out_type=torch.int8).scale.requires_grad
     assert torch.equal(gv.gv_quantize_rows(later)[0], gv.gv_quantize_rows(later.detach())[0])
+
+
+@gpu
+def test_autograd_sees_what_is_overwritten(gv):
+    import torch
+
+    x, gain = torch.randn(6, 32, device="cuda"), torch.ones(32, device="cuda")
+
+    def fails_after(write):
+        """A saved tensor that `write` goes over makes the backward pass raise."""
+        saved, leaf = torch.randn(6, 32, device="cuda"), torch.ones(6, 32, device="cuda", requires_grad=True)
+        loss = (leaf * saved).sum()
+        write(saved)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+
+    fails_after(lambda s: gv.gv_drop_rows(s, 0.5, 1, out=s))
+    fails_after(lambda s: gv.gv_norm_rows(x, gain, out=s))
+    fails_after(lambda s: gv.gv_norm_rows(x, gain, s, sum=s))
+    fails_after(lambda s: gv.gv_score_rows(*gv.gv_quantize_rows(torch.randn(32, 32, device="cuda")), x, out=s))
+    scale = torch.empty(6, device="cuda")
+    before = scale._version
+    codes = gv.gv_norm_rows(x, gain, out_type=torch.int8, scale=scale)
+    assert scale._version > before and codes.scale is scale
+    assert gv.gv_norm_rows(x, gain).out._version == 0 and x._version == 0  # inputs and new results are not touched
