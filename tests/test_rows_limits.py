@@ -255,3 +255,30 @@ def test_autograd_sees_what_is_overwritten(gv):
     codes = gv.gv_norm_rows(x, gain, out_type=torch.int8, scale=scale)
     assert scale._version > before and codes.scale is scale
     assert gv.gv_norm_rows(x, gain).out._version == 0 and x._version == 0  # inputs and new results are not touched
+
+
+# ------------------------------------------------------------------------------------------------ the package and the runtime around it
+
+
+def test_the_package_is_imported_without_torch(gv):
+    """Constants, the list of exports and the build need no torch; the names of rows.py are there all the same."""
+    import os
+    import subprocess
+    import sys
+
+    from paper_1903_00757_amd import rows
+
+    code = ("import sys; sys.modules['torch'] = None\n"  # an import of torch raises
+            "import paper_1903_00757_amd as gv, paper_1903_00757_amd.build as b\n"
+            "assert gv.GV_BF16 == 1 and 'gv_drop_rows' in gv.EXPORTS and b.SOURCES\n"
+            "assert 'gv_drop_rows' in dir(gv)\n"
+            "try: gv.gv_norm_rows\n"
+            "except ImportError: print('needs torch')\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(gv.__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert done.returncode == 0 and done.stdout == "needs torch\n", done.stderr
+    names = {}
+    exec("from paper_1903_00757_amd import *", names)
+    for name in rows.__all__:
+        assert getattr(gv, name) is getattr(rows, name) and names[name] is getattr(rows, name)
+    assert names["gv_create"] is gv.gv_create and gv.rows is rows and not hasattr(gv, "gv_no_such_call")
