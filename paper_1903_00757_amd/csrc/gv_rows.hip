@@ -292,33 +292,32 @@ Shape shape_of(uint32_t cols) {
 }
 
 template <int kLanes, int kPieces, class Run>
-void with_shape(Run &&run) {
-    run(std::integral_constant<int, kLanes>(), std::integral_constant<int, kPieces>());
+hipError_t with_shape(Run &&run) {
+    return run(std::integral_constant<int, kLanes>(), std::integral_constant<int, kPieces>());
 }
 template <class Run>
-void by_shape(uint32_t cols, Run &&run) {
+hipError_t by_shape(uint32_t cols, Run &&run) {
     const Shape s = shape_of(cols);
-    if (s.lanes == 1) with_shape<1, 1>(run);
-    else if (s.lanes == 2) with_shape<2, 1>(run);
-    else if (s.lanes == 4) with_shape<4, 1>(run);
-    else if (s.lanes == 8 && s.pieces == 1) with_shape<8, 1>(run);
-    else if (s.lanes == 8) with_shape<8, 2>(run);
-    else if (s.lanes == 16) with_shape<16, 2>(run);
-    else if (s.lanes == 32) with_shape<32, 2>(run);
-    else if (s.lanes == 64) with_shape<64, 2>(run);
-    else if (s.lanes == 256) with_shape<256, 1>(run);
-    else if (s.pieces == 1) with_shape<kMostLanes, 1>(run);
-    else if (s.pieces == 2) with_shape<kMostLanes, 2>(run);
-    else if (s.pieces == 3) with_shape<kMostLanes, 3>(run);
-    else with_shape<kMostLanes, 4>(run);
+    if (s.lanes == 1) return with_shape<1, 1>(run);
+    if (s.lanes == 2) return with_shape<2, 1>(run);
+    if (s.lanes == 4) return with_shape<4, 1>(run);
+    if (s.lanes == 8 && s.pieces == 1) return with_shape<8, 1>(run);
+    if (s.lanes == 8) return with_shape<8, 2>(run);
+    if (s.lanes == 16) return with_shape<16, 2>(run);
+    if (s.lanes == 32) return with_shape<32, 2>(run);
+    if (s.lanes == 64) return with_shape<64, 2>(run);
+    if (s.lanes == 256) return with_shape<256, 1>(run);
+    if (s.pieces == 1) return with_shape<kMostLanes, 1>(run);
+    if (s.pieces == 2) return with_shape<kMostLanes, 2>(run);
+    if (s.pieces == 3) return with_shape<kMostLanes, 3>(run);
+    return with_shape<kMostLanes, 4>(run);
 }
 
 template <class Run>
 hipError_t by_type(int type, Run &&run) {
-    if (type == GV_F32) run((float *)nullptr);
-    else if (type == GV_BF16) run((__bf16 *)nullptr);
-    else run((_Float16 *)nullptr);
-    return hipGetLastError();
+    if (type == GV_F32) return run((float *)nullptr);
+    if (type == GV_BF16) return run((__bf16 *)nullptr);
+    return run((_Float16 *)nullptr);
 }
 
 }  // namespace
@@ -343,19 +342,19 @@ hipError_t launch_drop(const DropRowsArgs &a, hipStream_t stream) {
     const uint32_t blocks = (uint32_t)std::min<uint64_t>((a.rows * pieces + kDropThreads - 1) / kDropThreads, kMostBlocks);
     return by_type(a.type, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        k_drop<T><<<blocks, kDropThreads, 0, stream>>>(a, walk_of(a.rows, pieces, (uint64_t)blocks * kDropThreads));
+        return launch(k_drop<T>, blocks, kDropThreads, 0, stream, a, walk_of(a.rows, pieces, (uint64_t)blocks * kDropThreads));
     });
 }
 
 hipError_t launch_norm(const NormArgs &a, hipStream_t stream) {
     return by_type(a.type, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        by_shape(a.cols, [&](auto lanes, auto pieces) {
+        return by_shape(a.cols, [&](auto lanes, auto pieces) {
             constexpr int kLanes = decltype(lanes)::value, kPieces = decltype(pieces)::value, kThreads = threads_of(kLanes);
             constexpr uint64_t kRows = kThreads / kLanes;
             const uint32_t blocks = (uint32_t)std::min<uint64_t>((a.rows + kRows - 1) / kRows, kMostBlocks);
-            if (a.out_type == GV_I8) k_norm<T, kLanes, kPieces, true><<<blocks, kThreads, 0, stream>>>(a);
-            else k_norm<T, kLanes, kPieces, false><<<blocks, kThreads, 0, stream>>>(a);
+            if (a.out_type == GV_I8) return launch(k_norm<T, kLanes, kPieces, true>, blocks, kThreads, 0, stream, a);
+            return launch(k_norm<T, kLanes, kPieces, false>, blocks, kThreads, 0, stream, a);
         });
     });
 }
@@ -366,11 +365,12 @@ hipError_t launch_norm_grad(const NormGradArgs &args, hipStream_t stream) {
         NormGradArgs a = args;
         const uint32_t parts = norm_grad_parts(a.rows, a.cols);
         if (parts == 1) a.partial = a.grad_gain;
-        by_shape(a.cols, [&](auto lanes, auto pieces) {
+        const hipError_t e = by_shape(a.cols, [&](auto lanes, auto pieces) {
             constexpr int kLanes = decltype(lanes)::value, kPieces = decltype(pieces)::value;
-            k_norm_grad<T, kLanes, kPieces><<<parts, grad_threads_of(kLanes), 0, stream>>>(a);
+            return launch(k_norm_grad<T, kLanes, kPieces>, parts, grad_threads_of(kLanes), 0, stream, a);
         });
-        if (a.grad_gain && parts > 1) k_gain_join<<<(a.cols + 31) / 32, 1024, 0, stream>>>(a.partial, a.grad_gain, parts, a.cols);
+        if (e != hipSuccess || !a.grad_gain || parts == 1) return e;
+        return launch(k_gain_join, (a.cols + 31) / 32, 1024, 0, stream, (const float *)a.partial, a.grad_gain, parts, a.cols);
     });
 }
 

@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace gv {
 
 // Items i = 0, 1, ... of rows of `each` items, taken by threads in turn: a thread goes on by the grid's threads, which are
@@ -75,6 +77,18 @@ struct ScoreArgs {
     uint32_t cols, group;
     int type;
 };
+
+// Launches a kernel.  hipLaunchKernel says itself what became of it: the thread's last error may be of a call before, and is its
+// caller's to ask for; that of a launch is returned here and left to nobody else.
+template <class... Parameters, class... Arguments>
+hipError_t launch(void (*kernel)(Parameters...), uint32_t blocks, uint32_t threads, uint32_t shared_bytes, hipStream_t stream,
+                  const Arguments &...arguments) {
+    static_assert((std::is_same_v<Parameters, Arguments> && ...), "a kernel is given its own parameters");
+    void *at[] = {const_cast<Arguments *>(&arguments)...};
+    const hipError_t e = hipLaunchKernel((const void *)kernel, dim3(blocks), dim3(threads), at, shared_bytes, stream);
+    if (e != hipSuccess) (void)hipGetLastError();
+    return e;
+}
 
 // how many partial sums of the gain's gradient the backward pass leaves; one goes to its place at once
 uint32_t norm_grad_parts(uint64_t rows, uint32_t cols);

@@ -659,34 +659,32 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantizeArgs a, Walk walk
 // ---------------------------------------------------------------------------
 
 template <bool kFloat, int kColumns, int kLanes, bool kLong>
-void score_few(const ScoreArgs &a, hipStream_t stream) {
+hipError_t score_few(const ScoreArgs &a, hipStream_t stream) {
     const uint32_t slots = (a.cols + kSlot - 1) / kSlot;
     const uint32_t bytes = kColumns * 32 * slots;
     const uint64_t waves = (a.rows + 64 / kLanes - 1) / (64 / kLanes);  // of one load each
-    if (waves <= 4096) {  // fewer than four loads for each of four waves on every compute unit: spread them
-        k_score_few<kFloat, kColumns, kLanes, 1, kLong><<<(uint32_t)((waves + kWaves - 1) / kWaves), kThreads, bytes, stream>>>(a);
-    } else {
-        const uint64_t tiles = (waves + 3) / 4, all = (tiles + kWaves - 1) / kWaves;
-        const uint64_t turns = (all + (kLong ? 1024 : 2048) - 1) / (kLong ? 1024 : 2048);  // of every workgroup, as many of each
-        k_score_few<kFloat, kColumns, kLanes, 4, kLong><<<(uint32_t)((all + turns - 1) / turns), kThreads, bytes, stream>>>(a);
-    }
+    if (waves <= 4096)  // fewer than four loads for each of four waves on every compute unit: spread them
+        return launch(k_score_few<kFloat, kColumns, kLanes, 1, kLong>, (uint32_t)((waves + kWaves - 1) / kWaves), kThreads, bytes, stream, a);
+    const uint64_t tiles = (waves + 3) / 4, all = (tiles + kWaves - 1) / kWaves;
+    const uint64_t turns = (all + (kLong ? 1024 : 2048) - 1) / (kLong ? 1024 : 2048);  // of every workgroup, as many of each
+    return launch(k_score_few<kFloat, kColumns, kLanes, 4, kLong>, (uint32_t)((all + turns - 1) / turns), kThreads, bytes, stream, a);
 }
 
 template <bool kFloat, int kColumns>
-void score_few_by_length(const ScoreArgs &a, hipStream_t stream) {
+hipError_t score_few_by_length(const ScoreArgs &a, hipStream_t stream) {
     const uint32_t slots = (a.cols + kSlot - 1) / kSlot;
-    if (slots <= 1) score_few<kFloat, kColumns, 1, false>(a, stream);
-    else if (slots <= 2) score_few<kFloat, kColumns, 2, false>(a, stream);
-    else if (slots <= 4) score_few<kFloat, kColumns, 4, false>(a, stream);
-    else if (slots <= 8) score_few<kFloat, kColumns, 8, false>(a, stream);
-    else if (slots <= 16) score_few<kFloat, kColumns, 16, false>(a, stream);
-    else if (slots <= 32) score_few<kFloat, kColumns, 32, false>(a, stream);
-    else if (slots <= 64) score_few<kFloat, kColumns, 64, false>(a, stream);
-    else score_few<kFloat, kColumns, 64, true>(a, stream);
+    if (slots <= 1) return score_few<kFloat, kColumns, 1, false>(a, stream);
+    if (slots <= 2) return score_few<kFloat, kColumns, 2, false>(a, stream);
+    if (slots <= 4) return score_few<kFloat, kColumns, 4, false>(a, stream);
+    if (slots <= 8) return score_few<kFloat, kColumns, 8, false>(a, stream);
+    if (slots <= 16) return score_few<kFloat, kColumns, 16, false>(a, stream);
+    if (slots <= 32) return score_few<kFloat, kColumns, 32, false>(a, stream);
+    if (slots <= 64) return score_few<kFloat, kColumns, 64, false>(a, stream);
+    return score_few<kFloat, kColumns, 64, true>(a, stream);
 }
 
 template <bool kFloat, int kTiles, int kPer>
-void score_many(const ScoreArgs &a, hipStream_t stream) {
+hipError_t score_many(const ScoreArgs &a, hipStream_t stream) {
     // Two row tiles a wave write whole lines of a query's scores and read its digits once for both (16 queries x 4*10^6
     // rows of 128: 119 us, 124 with one; 4 queries in floats: 69 and 97; 16 bfloat16 queries x 5*10^5 rows of 1024 in groups
     // of 32: 139 and 173).  Rows of over 256 columns in larger groups, whose sums are joined more seldom, gain more from more
@@ -704,65 +702,61 @@ void score_many(const ScoreArgs &a, hipStream_t stream) {
         return (uint32_t)((std::min(all, most) + 7) / 8 * 8);
     };
     if (tiles <= 4096 || (slots > 8 && kPer > 1))
-        k_score_many<kFloat, kTiles, kPer, 1><<<across(1) * passes, kAll, bytes, stream>>>(a, segment, passes);
-    else
-        k_score_many<kFloat, kTiles, kPer, kRowTiles><<<across(kRowTiles) * passes, kAll, bytes, stream>>>(a, segment, passes);
+        return launch(k_score_many<kFloat, kTiles, kPer, 1>, across(1) * passes, kAll, bytes, stream, a, segment, passes);
+    return launch(k_score_many<kFloat, kTiles, kPer, kRowTiles>, across(kRowTiles) * passes, kAll, bytes, stream, a, segment, passes);
 }
 
 template <bool kFloat, int kTiles, int kPer, int kSlots>
-void score_narrow(const ScoreArgs &a, hipStream_t stream) {
+hipError_t score_narrow(const ScoreArgs &a, hipStream_t stream) {
     constexpr int kAll = many_threads(kTiles), kEach = (kFloat ? 4 : 16) * kTiles, kRows = kAll / kSlots;
     const uint32_t passes = (uint32_t)((a.queries + kEach - 1) / kEach);
     const uint64_t across = std::min<uint64_t>((a.rows + kRows - 1) / kRows, std::max<uint64_t>(1, (kAll > 256 ? 512 : 1024) / passes));
-    k_score_narrow<kFloat, kTiles, kPer, kSlots><<<(uint32_t)((across + 7) / 8 * 8) * passes, kAll, 0, stream>>>(a, passes);
+    return launch(k_score_narrow<kFloat, kTiles, kPer, kSlots>, (uint32_t)((across + 7) / 8 * 8) * passes, kAll, 0, stream, a, passes);
 }
 
 template <bool kFloat, int kTiles>
-void score_many_by_group(const ScoreArgs &a, hipStream_t stream) {
-    if (a.cols <= kSlot) score_narrow<kFloat, kTiles, 1, 1>(a, stream);
-    else if (a.cols <= 2 * kSlot && a.group == 32) score_narrow<kFloat, kTiles, 1, 2>(a, stream);
-    else if (a.cols <= 2 * kSlot) score_narrow<kFloat, kTiles, 2, 2>(a, stream);
-    else if (a.group == 32) score_many<kFloat, kTiles, 1>(a, stream);
-    else if (a.group == 64) score_many<kFloat, kTiles, 2>(a, stream);
-    else score_many<kFloat, kTiles, 4>(a, stream);
+hipError_t score_many_by_group(const ScoreArgs &a, hipStream_t stream) {
+    if (a.cols <= kSlot) return score_narrow<kFloat, kTiles, 1, 1>(a, stream);
+    if (a.cols <= 2 * kSlot && a.group == 32) return score_narrow<kFloat, kTiles, 1, 2>(a, stream);
+    if (a.cols <= 2 * kSlot) return score_narrow<kFloat, kTiles, 2, 2>(a, stream);
+    if (a.group == 32) return score_many<kFloat, kTiles, 1>(a, stream);
+    if (a.group == 64) return score_many<kFloat, kTiles, 2>(a, stream);
+    return score_many<kFloat, kTiles, 4>(a, stream);
 }
 
 template <class T>
-void quantize(const QuantizeArgs &a, hipStream_t stream) {
+hipError_t quantize(const QuantizeArgs &a, hipStream_t stream) {
     const uint32_t pieces = (a.cols + a.group - 1) / a.group * (a.group / 8);  // of a row, with those that fill its last group
     const uint32_t blocks = (uint32_t)std::min<uint64_t>((a.rows * pieces + kThreads - 1) / kThreads, 8192);
     const Walk walk = walk_of(a.rows, pieces, (uint64_t)blocks * kThreads);
-    if (a.group == 32) k_quantize<T, 4><<<blocks, kThreads, 0, stream>>>(a, walk);
-    else if (a.group == 64) k_quantize<T, 8><<<blocks, kThreads, 0, stream>>>(a, walk);
-    else k_quantize<T, 16><<<blocks, kThreads, 0, stream>>>(a, walk);
+    if (a.group == 32) return launch(k_quantize<T, 4>, blocks, kThreads, 0, stream, a, walk);
+    if (a.group == 64) return launch(k_quantize<T, 8>, blocks, kThreads, 0, stream, a, walk);
+    return launch(k_quantize<T, 16>, blocks, kThreads, 0, stream, a, walk);
 }
 
 }  // namespace
 
 hipError_t launch_quantize(const QuantizeArgs &a, hipStream_t stream) {
-    if (a.type == GV_F32) quantize<float>(a, stream);
-    else if (a.type == GV_BF16) quantize<__bf16>(a, stream);
-    else quantize<_Float16>(a, stream);
-    return hipGetLastError();
+    if (a.type == GV_F32) return quantize<float>(a, stream);
+    if (a.type == GV_BF16) return quantize<__bf16>(a, stream);
+    return quantize<_Float16>(a, stream);
 }
 
 hipError_t launch_score(const ScoreArgs &a, hipStream_t stream) {
     const uint64_t q = a.queries;
     if (a.type == GV_I8) {
-        if (q == 1) score_few_by_length<false, 1>(a, stream);
-        else if (q == 2) score_few_by_length<false, 2>(a, stream);
-        else if (q <= 4) score_few_by_length<false, 4>(a, stream);
-        else if (q <= 16) score_many_by_group<false, 1>(a, stream);
-        else if (q <= 32) score_many_by_group<false, 2>(a, stream);
-        else score_many_by_group<false, 4>(a, stream);
-    } else {
-        if (q == 1) score_few_by_length<true, 4>(a, stream);
-        else if (q <= 4) score_many_by_group<true, 1>(a, stream);
-        else if (q <= 8) score_many_by_group<true, 2>(a, stream);
-        else if (q <= 16) score_many_by_group<true, 4>(a, stream);
-        else score_many_by_group<true, 8>(a, stream);
+        if (q == 1) return score_few_by_length<false, 1>(a, stream);
+        if (q == 2) return score_few_by_length<false, 2>(a, stream);
+        if (q <= 4) return score_few_by_length<false, 4>(a, stream);
+        if (q <= 16) return score_many_by_group<false, 1>(a, stream);
+        if (q <= 32) return score_many_by_group<false, 2>(a, stream);
+        return score_many_by_group<false, 4>(a, stream);
     }
-    return hipGetLastError();
+    if (q == 1) return score_few_by_length<true, 4>(a, stream);
+    if (q <= 4) return score_many_by_group<true, 1>(a, stream);
+    if (q <= 8) return score_many_by_group<true, 2>(a, stream);
+    if (q <= 16) return score_many_by_group<true, 4>(a, stream);
+    return score_many_by_group<true, 8>(a, stream);
 }
 
 }  // namespace gv

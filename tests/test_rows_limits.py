@@ -282,3 +282,48 @@ def test_the_package_is_imported_without_torch(gv):
     for name in rows.__all__:
         assert getattr(gv, name) is getattr(rows, name) and names[name] is getattr(rows, name)
     assert names["gv_create"] is gv.gv_create and gv.rows is rows and not hasattr(gv, "gv_no_such_call")
+
+
+def runtime():
+    """The HIP runtime of this process."""
+    with open("/proc/self/maps") as f:
+        path = next(line.split()[-1] for line in f if "libamdhip64.so" in line)
+    return ctypes.CDLL(path)
+
+
+@gpu
+def test_errors_of_others_stay_with_them(gv):
+    """An error that a call before left in the thread is neither reported by these calls nor taken from its owner."""
+    import torch
+
+    lib, hip = gv.load(), runtime()
+    x, out, gain = torch.ones(8, 32, device="cuda"), torch.empty(8, 32, device="cuda"), torch.ones(32, device="cuda")
+    rstd, grad_gain, space = torch.ones(5000, device="cuda"), torch.empty(32, device="cuda"), torch.empty(1 << 16, device="cuda")
+    long, back = torch.ones(5000, 32, device="cuda"), torch.empty(5000, 32, device="cuda")
+    codes, scales = torch.empty(8, 16, dtype=torch.uint8, device="cuda"), torch.empty(8, 1, dtype=torch.bfloat16, device="cuda")
+    scores = torch.empty(8, 8, device="cuda")
+    torch.cuda.synchronize()
+    x_at, out_at = x.data_ptr(), out.data_ptr()
+    calls = [
+        lambda: lib.gv_drop_rows(8, 32, gv.GV_F32, x_at, 32, 0.0, 1, 0, out_at, 32, None),
+        lambda: lib.gv_norm_rows(8, 32, gv.GV_F32, x_at, 32, None, 0, gain.data_ptr(), 0.0, 0.0, 0, 0, None, 0, gv.GV_F32, out_at, 32,
+                                 None, None, None),
+        lambda: lib.gv_norm_rows_backward(5000, 32, gv.GV_F32, long.data_ptr(), 32, long.data_ptr(), 32, gain.data_ptr(), rstd.data_ptr(),
+                                          None, 0, 0.0, 0, 0, back.data_ptr(), 32, None, 0, grad_gain.data_ptr(), space.data_ptr(),
+                                          space.nbytes, None),
+        lambda: lib.gv_quantize_rows(8, 32, gv.GV_F32, x_at, 32, 32, codes.data_ptr(), scales.data_ptr(), None),
+        lambda: lib.gv_score_rows(8, 32, 32, codes.data_ptr(), scales.data_ptr(), 1, gv.GV_F32, x_at, 32, None, scores.data_ptr(), 8, None),
+        lambda: lib.gv_score_rows(8, 32, 32, codes.data_ptr(), scales.data_ptr(), 8, gv.GV_F32, x_at, 32, None, scores.data_ptr(), 8, None),
+    ]
+    hip.hipGetLastError()
+    results = []
+    try:
+        for call in calls:
+            refused = hip.hipSetDevice(1 << 20)  # there is no such GPU
+            results.append((refused != 0, call(), hip.hipGetLastError() == refused))
+    finally:
+        hip.hipGetLastError()
+    assert results == [(True, gv.GV_OK, True)] * len(calls), results
+    torch.cuda.synchronize()
+    seventh = torch.tensor(1 / 7).to(torch.bfloat16).float()  # the scale of a row of ones in 4 bits, whose codes are 7
+    assert (out == 1).all() and (grad_gain == 5000).all() and (scores == 32 * 7 * seventh.cuda()).all()
