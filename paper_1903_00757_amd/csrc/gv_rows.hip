@@ -320,16 +320,25 @@ hipError_t by_type(int type, Run &&run) {
     return run((_Float16 *)nullptr);
 }
 
+// Workgroups of the gradients, and the rows that one takes in a turn.
+struct GradGrid {
+    uint64_t each;
+    uint32_t blocks;
+};
+GradGrid grad_grid(uint64_t rows, uint32_t cols) {
+    const int lanes = shape_of(cols).lanes, threads = grad_threads_of(lanes);
+    const uint64_t each = threads / lanes;
+    return {each, (uint32_t)std::min<uint64_t>((rows + each - 1) / each, kGradLanes / threads)};
+}
+
 }  // namespace
 
 uint32_t norm_grad_parts(uint64_t rows, uint32_t cols) {
-    const int lanes = shape_of(cols).lanes, threads = grad_threads_of(lanes);
-    const uint64_t each = threads / lanes;
+    const GradGrid grid = grad_grid(rows, cols);
     // A few turns of one workgroup take less than a launch that joins several (200 rows of 128 through the norm and back: 21 us
     // among others, 27 with the launch, 37 alone either way; 30 rows of 1000 22 and 27, alone 42 and 38; twice as many turns
     // 31 and 27 at 128 rows of 357).
-    if (rows <= 4 * each) return 1;
-    return (uint32_t)std::min<uint64_t>((rows + each - 1) / each, kGradLanes / threads);
+    return rows <= 4 * grid.each ? 1 : grid.blocks;
 }
 
 // Workgroups that come and go pass through memory side by side; a grid that loops drifts apart (dropout of
@@ -363,7 +372,7 @@ hipError_t launch_norm_grad(const NormGradArgs &args, hipStream_t stream) {
     return by_type(args.type, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
         NormGradArgs a = args;
-        const uint32_t parts = norm_grad_parts(a.rows, a.cols);
+        const uint32_t parts = a.grad_gain ? norm_grad_parts(a.rows, a.cols) : grad_grid(a.rows, a.cols).blocks;
         if (parts == 1) a.partial = a.grad_gain;
         const hipError_t e = by_shape(a.cols, [&](auto lanes, auto pieces) {
             constexpr int kLanes = decltype(lanes)::value, kPieces = decltype(pieces)::value;

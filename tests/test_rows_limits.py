@@ -327,3 +327,43 @@ def test_errors_of_others_stay_with_them(gv):
     torch.cuda.synchronize()
     seventh = torch.tensor(1 / 7).to(torch.bfloat16).float()  # the scale of a row of ones in 4 bits, whose codes are 7
     assert (out == 1).all() and (grad_gain == 5000).all() and (scores == 32 * 7 * seventh.cuda()).all()
+
+
+class KernelNode(ctypes.Structure):
+    """hipKernelNodeParams"""
+    _fields_ = [("block", ctypes.c_uint32 * 3), ("extra", ctypes.c_void_p), ("func", ctypes.c_void_p),
+                ("grid", ctypes.c_uint32 * 3), ("params", ctypes.c_void_p), ("shared", ctypes.c_uint32)]
+
+
+def launches_of(work):
+    """(workgroups, threads) of every kernel that `work` launches, in order."""
+    import torch
+
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        held = work()
+    hip, count, found = runtime(), ctypes.c_size_t(), []
+    raw = ctypes.c_void_p(graph.raw_cuda_graph())
+    assert hip.hipGraphGetNodes(raw, None, ctypes.byref(count)) == 0
+    nodes = (ctypes.c_void_p * count.value)()
+    assert hip.hipGraphGetNodes(raw, nodes, ctypes.byref(count)) == 0
+    for node in nodes:
+        kind, params = ctypes.c_int(), KernelNode()
+        assert hip.hipGraphNodeGetType(ctypes.c_void_p(node), ctypes.byref(kind)) == 0 and kind.value == 0
+        assert hip.hipGraphKernelNodeGetParams(ctypes.c_void_p(node), ctypes.byref(params)) == 0
+        found.append((params.grid[0], params.block[0]))
+    del held
+    return found
+
+
+@gpu
+def test_gradients_without_the_gains_spread_their_rows(gv):
+    """One workgroup takes a few turns of rows where that saves the launch that joins the gain's gradient, and only there."""
+    import torch
+
+    x, gain, rstd = torch.randn(256, 128, device="cuda"), torch.ones(128, device="cuda"), torch.ones(256, device="cuda")
+    both = gv.gv_norm_rows_backward(x, x, gain, rstd)
+    without = gv.gv_norm_rows_backward(x, x, gain, rstd, keep_gain=False)
+    assert torch.equal(both.x, without.x) and without.gain is None
+    assert launches_of(lambda: gv.gv_norm_rows_backward(x, x, gain, rstd)) == [(1, 512)]
+    assert launches_of(lambda: gv.gv_norm_rows_backward(x, x, gain, rstd, keep_gain=False)) == [(4, 512)]
