@@ -367,3 +367,76 @@ def test_gradients_without_the_gains_spread_their_rows(gv):
     assert torch.equal(both.x, without.x) and without.gain is None
     assert launches_of(lambda: gv.gv_norm_rows_backward(x, x, gain, rstd)) == [(1, 512)]
     assert launches_of(lambda: gv.gv_norm_rows_backward(x, x, gain, rstd, keep_gain=False)) == [(4, 512)]
+
+
+# ------------------------------------------------------------------------------------------------ past the sizes where layouts change
+
+# just past them, with odd remainders: four loads a wave of the few-query kernels (4096 waves; 64 to 1 rows each), two row tiles of
+# the others (65536 rows), workgroups that take a second block, and digits that are staged again for it
+LARGE = [(70_001, 128, 32, (1, 2, 4, 5, 16, 17, 40)), (70_001, 96, 32, (1, 3, 4, 9, 16, 17)), (70_003, 160, 64, (1, 2, 6)),
+         (70_003, 256, 128, (2, 16)), (270_001, 32, 32, (1, 2, 4, 5, 20)), (270_001, 20, 64, (1, 5, 33)), (140_001, 64, 64, (1, 3, 5, 20)),
+         (140_001, 50, 32, (1, 4, 17, 40)), (36_001, 256, 32, (1, 2, 4)), (17_001, 512, 128, (1, 2, 4)), (9_001, 1024, 64, (1, 2, 4)),
+         (4_101, 2048, 32, (1, 4)), (4_101, 2100, 32, (1, 2, 4)), (70_001, 544, 64, (4, 20, 33)), (70_001, 1056, 32, (5, 40))]
+
+
+@gpu
+@pytest.mark.parametrize("rows, cols, group, batches", LARGE)
+@pytest.mark.parametrize("kind", ["f32", "bf16", "i8"])
+def test_scores_of_large_tables(gv, rows, cols, group, batches, kind):
+    import torch
+
+    gen = torch.Generator(device="cuda").manual_seed(rows + cols)
+    groups, parts = -(-cols // group), -(-cols // 32)
+    q = torch.randint(-8, 8, (rows, cols), device="cuda", generator=gen, dtype=torch.int8)
+    wide = torch.nn.functional.pad(q, (0, 32 * parts - cols))
+    codes = ((wide[:, 0::2] & 15) | (wide[:, 1::2] << 4)).view(torch.uint8).contiguous()
+    scales = torch.exp(torch.randn(rows, groups, device="cuda", generator=gen)).to(torch.bfloat16)
+    w = q.double() * scales.double().repeat_interleave(group, dim=1)[:, :cols]
+    for queries in batches:
+        if kind == "i8":
+            t = torch.randint(-128, 128, (queries, cols), device="cuda", generator=gen, dtype=torch.int8)
+            x_scale = torch.exp(torch.randn(queries, device="cuda", generator=gen))
+            x = t.double() * x_scale.double()[:, None]
+        else:
+            t = torch.randn(queries, cols, device="cuda", generator=gen).to(torch.float32 if kind == "f32" else torch.bfloat16)
+            x, x_scale = t.double(), None
+        got = gv.gv_score_rows(codes, scales, t, group=group, scale=x_scale)
+        sums, weights = torch.matmul(x.abs(), w.abs().t()), w.abs().sum(1)
+        tolerance = (groups + 8) * U * sums + 2.0 ** -28 * x.abs().amax(1, keepdim=True) * weights
+        off = (got.double() - torch.matmul(x, w.t())).abs()
+        assert (off <= tolerance).all(), (queries, (off / tolerance).max().item(), (off > tolerance).sum().item())
+        for lo in (0, rows // 2 - 17, rows - 35):  # the same bits as from a small table
+            part = gv.gv_score_rows(codes[lo:lo + 35], scales[lo:lo + 35], t, group=group, scale=x_scale)
+            assert torch.equal(part, got[:, lo:lo + 35]), (queries, lo)
+
+
+# several workgroups for every number of lanes that hold a row (1, 2, 4, 8, 16, 32, 64, 256 and 512), so that the gain's gradient
+# is joined from parts; 520 and 1100 rows are more than the parts that there may be
+JOINED = [(3000, 8), (1100, 16), (600, 31), (900, 100), (130, 257), (200, 200), (37, 1000), (9, 1025), (1100, 2048), (9, 4099), (520, 8192),
+          (6, 16383)]
+
+
+@gpu
+@pytest.mark.parametrize("rows, cols", JOINED)
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_gradient_of_the_gain_from_several_workgroups(gv, rows, cols, kind):
+    import torch
+
+    assert gv.gv_norm_rows_workspace(rows, cols) > 4 * cols
+    rng = np.random.default_rng(rows + cols)
+    for pad, shift in [(0, 0), (3, 1)]:
+        st, h = make_rows(torch, rng, rows, cols, kind, pad, shift)
+        gt, grad = make_rows(torch, rng, rows, cols, kind, pad, shift)
+        gain = torch.from_numpy(rng.standard_normal(cols).astype(np.float32)).cuda()
+        rstd = (1 / np.sqrt((h * h).mean(1) + 1e-5)).astype(np.float32)
+        rs = rstd.astype(np.float64)[:, None]
+        dx, _, dg = grads_in_64_bits(grad, h, gain.double().cpu().numpy(), rs, None, None)
+        got = gv.gv_norm_rows_backward(gt, st, gain, torch.from_numpy(rstd).cuda())
+        # h rstd rounds once; a product passes through at most 2 additions in its lane, 6 across lanes, 8 across waves, 32 in a
+        # thread of the join and 5 across its lanes
+        n, u = h * rs, grad * gain.double().cpu().numpy()
+        check(got.gain, dg, 54 * U * np.abs(grad * n).sum(0), ("gain", pad))
+        # a lane holds up to 32 values of a row; with the lanes and waves a mean passes through at most 46 additions
+        off = rs * (4 * U * np.abs(u) + 54 * U * np.abs(n) * np.abs(u * n).mean(1, keepdims=True)) + 3 * U * np.abs(dx)
+        rel, least = rounding(kind)
+        check(got.x, dx, off + 1.01 * rel * (np.abs(dx) + off) + least, ("x", pad))
