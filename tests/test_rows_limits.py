@@ -440,3 +440,28 @@ def test_gradient_of_the_gain_from_several_workgroups(gv, rows, cols, kind):
         off = rs * (4 * U * np.abs(u) + 54 * U * np.abs(n) * np.abs(u * n).mean(1, keepdims=True)) + 3 * U * np.abs(dx)
         rel, least = rounding(kind)
         check(got.x, dx, off + 1.01 * rel * (np.abs(dx) + off) + least, ("x", pad))
+
+
+@gpu
+@pytest.mark.parametrize("rows, cols, group, queries", [(3001, 128, 32, 300), (20_003, 160, 64, 1000), (500, 40, 32, 5000),
+                                                        (40, 96, 128, 1 << 16), (33, 2100, 32, 257)])
+@pytest.mark.parametrize("kind", ["f32", "i8"])
+def test_scores_of_more_queries_than_a_pass_takes(gv, rows, cols, group, queries, kind):
+    import torch
+
+    gen = torch.Generator(device="cuda").manual_seed(rows + queries)
+    codes, scales = gv.gv_quantize_rows(torch.randn(rows, cols, device="cuda", generator=gen), group=group)
+    if kind == "i8":
+        t = torch.randint(-128, 128, (queries, cols), device="cuda", generator=gen, dtype=torch.int8)
+        x_scale = torch.exp(torch.randn(queries, device="cuda", generator=gen))
+        x = t.double() * x_scale.double()[:, None]
+    else:
+        t = torch.randn(queries, cols, device="cuda", generator=gen)
+        x, x_scale = t.double(), None
+    q = torch.stack([codes & 15, codes >> 4], -1).view(rows, -1)[:, :cols].to(torch.int8)
+    w = torch.where(q > 7, q - 16, q).double() * scales.double().repeat_interleave(group, dim=1)[:, :cols]
+    got = gv.gv_score_rows(codes, scales, t, group=group, scale=x_scale)
+    tolerance = ((scales.shape[1] + 8) * U * torch.matmul(x.abs(), w.abs().t())
+                 + 2.0 ** -28 * x.abs().amax(1, keepdim=True) * w.abs().sum(1))
+    off = (got.double() - torch.matmul(x, w.t())).abs()
+    assert (off <= tolerance).all(), ((off / tolerance).max().item(), (off > tolerance).sum().item())
