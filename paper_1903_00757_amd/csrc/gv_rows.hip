@@ -335,7 +335,7 @@ GradGrid grad_grid(uint64_t rows, uint32_t cols) {
 
 uint32_t norm_grad_parts(uint64_t rows, uint32_t cols) {
     const GradGrid grid = grad_grid(rows, cols);
-    // A few turns of one workgroup take less than a launch that joins several (200 rows of 128 through the norm and back: 21 us
+    // A few turns of one workgroup mostly take less than a launch that joins several (200 rows of 128 through the norm and back: 21 us
     // among others, 27 with the launch, 37 alone either way; 30 rows of 1000 22 and 27, alone 42 and 38; twice as many turns
     // 31 and 27 at 128 rows of 357).
     return rows <= 4 * grid.each ? 1 : grid.blocks;
@@ -343,7 +343,7 @@ uint32_t norm_grad_parts(uint64_t rows, uint32_t cols) {
 
 // Workgroups that come and go pass through memory side by side; a grid that loops drifts apart (dropout of
 // 2^20 rows of 512 in bfloat16, there and back: 755 us, 901 with 4096 workgroups; 2^20 rows of 128 through the norm
-// and back: 435 and 462 us).  They loop past the largest grid of 2^32 threads alone.
+// and back: 435 and 462 us).  They loop past 2^22 workgroups alone (2^30 or 2^31 threads; a launch takes up to 2^32).
 constexpr uint64_t kMostBlocks = 1 << 22;
 
 hipError_t launch_drop(const DropRowsArgs &a, hipStream_t stream) {

@@ -396,9 +396,10 @@ constexpr int many_threads(int tiles) { return tiles == 8 ? 512 : 256; }  // 64 
 // everywhere, as the instruction wants it.  The digits of kTiles x 16 columns lie in LDS in the order of the lanes.  The digit
 // columns are the rows of the product: its lane r + 16 h then holds four digits of one query (or four queries in 8 bits) for
 // row r alone, whose scale is one value, and the digits join without another lane.
-// With few tiles bound by memory: 16 queries in 8 bits x 4*10^6 rows of 128 in 114 us, 288 MB read and 256 written, 4.8 TB/s.
-// With many by joining sums and the latency from load to store: 64 bfloat16 queries (16 tiles, two passes) x 10^6 rows
-// of 512 in 190 us, 2.7 TB/s and 1.4*10^15 operations/s on digits.
+// With few tiles bound by memory: 16 queries in 8 bits x 4*10^6 rows of 128 in 116 us, 288 MB read and 256 written, 4.7 TB/s.
+// With many by vector instructions, for unpacking codes and joining sums: 64 bfloat16 queries (16 tiles, two passes) x 10^6
+// rows of 512 in 190 us, 2.7 TB/s and 1.4*10^15 operations/s on digits; the SIMDs spend 56 % of their cycles on vector and 31 % on matrix
+// instructions, LDS is busy for 33 % of its own.
 template <bool kFloat, int kTiles, int kPer, int kRowTiles>
 __global__ __launch_bounds__(many_threads(kTiles), 4) void k_score_many(ScoreArgs a, uint32_t segment, uint32_t passes) {
     constexpr int kQueries = kFloat ? 4 : 16;  // of a tile
@@ -545,7 +546,7 @@ __global__ __launch_bounds__(many_threads(kTiles), 4) void k_score_many(ScoreArg
 
 // Many queries and rows of up to 64 columns: a load holds 64 / kSlots rows of kSlots slots (lane r + 16 h: slot h mod kSlots
 // of row 16 (h / kSlots) + r), so that after the transposition word j is slot j mod kSlots of tile j / kSlots.
-// One group: of the row (kPer = kSlots), or of each slot.  20 bfloat16 queries x 10^6 rows of 64 in 25 us, 4.6 TB/s; with loads
+// One group: of the row (kPer = kSlots), or of each slot.  20 bfloat16 queries x 10^6 rows of 64 in 26 us, 4.5 TB/s; with loads
 // of 16 rows that leave lanes idle 30.
 template <bool kFloat, int kTiles, int kPer, int kSlots>
 __global__ __launch_bounds__(many_threads(kTiles), 4) void k_score_narrow(ScoreArgs a, uint32_t passes) {
@@ -631,7 +632,7 @@ __global__ __launch_bounds__(many_threads(kTiles), 4) void k_score_narrow(ScoreA
 }
 
 // ---------------------------------------------------------------------------
-// A table from rows: 8 columns a lane, kLanes lanes to a group.  10^6 rows of 128 floats in 114 us, 5.1 TB/s.
+// A table from rows: 8 columns a lane, kLanes lanes to a group.  10^6 rows of 128 floats in 112 us, 5.2 TB/s.
 template <class T, int kLanes>
 __global__ __launch_bounds__(kThreads) void k_quantize(QuantizeArgs a, Walk walk) {
     const uint32_t groups = walk.each / kLanes, slots = (a.cols + kSlot - 1) / kSlot;
@@ -689,7 +690,7 @@ hipError_t score_many(const ScoreArgs &a, hipStream_t stream) {
     // rows of 128: 119 us, 124 with one; 4 queries in floats: 69 and 97; 16 bfloat16 queries x 5*10^5 rows of 1024 in groups
     // of 32: 139 and 173).  Rows of over 256 columns in larger groups, whose sums are joined more seldom, gain more from more
     // waves (4 queries x 10^6 rows of 512 in groups of 128: 73 us and 63), and more tiles of 8-bit queries do not fit the
-    // registers twice (64 queries x 10^6 rows of 128: 165 us, 90 with one).
+    // registers twice (64 queries x 10^6 rows of 128: 165 us, 92 with one).
     constexpr int kRowTiles = kTiles == 1 || (kFloat && kTiles < 8) ? 2 : 1, kAll = many_threads(kTiles), kEach = (kFloat ? 4 : 16) * kTiles;
     const uint32_t slots = (a.cols + kSlot - 1) / kSlot;
     const uint32_t segment = std::min((slots + 3) / 4 * 4, 128u / kTiles), bytes = segment * kTiles * 512;
