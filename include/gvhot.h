@@ -387,7 +387,8 @@ int gv_drop_rows(uint64_t rows, uint32_t cols, int type, const void *dev_x, uint
 
 /* Root-mean-square norm with the residual's addition:
  *   h = residual + dropout(x) (dropout as gv_drop_rows; drop = 0 leaves x; dev_residual NULL: h = dropout(x))
- *   out = h * rstd * gain,  rstd = 1 / sqrt(mean(h^2) + eps),  eps >= 0, wherever h^2 lies; 0 where that has no float
+ *   out = h * rstd * gain,  rstd = 1 / sqrt(mean(h^2) + eps),  eps >= 0
+ * (the squares may lie outside fp32; a row whose rstd has no float, one of zeros with eps = 0, has rstd 0)
  * x, residual and sum are of `type`, gain float[cols].  dev_sum (may be NULL) receives h, dev_rstd (float[rows], may be
  * NULL) what the backward pass needs.  out_type = type, or GV_I8 with dev_out_scale[rows]: with v = h * gain, a = max |v| of
  * the row and step = a * (1 / 127) in fp32, out = v * (1 / step) rounded to the nearest whole number (even at ties) and

@@ -61,8 +61,11 @@ struct Bytes {
     int exponent;  // 2^-100 to 2^100: a sum, up to 2^21, times the first and the rest of a subnormal scale are normal floats
     __device__ __forceinline__ explicit Bytes(uint32_t bits)
         : scale(__uint_as_float(bits)), exponent(std::min(std::max((int)(bits >> 23 & 255u), 27), 227)) {}
-    // of a sum; NaN where it would be subnormal, so that the scores are made again
-    __device__ __forceinline__ float unit() const { return exponent == 27 && scale != 0.0f ? __builtin_nanf("") : scale * 0.0625f; }
+    // of a sum; NaN where it is subnormal and may be rounded, so that the scores are made again
+    __device__ __forceinline__ float unit() const {
+        const float all = scale * 0.0625f;
+        return scale != 0.0f && fabsf(all) < 0x1p-126f ? __builtin_nanf("") : all;
+    }
     __device__ __forceinline__ float first_unit() const { return __uint_as_float((uint32_t)(exponent - 4) << 23); }
     __device__ __forceinline__ float rest() const { return scale * __uint_as_float((uint32_t)(254 - exponent) << 23); }
 };
