@@ -1,0 +1,391 @@
+"""What a head on learned rows is trained with and what answers are taken with: rows by index with their gradient, a layer
+with its gradient, and the selection of the best rows and paths.
+
+A case is one pass through one of the operators on rows in device memory, as a program that trains a head on embeddings, or
+follows the likeliest paths through them, makes it.  With ``own`` the pass goes through the entry points of
+``paper_1903_00757_amd``; otherwise the same formulas are computed with elementary torch operations in 32 bits (sums of many
+rows and what decides an order in 64).
+
+Fields of a case
+  path       lookup   rows of a table by index, scaled                                        gv_lookup_rows
+             grad     its gradient: the rows of a batch added up by index                     gv_lookup_rows_backward
+             layer    out = residual + act(x weight^T + bias)                                 gv_dense_rows
+             train    the same, forward and backward                                          gv_dense_rows, gv_dense_rows_backward
+             select   the best rows over the scores of beams, and the beams' states           gv_select_rows, gv_lookup_rows
+  rows       of the batch: indices, rows of x, or beams in all
+  cols       length of the table's rows, of x's rows, or of the beams' states (0: none)
+  type       f32, bf16, f16: of the table, the gradients that come in, x, or the scores
+  out_type   of what a lookup or its gradient gives
+  table      rows of the table, or scores of a beam
+  index      i32, i64, or pair: a column of int32 pairs, as pools hold them
+  none       share of the indices that name no row (-1), of scores that are masked (-inf), and of beams that have ended
+  add        the gradient is added to rows that are there
+  out        columns of the layer's result
+  act        none, relu, gelu, silu
+  bias, residual
+  beams      that share a selection
+  best       rows that are selected for each
+  log        scores count by their logarithmic softmax
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+FIELDS = dict(rows=1, cols=0, type="f32", out_type="f32", table=0, index="i64", none=0.0, add=False, out=0, act="none", bias=False,
+              residual=False, beams=1, best=0, log=False)
+
+
+def _case(name, path, **fields):
+    return dict(FIELDS, name=name, path=path, **fields)
+
+
+def listed():
+    return [
+        # the rows of one small query
+        _case("lookup, 64 rows, d128", "lookup", rows=64, cols=128, table=10_000),
+        # the nodes of a million edge samples, for a head in 16 bits
+        _case("lookup, million rows, d128", "lookup", rows=1 << 20, cols=128, table=1_000_000, out_type="bf16", index="pair"),
+        # a small step of a head's training: odd sizes, some places of the batch empty
+        _case("gradient, small and odd", "grad", rows=997, cols=353, table=5003, none=0.05),
+        # a large step: a million samples, the hottest node in every hundredth of them
+        _case("gradient, million rows, d128", "grad", rows=1 << 20, cols=128, type="bf16", table=1_000_000, index="pair"),
+        # one query through a layer
+        _case("layer, one row", "layer", rows=1, cols=512, out=2048, type="bf16", act="gelu", bias=True),
+        # a server's batch of queries through a wide layer
+        _case("layer, 16 rows, 4096 x 4096", "layer", rows=16, cols=4096, out=4096, type="bf16", act="silu", bias=True, residual=True),
+        # a deep head's wide layer on a large batch
+        _case("layer, 8192 rows, 4096 x 4096", "layer", rows=8192, cols=4096, out=4096, type="bf16", act="gelu", bias=True, residual=True),
+        # a small odd step in full precision
+        _case("train, small and odd", "train", rows=1021, cols=357, out=500, type="f32", act="silu", bias=True),
+        # a large step on rows of a trained length
+        _case("train, 65536 rows, 512 x 2048", "train", rows=65_536, cols=512, out=2048, type="bf16", act="gelu", bias=True),
+        # the nodes that follow one query's
+        _case("select, one query", "select", rows=1, table=10_000, best=10, log=True),
+        # a shortlist for each of a server's batch of queries
+        _case("select, 64 queries, best 100", "select", rows=64, table=1_000_000, best=100),
+        # the likeliest paths from 16 nodes, eight of each
+        _case("select, 16 x 8 beams", "select", rows=128, cols=512, table=1_000_000, beams=8, best=8, log=True, none=0.05),
+    ]
+
+
+def _spread(rng, lo, hi):
+    """A whole number between lo and hi, even on the logarithm's scale."""
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
+
+
+def _length(rng, lo, hi):
+    """The length of a row: one of those that the library trains, or any other."""
+    return rng.choice([32, 64, 96, 128, 160, 256, 352, 512]) if rng.random() < 0.5 else _spread(rng, lo, hi)
+
+
+def draw(rng):
+    path = rng.choice(["lookup", "grad", "grad", "layer", "train", "select", "select"])
+    kind = rng.choice(["f32", "bf16", "bf16", "f16"])
+    if path in ("lookup", "grad"):
+        cols = _length(rng, 1, 8192)
+        case = _case("", path, rows=_spread(rng, 1, min(1 << 20, (1 << 28) // 4 // cols)), cols=cols, type=kind,
+                     out_type=rng.choice([kind, "f32"] if path == "grad" else [kind, "bf16"]),
+                     table=_spread(rng, 100, min(4_000_000, (1 << 29) // 4 // cols)), index=rng.choice(["i32", "i64", "pair"]),
+                     none=rng.choice([0.0, 0.05]), add=path == "grad" and rng.random() < 0.3)
+    elif path in ("layer", "train"):
+        cols, out = _length(rng, 1, 8192), _length(rng, 1, 8192)
+        most = (2e11 if kind != "f32" else 5e10) / (2 * cols * out) / (3 if path == "train" else 1)
+        # where a value next to relu's border falls goes by its last bit, and the whole gradient with it
+        case = _case("", path, rows=_spread(rng, 1, max(1, min(65_536, int(most), (1 << 26) // max(cols, out)))), cols=cols, out=out, type=kind,
+                     act=rng.choice(["none", "relu", "gelu", "silu"] if path == "layer" else ["none", "gelu", "silu"]),
+                     bias=rng.random() < 0.7, residual=rng.random() < 0.4)
+    else:
+        beams = 1 if rng.random() < 0.4 else _spread(rng, 2, 16)
+        groups = _spread(rng, 1, 64 if beams == 1 else 16)
+        table = _spread(rng, 100, min(4_000_000, (1 << 26) // (groups * beams)))
+        case = _case("", path, rows=groups * beams, cols=0 if rng.random() < 0.5 else _length(rng, 1, 1024), type=kind, table=table,
+                     beams=beams, best=_spread(rng, 1, 128) if beams == 1 else beams, log=beams > 1 or rng.random() < 0.5,
+                     none=rng.choice([0.0, 0.05]))
+    del case["name"]
+    return case
+
+
+# ---------------------------------------------------------------------------------------------------- inputs
+
+
+def _indices(gen, case):
+    """Nodes as samples name them: the hottest in every hundredth (of a million), in any order."""
+    n, m = case["rows"], case["table"]
+    rank = (m * torch.rand(n, device="cuda", generator=gen, dtype=torch.float64) ** 3).long().clamp_(max=m - 1)
+    index = torch.randperm(m, device="cuda", generator=gen)[rank]
+    if case["none"]:
+        index[torch.rand(n, device="cuda", generator=gen) < case["none"]] = -1
+    if case["index"] == "pair":
+        pairs = torch.randint(m, (n, 2), device="cuda", generator=gen, dtype=torch.int32)
+        pairs[:, 0] = index
+        return pairs[:, 0]
+    return index.int() if case["index"] == "i32" else index
+
+
+def _rows(gen, n, cols, kind):
+    """Rows as embeddings are: their lengths differ."""
+    x = torch.randn(n, cols, device="cuda", generator=gen)
+    x *= torch.exp(0.5 * torch.randn(n, 1, device="cuda", generator=gen))
+    return x.to(TYPES[kind])
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    path, n, c, kind = case["path"], case["rows"], case["cols"], case["type"]
+    state = dict(case=case)
+    if path in ("lookup", "grad"):
+        state["index"] = _indices(gen, case)
+        state["scale"] = math.sqrt(c)
+        if path == "lookup":
+            state["table"] = _rows(gen, case["table"], c, kind)
+        else:
+            state["grad"] = _rows(gen, n, c, kind)
+            if case["add"]:
+                state["there"] = _rows(gen, case["table"], c, case["out_type"])
+    elif path in ("layer", "train"):
+        state["x"] = _rows(gen, n, c, kind)
+        state["weight"] = (torch.randn(case["out"], c, device="cuda", generator=gen) / math.sqrt(c)).to(TYPES[kind])
+        if case["bias"]:
+            state["bias"] = (0.1 * torch.randn(case["out"], device="cuda", generator=gen)).to(TYPES[kind])
+        if case["residual"]:
+            state["residual"] = _rows(gen, n, case["out"], kind)
+        if path == "train":
+            state["grad"] = _rows(gen, n, case["out"], kind)
+    else:
+        m, b = case["table"], case["beams"]
+        scores = 3 * torch.randn(n, m, device="cuda", generator=gen)
+        if case["none"]:
+            scores[torch.rand(n, m, device="cuda", generator=gen) < case["none"]] = -math.inf
+        state["scores"] = scores.to(TYPES[kind])
+        if b > 1:
+            state["totals"] = -30 * torch.rand(n, device="cuda", generator=gen)
+            if case["none"]:
+                state["done"] = torch.rand(n, device="cuda", generator=gen) < case["none"]
+        if c:
+            state["states"] = torch.randn(n, c, device="cuda", generator=gen)
+    return state
+
+
+# ---------------------------------------------------------------------------------------------------- plain forms
+
+
+def _act(z, act):
+    if act == "relu":
+        return z.clamp_min(0)
+    if act == "gelu":
+        return 0.5 * z * (1 + torch.erf(z * math.sqrt(0.5)))
+    return z * torch.sigmoid(z) if act == "silu" else z
+
+
+def _slope(z, act):
+    if act == "gelu":
+        return 0.5 * (1 + torch.erf(z * math.sqrt(0.5))) + z * torch.exp(-0.5 * z * z) * math.sqrt(0.5 / math.pi)
+    s = torch.sigmoid(z)
+    return s * (1 + z * (1 - s))
+
+
+def _lookup(table, index, scale, kind):
+    named = (index >= 0) & (index < table.shape[0])
+    got = table[torch.where(named, index, 0).long()].float() * scale
+    return torch.where(named.unsqueeze(1), got, 0.0).to(kind)
+
+
+def run(state):
+    case = state["case"]
+    if own:
+        return _run_own(state, case)
+    path, kind = case["path"], TYPES[case["type"]]
+    if path == "lookup":
+        return _lookup(state["table"], state["index"], state["scale"], TYPES[case["out_type"]])
+    if path == "grad":
+        index = state["index"].long()
+        sums = torch.zeros(case["table"] + 1, case["cols"], dtype=torch.float64, device="cuda")  # the last row: of no index
+        sums.index_add_(0, torch.where(index < 0, case["table"], index), state["grad"].double())
+        sums = sums[:-1] * state["scale"]
+        if case["add"]:
+            sums += state["there"]
+        return sums.to(TYPES[case["out_type"]])
+    if path == "select":
+        return _select(state, case)
+    x, w = state["x"].float(), state["weight"].float()
+    z = torch.matmul(x, w.t())
+    if case["bias"]:
+        z = z + state["bias"].float()
+    y = _act(z, case["act"])
+    if case["residual"]:
+        y = y + state["residual"].float()
+    if path == "layer":
+        return y.to(kind)
+    out = {"y": y.to(kind)}
+    g = state["grad"].float()
+    if case["act"] != "none":
+        out["pre"] = z.to(kind)  # the backward pass has it as it was kept
+        g = g * _slope(out["pre"].float(), case["act"])
+    out["grad_x"] = torch.matmul(g, w).to(kind)
+    out["grad_weight"] = torch.matmul(g.t(), x).to(kind)
+    if case["bias"]:
+        out["grad_bias"] = g.sum(0).to(kind)
+    return out
+
+
+def _select(state, case):
+    n, m, b, best = case["rows"], case["table"], case["beams"], case["best"]
+    s = state["scores"].double()
+    s = torch.where(torch.isnan(s), -math.inf, s)
+    if case["log"]:
+        s = s - s.amax(1, keepdim=True).clamp_min(-1e300)
+        s = s - torch.log(torch.exp(s).sum(1, keepdim=True))
+    if "totals" in state:
+        s = s + state["totals"].double().view(n, 1)
+    if "done" in state:
+        ended = state["done"].view(n, 1)
+        s = torch.where(ended, -math.inf, s)
+        s[:, 0:1] = torch.where(ended, state["totals"].double().view(n, 1), s[:, 0:1])
+    total, at = torch.sort(s.view(n // b, b * m), dim=1, descending=True, stable=True)
+    total, at = total[:, :best], at[:, :best]
+    some = total > -math.inf
+    first = b * torch.arange(n // b, device="cuda").view(-1, 1)
+    out = {"total": total.float(), "row": torch.where(some, at % m, -1), "parent": torch.where(some, first + at // m, -1)}
+    if case["cols"]:
+        out["states"] = _lookup(state["states"], out["parent"].view(-1), 1.0, torch.float32)
+    return out
+
+
+def _run_own(state, case):
+    import paper_1903_00757_amd as gv
+
+    path = case["path"]
+    if path == "lookup":
+        return gv.gv_lookup_rows(state["table"], state["index"], scale=state["scale"], out_type=TYPES[case["out_type"]])
+    if path == "grad":
+        if case["add"]:
+            return gv.gv_lookup_rows_backward(state["grad"], state["index"], case["table"], scale=state["scale"], out=state["there"].clone(),
+                                              add=True)
+        return gv.gv_lookup_rows_backward(state["grad"], state["index"], case["table"], scale=state["scale"], out_type=TYPES[case["out_type"]])
+    if path == "select":
+        got = gv.gv_select_rows(state["scores"], case["best"], beams=case["beams"], totals=state.get("totals"), done=state.get("done"),
+                                end=0, log_softmax=case["log"])
+        out = {"total": got.total, "row": got.row, "parent": got.parent}
+        if case["cols"]:
+            out["states"] = gv.gv_lookup_rows(state["states"], got.parent.view(-1))
+        return out
+    act = {"none": gv.GV_ACT_NONE, "relu": gv.GV_ACT_RELU, "gelu": gv.GV_ACT_GELU, "silu": gv.GV_ACT_SILU}[case["act"]]
+    train = path == "train"
+    got = gv.gv_dense_rows(state["x"], state["weight"], state.get("bias"), state.get("residual"), act=act,
+                           keep_pre=train and case["act"] != "none")
+    if not train:
+        return got.out
+    grads = gv.gv_dense_rows_backward(state["grad"], state["x"], state["weight"], got.pre, act=act, keep_bias=case["bias"])
+    out = {"y": got.out, "grad_x": grads.x, "grad_weight": grads.weight}
+    if got.pre is not None:
+        out["pre"] = got.pre
+    if case["bias"]:
+        out["grad_bias"] = grads.bias
+    return out
+
+
+# ---------------------------------------------------------------------------------------------------- what a pass cannot do without
+
+
+def work(case):
+    path, n, c, m, es = case["path"], case["rows"], case["cols"], case["table"], SIZE[case["type"]]
+    index = 8 if case["index"] == "i64" else 4
+    if path == "lookup":
+        return {"bytes": n * (index + c * (es + SIZE[case["out_type"]])), "flops": n * c}
+    if path == "grad":
+        return {"bytes": n * (index + c * es) + m * c * SIZE[case["out_type"]] * (2 if case["add"] else 1), "flops": 2 * n * c}
+    if path == "select":
+        k = n // case["beams"] * case["best"]
+        return {"bytes": n * m * es + 20 * k + 8 * k * c, "flops": (4 if case["log"] else 1) * n * m}
+    o = case["out"]
+    moved = n * c + c * o + n * o * (2 if case["residual"] else 1) + (o if case["bias"] else 0)
+    flops = 2 * n * c * o
+    if path == "train":
+        pre = 0 if case["act"] == "none" else 2 * n * o  # written, and read again
+        moved += n * o + n * c + c * o + pre + n * c + c * o + (o if case["bias"] else 0)
+        flops *= 3
+    return {"bytes": es * moved, "flops": flops}
+
+
+# ---------------------------------------------------------------------------------------------------- in 64 bits
+
+
+def exact(case, seed):
+    state = prepare(case, seed)
+    path, n = case["path"], case["rows"]
+    if path == "lookup":
+        out = torch.zeros(n, case["cols"], dtype=torch.float64, device="cuda")
+        at = torch.nonzero(state["index"] >= 0).view(-1)
+        out[at] = state["table"].index_select(0, state["index"][at].long()).double() * state["scale"]
+        return out
+    if path == "grad":
+        at = torch.nonzero(state["index"] >= 0).view(-1)
+        index, order = torch.sort(state["index"][at].long(), stable=True)
+        at = at[order]
+        ends = torch.cumsum(torch.bincount(index, minlength=case["table"]), 0)
+        out = torch.empty(case["table"], case["cols"], dtype=torch.float64, device="cuda")
+        step = max(1, (1 << 26) // max(1, at.numel()))  # columns at a time
+        for lo in range(0, case["cols"], step):
+            run_ = torch.cumsum(state["grad"][at, lo:lo + step].double(), 0)
+            run_ = torch.cat([torch.zeros_like(run_[:1]) if at.numel() else run_.new_zeros(1, run_.shape[1]), run_])
+            upto = run_[ends]
+            out[:, lo:lo + step] = torch.diff(upto, dim=0, prepend=torch.zeros_like(upto[:1])) * state["scale"]
+        return out + state["there"].double() if case["add"] else out
+    if path == "select":
+        b, best = case["beams"], case["best"]
+        some = []
+        for beam in range(n):
+            s = state["scores"][beam].double()
+            base = state["totals"][beam].double() if "totals" in state else 0.0
+            if "done" in state and bool(state["done"][beam]):
+                some.append(base.view(1))
+                continue
+            top = torch.topk(s, min(best, s.numel())).values
+            some.append(top + base - (torch.logsumexp(s, 0) if case["log"] else 0.0))
+        total = torch.full((n // b, best), -math.inf, dtype=torch.float64, device="cuda")
+        for group in range(n // b):
+            v = torch.sort(torch.cat(some[group * b:(group + 1) * b]), descending=True).values[:best]
+            total[group, :v.numel()] = v
+        out = {"total": total, "row": None, "parent": None}  # ties leave the places open
+        if case["cols"]:
+            out["states"] = None
+        return out
+    act, o = case["act"], case["out"]
+    root2 = math.sqrt(2.0)
+    w = state["weight"].double()
+    bias = state["bias"].double() if case["bias"] else torch.zeros(o, dtype=torch.float64, device="cuda")
+    step = max(1, (1 << 25) // max(case["cols"], o))  # rows at a time
+    parts, grad_w, grad_b = [], torch.zeros_like(w), torch.zeros_like(bias)
+    for lo in range(0, n, step):
+        x = state["x"][lo:lo + step].double()
+        z = torch.addmm(bias, x, w.t())
+        half = torch.special.erfc(-z / root2) / 2
+        logistic = 1 / (1 + torch.exp(-z))
+        y = {"none": z, "relu": torch.where(z > 0, z, 0.0), "gelu": z * half, "silu": z * logistic}[act]
+        if case["residual"]:
+            y = state["residual"][lo:lo + step].double() + y
+        if path == "layer":
+            parts.append({"y": y})
+            continue
+        g = state["grad"][lo:lo + step].double()
+        if act == "gelu":
+            g = g * (half + z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi))
+        elif act == "silu":
+            g = g * (logistic + z * logistic * (1 - logistic))
+        parts.append({"y": y, "grad_x": g @ w, **({} if act == "none" else {"pre": z})})
+        grad_w += g.t().contiguous() @ x
+        grad_b += g.sum(0)
+    out = {k: torch.cat([p[k] for p in parts]) for k in parts[0]}
+    if path == "layer":
+        return out["y"]
+    out["grad_weight"] = grad_w
+    if case["bias"]:
+        out["grad_bias"] = grad_b
+    return out
