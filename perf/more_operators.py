@@ -48,29 +48,29 @@ def _case(name, path, **fields):
 def listed():
     return [
         # the rows of one small query
-        _case("lookup, 64 rows, d128", "lookup", rows=64, cols=128, table=10_000),
+        _case("lookup 64 rows d128", "lookup", rows=64, cols=128, table=10_000),
         # the nodes of a million edge samples, for a head in 16 bits
-        _case("lookup, million rows, d128", "lookup", rows=1 << 20, cols=128, table=1_000_000, out_type="bf16", index="pair"),
+        _case("lookup million rows d128", "lookup", rows=1 << 20, cols=128, table=1_000_000, out_type="bf16", index="pair"),
         # a small step of a head's training: odd sizes, some places of the batch empty
-        _case("gradient, small and odd", "grad", rows=997, cols=353, table=5003, none=0.05),
+        _case("gradient small and odd", "grad", rows=997, cols=353, table=5003, none=0.05),
         # a large step: a million samples, the hottest node in every hundredth of them
-        _case("gradient, million rows, d128", "grad", rows=1 << 20, cols=128, type="bf16", table=1_000_000, index="pair"),
+        _case("gradient million rows d128", "grad", rows=1 << 20, cols=128, type="bf16", table=1_000_000, index="pair"),
         # one query through a layer
-        _case("layer, one row", "layer", rows=1, cols=512, out=2048, type="bf16", act="gelu", bias=True),
+        _case("layer one row", "layer", rows=1, cols=512, out=2048, type="bf16", act="gelu", bias=True),
         # a server's batch of queries through a wide layer
-        _case("layer, 16 rows, 4096 x 4096", "layer", rows=16, cols=4096, out=4096, type="bf16", act="silu", bias=True, residual=True),
+        _case("layer 16 rows 4096 x 4096", "layer", rows=16, cols=4096, out=4096, type="bf16", act="silu", bias=True, residual=True),
         # a deep head's wide layer on a large batch
-        _case("layer, 8192 rows, 4096 x 4096", "layer", rows=8192, cols=4096, out=4096, type="bf16", act="gelu", bias=True, residual=True),
+        _case("layer 8192 rows 4096 x 4096", "layer", rows=8192, cols=4096, out=4096, type="bf16", act="gelu", bias=True, residual=True),
         # a small odd step in full precision
-        _case("train, small and odd", "train", rows=1021, cols=357, out=500, type="f32", act="silu", bias=True),
+        _case("train small and odd", "train", rows=1021, cols=357, out=500, type="f32", act="silu", bias=True),
         # a large step on rows of a trained length
-        _case("train, 65536 rows, 512 x 2048", "train", rows=65_536, cols=512, out=2048, type="bf16", act="gelu", bias=True),
+        _case("train 65536 rows 512 x 2048", "train", rows=65_536, cols=512, out=2048, type="bf16", act="gelu", bias=True),
         # the nodes that follow one query's
-        _case("select, one query", "select", rows=1, table=10_000, best=10, log=True),
+        _case("select one query", "select", rows=1, table=10_000, best=10, log=True),
         # a shortlist for each of a server's batch of queries
-        _case("select, 64 queries, best 100", "select", rows=64, table=1_000_000, best=100),
+        _case("select 64 queries best 100", "select", rows=64, table=1_000_000, best=100),
         # the likeliest paths from 16 nodes, eight of each
-        _case("select, 16 x 8 beams", "select", rows=128, cols=512, table=1_000_000, beams=8, best=8, log=True, none=0.05),
+        _case("select 16 x 8 beams", "select", rows=128, cols=512, table=1_000_000, beams=8, best=8, log=True, none=0.05),
     ]
 
 
