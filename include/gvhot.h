@@ -370,11 +370,12 @@ int gv_link_prediction_auc(gv_ctx *ctx, const uint32_t *host_edge_first, const u
  * and can be captured into a graph; gv_last_error(NULL) has the text of a refusal.  The matrices of a context may be
  * passed (gv_device_embeddings) once gv_sync has waited for their training.
  * A matrix of `rows` rows is a pointer, aligned to its values, and a stride: the values from one row to the next, at least
- * cols (the values of a row lie together).  GV_F32 = float, GV_BF16 = bfloat16, GV_F16 = IEEE half, GV_I8 = int8.
+ * cols (the values of a row lie together).  GV_F32 = float, GV_BF16 = bfloat16, GV_F16 = IEEE half, GV_I8 = int8; GV_I32 = int32
+ * and GV_I64 = int64 are types of indices and of what gv_lookup_rows copies.
  * rows <= 2^31, 1 <= cols <= GV_MAX_ROW_COLS; rows = 0 is an empty call.  An output may be the very matrix (pointer, stride and
  * type) of an input of the same call; matrices that overlap otherwise leave undefined values.
  * Arithmetic is fp32 whatever the types; a result is rounded once, to nearest even, when it is written.          */
-enum { GV_F32 = 0, GV_BF16 = 1, GV_F16 = 2, GV_I8 = 3 };
+enum { GV_F32 = 0, GV_BF16 = 1, GV_F16 = 2, GV_I8 = 3, GV_I32 = 4, GV_I64 = 5 };
 #define GV_MAX_ROW_COLS 16384u
 
 /* Dropout: out = keep ? x * 65536 / (65536 - t) : 0, t = floor(65536 drop + 1/2), 0 <= drop, t < 65536.  keep(i, c) holds
@@ -431,6 +432,26 @@ int gv_quantize_rows(uint64_t rows, uint32_t cols, int type, const void *dev_x, 
 int gv_score_rows(uint64_t rows, uint32_t cols, uint32_t group, const uint8_t *dev_codes, const uint16_t *dev_scales,
                   uint64_t queries, int type, const void *dev_x, uint64_t x_stride, const float *dev_x_scale, float *dev_out,
                   uint64_t out_stride, void *stream);
+
+/* Rows by index: out[t] = scale * table[index[t]], t < count.  An index is GV_I32 or GV_I64, index[t] lies t * index_stride values
+ * behind the first (a column of a pool has stride 2); one that names no row (negative, or >= rows) gives a row of zeros.
+ * table has `rows` rows of `type`, out `count` rows of out_type: GV_F32, GV_BF16 and GV_F16 in any pair, or the same type of whole
+ * numbers with scale 1.  With scale 1 and one type, values are copied bit by bit.  out may not overlap the table.  count <= 2^31;
+ * count = 0 is an empty call, and a table of no rows gives zeros.                                                    */
+int gv_lookup_rows(uint64_t count, const void *dev_index, uint64_t index_stride, int index_type, uint64_t rows, uint32_t cols, int type,
+                   const void *dev_table, uint64_t table_stride, float scale, int out_type, void *dev_out, uint64_t out_stride,
+                   void *stream);
+/* Its gradient, from grad (of out, `count` rows of `type`) for the table:
+ *   out[i] = (add ? out[i] : 0) + scale * sum over the t with index[t] = i of grad[t]
+ * of out_type, `rows` rows; type and out_type are GV_F32, GV_BF16 or GV_F16 in any pair.  Rows that no index names become 0,
+ * or with add stay as they are, untouched: with the table itself as out and a negative scale, add makes a step of descent on the
+ * rows that the batch names.  Sums are fp32, in an order that the indices decide: a call gives the same bits each time.  grad and out
+ * may not overlap.  dev_workspace points to workspace_bytes bytes (at least those of gv_lookup_rows_workspace, which may be none;
+ * aligned to 16) that the call may overwrite.                                                                          */
+int gv_lookup_rows_workspace(uint64_t count, uint64_t rows, uint32_t cols, int add, uint64_t *bytes);
+int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t index_stride, int index_type, uint64_t rows, uint32_t cols,
+                            int type, const void *dev_grad, uint64_t grad_stride, float scale, int add, int out_type, void *dev_out,
+                            uint64_t out_stride, void *dev_workspace, uint64_t workspace_bytes, void *stream);
 
 /* Wait for all queued device work of the context; folds event timings into the
  * statistics; reports samples that named an id >= n (GV_EINVAL, once), and training that has

@@ -20,7 +20,7 @@ GV_MAX_POOL_SLOTS = 16
 GV_STATIC_SCRATCH_WORDS = 1 << 22
 GV_MAX_PARTITIONS = 64
 GV_SHUFFLE_NONE, GV_SHUFFLE_PSEUDO = 0, 1
-GV_F32, GV_BF16, GV_F16, GV_I8 = 0, 1, 2, 3
+GV_F32, GV_BF16, GV_F16, GV_I8, GV_I32, GV_I64 = 0, 1, 2, 3, 4, 5
 GV_MAX_ROW_COLS = 16384
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgvhot.so")
@@ -34,6 +34,7 @@ EXPORTS = [
     "gv_get_partitions", "gv_redistribute_pool", "gv_train_device_blocks", "gv_draw_negatives_partitioned",
     "gv_build_walk_tables", "gv_augment_weighted", "gv_set_weighted_graph",
     "gv_drop_rows", "gv_norm_rows", "gv_norm_rows_workspace", "gv_norm_rows_backward", "gv_quantize_rows", "gv_score_rows",
+    "gv_lookup_rows", "gv_lookup_rows_workspace", "gv_lookup_rows_backward",
 ]
 
 
@@ -131,6 +132,10 @@ def load():
                                         vp, vp, u64, vp]
     L.gv_quantize_rows.argtypes = [u64, u32, i32, vp, u64, u32, vp, vp, vp]
     L.gv_score_rows.argtypes = [u64, u32, u32, vp, vp, u64, i32, vp, u64, vp, vp, u64, vp]
+    flt = C.c_float
+    L.gv_lookup_rows.argtypes = [u64, vp, u64, i32, u64, u32, i32, vp, u64, flt, i32, vp, u64, vp]
+    L.gv_lookup_rows_workspace.argtypes = [u64, u64, u32, i32, u64p]
+    L.gv_lookup_rows_backward.argtypes = [u64, vp, u64, i32, u64, u32, i32, vp, u64, flt, i32, i32, vp, u64, vp, u64, vp]
     for name in EXPORTS:
         if name not in ("gv_destroy", "gv_last_error"):
             getattr(L, name).restype = C.c_int

@@ -1,5 +1,5 @@
 // Internal interface between the checks of the operators on rows (gv_rows_api.cpp) and their kernels
-// (gv_rows.hip, gv_scores.hip).  Not part of the C boundary.
+// (gv_rows.hip, gv_scores.hip, gv_lookup.hip).  Not part of the C boundary.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -78,6 +78,38 @@ struct ScoreArgs {
     int type;
 };
 
+struct Index {
+    const void *at;
+    uint64_t stride;
+    int type;  // GV_I32 or GV_I64
+};
+
+struct LookupArgs {
+    Index index;
+    const void *table;
+    void *out;
+    uint64_t count, table_stride, out_stride;
+    uint32_t rows, cols;  // of the table
+    int type, out_type;
+    float scale;
+};
+
+struct LookupGradArgs {
+    Index index;
+    const void *grad;
+    void *out;
+    uint64_t count, grad_stride, out_stride;
+    uint32_t rows, cols;  // of the result
+    int type, out_type;
+    float scale;
+    bool add;
+    // of the workspace, and how the batch is cut
+    uint32_t *keys, *order, *digit_counts, *digit_totals;
+    uint8_t *flags;
+    float *partial;
+    uint32_t lanes, chunk, chunks;
+};
+
 // Launches a kernel.  hipLaunchKernel says itself what became of it: the thread's last error may be of a call before, and is its
 // caller's to ask for; that of a launch is returned here and left to nobody else.
 template <class... Parameters, class... Arguments>
@@ -98,5 +130,8 @@ hipError_t launch_norm_grad(const NormGradArgs &a, hipStream_t stream);
 hipError_t launch_drop(const DropRowsArgs &a, hipStream_t stream);
 hipError_t launch_quantize(const QuantizeArgs &a, hipStream_t stream);
 hipError_t launch_score(const ScoreArgs &a, hipStream_t stream);
+hipError_t launch_lookup(const LookupArgs &a, hipStream_t stream);
+uint64_t lookup_grad_workspace(uint64_t count, uint64_t rows, uint32_t cols, bool add);
+hipError_t launch_lookup_grad(const LookupGradArgs &a, void *workspace, hipStream_t stream);
 
 }  // namespace gv

@@ -8,13 +8,15 @@
 #include "gv_host.hpp"
 #include "gv_rows.hpp"
 
+#define GV_TRY(expr) do { const int rc_ = (expr); if (rc_ != GV_OK) return rc_; } while (0)
+
 namespace {
 
 using gv::fail_call;
 
 constexpr uint64_t kMostRows = 1ull << 31, kMostStride = 1ull << 40, kMostQueries = 1ull << 16;
 
-uint32_t size_of(int type) { return type == GV_F32 ? 4u : type == GV_I8 ? 1u : 2u; }
+uint32_t size_of(int type) { return type == GV_F32 || type == GV_I32 ? 4u : type == GV_I8 ? 1u : type == GV_I64 ? 8u : 2u; }
 
 struct Matrix {
     const char *name;
@@ -55,6 +57,33 @@ int drop_args(const char *call, double drop, uint64_t seed, uint64_t first_row, 
     return GV_OK;
 }
 
+int check_index(const char *call, const gv::Index &index, uint64_t count, uint64_t rows) {
+    if (count > kMostRows) return fail_call(GV_EINVAL, "%s: %llu indices: at most 2^31", call, (unsigned long long)count);
+    if (rows > kMostRows) return fail_call(GV_EINVAL, "%s: %llu rows: at most 2^31", call, (unsigned long long)rows);
+    if (index.type != GV_I32 && index.type != GV_I64)
+        return fail_call(GV_EINVAL, "%s: index_type %d: GV_I32 or GV_I64", call, index.type);
+    if (count == 0) return GV_OK;
+    if (index.stride > kMostStride)
+        return fail_call(GV_EINVAL, "%s: stride %llu of index: at most 2^40", call, (unsigned long long)index.stride);
+    return check_array(call, "index", index.at, size_of(index.type));
+}
+
+// Whether two matrices share memory.
+bool overlap(const Matrix &a, uint64_t a_rows, const Matrix &b, uint64_t b_rows, uint32_t cols) {
+    if (a_rows == 0 || b_rows == 0) return false;
+    const uintptr_t a_end = (uintptr_t)a.at + ((a_rows - 1) * a.stride + cols) * size_of(a.type);
+    const uintptr_t b_end = (uintptr_t)b.at + ((b_rows - 1) * b.stride + cols) * size_of(b.type);
+    return (uintptr_t)a.at < b_end && (uintptr_t)b.at < a_end;
+}
+
+int check_workspace(const char *call, const void *workspace, uint64_t bytes, uint64_t need) {
+    if (need > 0) GV_TRY(check_array(call, "workspace", workspace, 16));
+    if (bytes < need)
+        return fail_call(GV_EINVAL, "%s: workspace of %llu bytes: %llu are needed", call, (unsigned long long)bytes,
+                         (unsigned long long)need);
+    return GV_OK;
+}
+
 uint64_t workspace_of(uint64_t rows, uint32_t cols) {
     const uint32_t parts = gv::norm_grad_parts(rows, cols);
     return parts > 1 ? 4ull * parts * cols : 0;
@@ -65,8 +94,6 @@ int launched(const char *call, hipError_t e) {
 }
 
 }  // namespace
-
-#define GV_TRY(expr) do { const int rc_ = (expr); if (rc_ != GV_OK) return rc_; } while (0)
 
 extern "C" {
 
@@ -173,6 +200,57 @@ int gv_score_rows(uint64_t rows, uint32_t cols, uint32_t group, const uint8_t *d
                          (unsigned long long)rows);
     return launched(call, gv::launch_score({dev_codes, dev_scales, dev_x, dev_x_scale, dev_out, rows, queries, x_stride, out_stride,
                                             cols, group, type}, (hipStream_t)stream));
+}
+
+int gv_lookup_rows(uint64_t count, const void *dev_index, uint64_t index_stride, int index_type, uint64_t rows, uint32_t cols, int type,
+                   const void *dev_table, uint64_t table_stride, float scale, int out_type, void *dev_out, uint64_t out_stride,
+                   void *stream) {
+    const char *call = "gv_lookup_rows";
+    const gv::Index index{dev_index, index_stride, index_type};
+    if (type < GV_F32 || type > GV_I64) return fail_call(GV_EINVAL, "%s: bad type %d", call, type);
+    GV_TRY(check_shape(call, rows, cols, GV_F32, false));
+    if (type > GV_F16) {
+        if (out_type != type || scale != 1.0f) return fail_call(GV_EINVAL, "%s: whole numbers are copied: out_type is type, scale 1", call);
+    } else if (out_type < GV_F32 || out_type > GV_F16) {
+        return fail_call(GV_EINVAL, "%s: bad out_type %d", call, out_type);
+    }
+    GV_TRY(check_index(call, index, count, rows));
+    if (count == 0) return GV_OK;
+    const Matrix table{"table", dev_table, table_stride, type}, out{"out", dev_out, out_stride, out_type};
+    if (rows > 0) GV_TRY(check_matrices(call, cols, {table}));
+    GV_TRY(check_matrices(call, cols, {out}));
+    if (overlap(table, rows, out, count, cols)) return fail_call(GV_EINVAL, "%s: out overlaps the table", call);
+    return launched(call, gv::launch_lookup({index, dev_table, dev_out, count, table_stride, out_stride, (uint32_t)rows, cols, type, out_type,
+                                             scale}, (hipStream_t)stream));
+}
+
+int gv_lookup_rows_workspace(uint64_t count, uint64_t rows, uint32_t cols, int add, uint64_t *bytes) {
+    const char *call = "gv_lookup_rows_workspace";
+    if (count > kMostRows) return fail_call(GV_EINVAL, "%s: %llu indices: at most 2^31", call, (unsigned long long)count);
+    GV_TRY(check_shape(call, rows, cols, GV_F32, false));
+    if (!bytes) return fail_call(GV_EINVAL, "%s: null output", call);
+    *bytes = gv::lookup_grad_workspace(count, rows, cols, add != 0);
+    return GV_OK;
+}
+
+int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t index_stride, int index_type, uint64_t rows, uint32_t cols,
+                            int type, const void *dev_grad, uint64_t grad_stride, float scale, int add, int out_type, void *dev_out,
+                            uint64_t out_stride, void *dev_workspace, uint64_t workspace_bytes, void *stream) {
+    const char *call = "gv_lookup_rows_backward";
+    const gv::Index index{dev_index, index_stride, index_type};
+    GV_TRY(check_shape(call, rows, cols, type, false));
+    if (out_type < GV_F32 || out_type > GV_F16) return fail_call(GV_EINVAL, "%s: bad out_type %d", call, out_type);
+    GV_TRY(check_index(call, index, count, rows));
+    if (rows == 0 || (count == 0 && add)) return GV_OK;
+    const Matrix grad{"grad", dev_grad, grad_stride, type}, out{"out", dev_out, out_stride, out_type};
+    if (count > 0) GV_TRY(check_matrices(call, cols, {grad}));
+    GV_TRY(check_matrices(call, cols, {out}));
+    if (overlap(grad, count, out, rows, cols)) return fail_call(GV_EINVAL, "%s: out overlaps grad", call);
+    GV_TRY(check_workspace(call, dev_workspace, workspace_bytes, gv::lookup_grad_workspace(count, rows, cols, add != 0)));
+    gv::LookupGradArgs a{};
+    a.index = index, a.grad = dev_grad, a.out = dev_out, a.count = count, a.grad_stride = grad_stride, a.out_stride = out_stride;
+    a.rows = (uint32_t)rows, a.cols = cols, a.type = type, a.out_type = out_type, a.scale = scale, a.add = add != 0;
+    return launched(call, gv::launch_lookup_grad(a, dev_workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

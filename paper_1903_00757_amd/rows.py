@@ -15,14 +15,17 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from .binding import GV_BF16, GV_F16, GV_F32, GV_I8, GV_OK, GvError, load
+from .binding import GV_BF16, GV_F16, GV_F32, GV_I8, GV_I32, GV_I64, GV_OK, GvError, load
 
 __all__ = ["NormRows", "NormGrads", "gv_drop_rows", "gv_norm_rows", "gv_norm_rows_workspace", "gv_norm_rows_backward",
-           "gv_quantize_rows", "gv_score_rows"]
+           "gv_quantize_rows", "gv_score_rows", "gv_lookup_rows", "gv_lookup_rows_workspace", "gv_lookup_rows_backward"]
 
 _TYPES = {torch.float32: GV_F32, torch.bfloat16: GV_BF16, torch.float16: GV_F16}
 _TYPES_AND_BYTES = dict(_TYPES)
 _TYPES_AND_BYTES[torch.int8] = GV_I8
+_TYPES_AND_WHOLE = dict(_TYPES_AND_BYTES)
+_TYPES_AND_WHOLE.update({torch.uint8: GV_I8, torch.bool: GV_I8, torch.int32: GV_I32, torch.int64: GV_I64})
+_INDICES = {torch.int32: GV_I32, torch.int64: GV_I64}
 
 
 class NormRows(NamedTuple):
@@ -249,6 +252,82 @@ def gv_score_rows(codes, scales, x, *, group=32, scale=None, out=None):
         _without_graph(x, scales, scale, out)
     _call(load().gv_score_rows, gpu, rows, cols, group, codes_at, scales_at, queries, kind, at, stride, scale_at, out_at,
           out_stride)
+    if passed:
+        _written(out)
+    return out
+
+
+def _index(t, gpu):
+    """(address, stride, count, type) of the indices of a batch."""
+    kind = _INDICES.get(t.dtype)
+    if kind is None or t.get_device() != gpu:
+        _refuse("index: int32 or int64 on the same GPU are asked for")
+    if t.dim() != 1:
+        _refuse("index: a 1-D tensor")
+    return t.data_ptr(), t.stride(0), t.numel(), kind
+
+
+def gv_lookup_rows(table, index, *, scale=1.0, out_type=None, out=None):
+    """Rows of the table by index (a 1-D tensor, a column of pairs for instance), times scale; zeros where an index names no
+    row.  Types of whole numbers are copied.  The gradient of the table is gv_lookup_rows_backward."""
+    at, stride, rows, cols, kind, gpu = _first("table", table, _TYPES_AND_WHOLE)
+    index_at, index_stride, count, index_kind = _index(index, gpu)
+    passed = out is not None
+    dtype = out_type or (out.dtype if passed else table.dtype)
+    out_kind = kind if dtype is table.dtype else _TYPES.get(dtype)
+    if out_kind is None or (out_kind != kind and kind > GV_F16):
+        _refuse("out: float32, bfloat16 or float16, or the table's type")
+    if passed:
+        out_at, out_stride = _rows("out", out, count, cols, dtype, gpu)
+    else:
+        out = table.new_empty((count, cols), dtype=dtype)
+        out_at, out_stride = out.data_ptr(), cols
+    if _recording() and (table.requires_grad or passed):
+        _without_graph(table, out)
+    _call(load().gv_lookup_rows, gpu, count, index_at, index_stride, index_kind, rows, cols, kind, at, stride, scale, out_kind, out_at,
+          out_stride)
+    if passed:
+        _written(out)
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def gv_lookup_rows_workspace(count, rows, cols, add=False):
+    """Bytes of scratch that the gradient of a batch of `count` rows takes."""
+    n = C.c_uint64()
+    rc = load().gv_lookup_rows_workspace(count, rows, cols, 1 if add else 0, C.byref(n))
+    if rc != GV_OK:
+        raise GvError(rc, load().gv_last_error(None).decode())
+    return n.value
+
+
+def gv_lookup_rows_backward(grad_out, index, rows, *, scale=1.0, out_type=None, out=None, add=False):
+    """The gradient of a table of `rows` rows: the rows of grad_out added up by index, times scale.  With add, out's rows that the
+    batch names get theirs added and the others stay: gv_lookup_rows_backward(g, index, n, scale=-rate, out=table, add=True) is a
+    step on the table."""
+    at, stride, count, cols, kind, gpu = _first("grad_out", grad_out)
+    index_at, index_stride, named, index_kind = _index(index, gpu)
+    if named != count:
+        _refuse(f"index: {count} of them are asked for")
+    passed = out is not None
+    if add and not passed:
+        _refuse("add: out is asked for")
+    dtype = out_type or (out.dtype if passed else grad_out.dtype)
+    out_kind = _TYPES.get(dtype)
+    if out_kind is None:
+        _refuse("out: float32, bfloat16 or float16")
+    if passed:
+        out_at, out_stride = _rows("out", out, rows, cols, dtype, gpu)
+    else:
+        out = grad_out.new_empty((rows, cols), dtype=dtype)
+        out_at, out_stride = out.data_ptr(), cols
+    if _recording() and (grad_out.requires_grad or passed):
+        _without_graph(grad_out, out)
+    add = bool(add)
+    size = gv_lookup_rows_workspace(count, rows, cols, add)
+    space = torch.empty(size, dtype=_uint8, device=grad_out.device) if size else None
+    _call(load().gv_lookup_rows_backward, gpu, count, index_at, index_stride, index_kind, rows, cols, kind, at, stride, scale, add, out_kind,
+          out_at, out_stride, space.data_ptr() if size else None, size)
     if passed:
         _written(out)
     return out
