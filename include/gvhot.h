@@ -377,6 +377,8 @@ int gv_link_prediction_auc(gv_ctx *ctx, const uint32_t *host_edge_first, const u
  * Arithmetic is fp32 whatever the types; a result is rounded once, to nearest even, when it is written.          */
 enum { GV_F32 = 0, GV_BF16 = 1, GV_F16 = 2, GV_I8 = 3, GV_I32 = 4, GV_I64 = 5 };
 #define GV_MAX_ROW_COLS 16384u
+#define GV_MAX_BEAMS 512u
+#define GV_MAX_BEST 1024u
 
 /* Dropout: out = keep ? x * 65536 / (65536 - t) : 0, t = floor(65536 drop + 1/2), 0 <= drop, t < 65536.  keep(i, c) holds
  * when 16-bit number c mod 8 of Philox block (first_row + i, c / 8) of stream 5 of `seed` is not below t (number 2 w is the
@@ -452,6 +454,24 @@ int gv_lookup_rows_workspace(uint64_t count, uint64_t rows, uint32_t cols, int a
 int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t index_stride, int index_type, uint64_t rows, uint32_t cols,
                             int type, const void *dev_grad, uint64_t grad_stride, float scale, int add, int out_type, void *dev_out,
                             uint64_t out_stride, void *dev_workspace, uint64_t workspace_bytes, void *stream);
+
+/* The best rows over the scores of beams, as gv_score_rows gives them.  queries = groups x beams; the beams b of a group share a
+ * selection of `best` out of all (b, i), row i of beam b counting
+ *   totals[b] + scores[b][i] - log sum over i' of exp(scores[b][i'])    (log_softmax)
+ *   totals[b] + scores[b][i]                                            (otherwise)
+ * (dev_totals NULL: 0), the largest first; of equal ones the lower beam's, then the higher score, then the lower row.  What counts is
+ * taken in fp64.  dev_parent, dev_row and dev_total [groups][best] receive b (counted over all queries: what gv_lookup_rows takes to
+ * reorder what belongs to the beams), i, and what they count, rounded to float.  Scores of -inf and NaN are never selected and have
+ * no share in the sum; of scores of +inf each counts as an equal share.  A beam whose total is not finite offers nothing; one with
+ * dev_done[b] != 0 (may be NULL) offers row `end` (< rows) alone, with its total as it is, whatever its scores are.  Where
+ * there is less to select than `best`, parent and row are -1 and total -inf.
+ * scores are of `type` (GV_F32, GV_BF16, GV_F16), scores_stride >= rows.  queries <= 65536, rows <= 2^31, beams <= GV_MAX_BEAMS, best <=
+ * GV_MAX_BEST; queries = 0 is an empty call.  dev_workspace points to workspace_bytes bytes (at least those of
+ * gv_select_rows_workspace, which may be none; aligned to 16) that the call may overwrite.                              */
+int gv_select_rows_workspace(uint64_t queries, uint64_t rows, uint32_t beams, uint32_t best, uint64_t *bytes);
+int gv_select_rows(uint64_t queries, uint64_t rows, int type, const void *dev_scores, uint64_t scores_stride, uint32_t beams,
+                   const float *dev_totals, const uint8_t *dev_done, uint64_t end, int log_softmax, uint32_t best, int64_t *dev_parent,
+                   int64_t *dev_row, float *dev_total, void *dev_workspace, uint64_t workspace_bytes, void *stream);
 
 /* Wait for all queued device work of the context; folds event timings into the
  * statistics; reports samples that named an id >= n (GV_EINVAL, once), and training that has

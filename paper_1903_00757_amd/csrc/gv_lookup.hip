@@ -95,7 +95,7 @@ __device__ __forceinline__ void join_groups(float (&v)[8], float (*scratch)[8], 
 constexpr uint32_t kFew = 1024, kFillRows = 4096;
 
 template <class In, class Out>
-__global__ __launch_bounds__(kGradThreads) void k_grad_few(LookupGradArgs a, uint32_t parts, uint32_t fill_blocks) {
+__global__ __launch_bounds__(kGradThreads) void k_grad_few(LookupGradArgs a, uint32_t parts, uint32_t fill_blocks, uint32_t fill_rows) {
     constexpr int kEach = kFew / kGradThreads;
     __shared__ float scratch[kGradThreads][8];
     __shared__ uint16_t same[kFew];
@@ -103,8 +103,8 @@ __global__ __launch_bounds__(kGradThreads) void k_grad_few(LookupGradArgs a, uin
     const uint32_t tid = threadIdx.x, count = (uint32_t)a.count;
     if (blockIdx.x >= count * parts) {
         const uint64_t pieces = (a.cols + 7) / 8;
-        for (uint64_t first = (uint64_t)(blockIdx.x - count * parts) * kFillRows; first < a.rows; first += (uint64_t)fill_blocks * kFillRows) {
-            const uint32_t some = (uint32_t)std::min<uint64_t>(kFillRows, a.rows - first);
+        for (uint64_t first = (uint64_t)(blockIdx.x - count * parts) * fill_rows; first < a.rows; first += (uint64_t)fill_blocks * fill_rows) {
+            const uint32_t some = (uint32_t)std::min<uint64_t>(fill_rows, a.rows - first);
             for (uint32_t w = tid; w < kFillRows / 32; w += kGradThreads) named[w] = 0;
             __syncthreads();
             for (uint32_t t = tid; t < count; t += kGradThreads) {
@@ -530,11 +530,14 @@ hipError_t launch_lookup_grad(const LookupGradArgs &args, void *workspace, hipSt
     if (a.count <= kFew) {
         a.lanes = lanes_of(a.cols);
         const uint32_t parts = (a.cols + 511) / 512;
-        const uint32_t fill = a.add ? 0 : (uint32_t)std::min<uint64_t>((a.rows + kFillRows - 1) / kFillRows, 1 << 16);
+        // rows that a workgroup writes zeros to: 16 KB of them at least, and a thousand workgroups where that is enough
+        const uint64_t each = std::max<uint64_t>(std::max<uint64_t>(1, 512 / pieces), (a.rows + 1023) / 1024);
+        const uint32_t fill_rows = (uint32_t)std::min<uint64_t>(each, kFillRows);
+        const uint32_t fill = a.add ? 0 : (uint32_t)std::min<uint64_t>((a.rows + fill_rows - 1) / fill_rows, 1 << 16);
         if (a.count == 0 && fill == 0) return hipSuccess;
         return by_types(a.type, a.out_type, [&](auto *i, auto *o) {
             return launch(k_grad_few<std::remove_pointer_t<decltype(i)>, std::remove_pointer_t<decltype(o)>>, (uint32_t)a.count * parts + fill,
-                          kGradThreads, 0, stream, a, parts, fill);
+                          kGradThreads, 0, stream, a, parts, fill, fill_rows);
         });
     }
     const Plan p = plan_of(a.count, a.rows, a.cols, a.add);

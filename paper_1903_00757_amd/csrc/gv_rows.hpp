@@ -1,5 +1,5 @@
 // Internal interface between the checks of the operators on rows (gv_rows_api.cpp) and their kernels
-// (gv_rows.hip, gv_scores.hip, gv_lookup.hip).  Not part of the C boundary.
+// (gv_rows.hip, gv_scores.hip, gv_lookup.hip, gv_select.hip).  Not part of the C boundary.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -110,6 +110,21 @@ struct LookupGradArgs {
     uint32_t lanes, chunk, chunks;
 };
 
+struct SelectArgs {
+    const void *scores;
+    const float *totals;   // may be null
+    const uint8_t *done;   // may be null
+    int64_t *parent, *row;
+    float *total;
+    uint64_t queries, rows, stride;
+    uint32_t beams, best, end;
+    int type;
+    bool log_softmax;
+    // of the workspace, and how scores are cut
+    void *summaries, *candidates;
+    uint32_t parts, part_rows, slots;
+};
+
 // Launches a kernel.  hipLaunchKernel says itself what became of it: the thread's last error may be of a call before, and is its
 // caller's to ask for; that of a launch is returned here and left to nobody else.
 template <class... Parameters, class... Arguments>
@@ -132,6 +147,8 @@ hipError_t launch_quantize(const QuantizeArgs &a, hipStream_t stream);
 hipError_t launch_score(const ScoreArgs &a, hipStream_t stream);
 hipError_t launch_lookup(const LookupArgs &a, hipStream_t stream);
 uint64_t lookup_grad_workspace(uint64_t count, uint64_t rows, uint32_t cols, bool add);
+uint64_t select_workspace(uint64_t queries, uint64_t rows, uint32_t beams, uint32_t best);
+hipError_t launch_select(const SelectArgs &a, void *workspace, hipStream_t stream);
 hipError_t launch_lookup_grad(const LookupGradArgs &a, void *workspace, hipStream_t stream);
 
 }  // namespace gv

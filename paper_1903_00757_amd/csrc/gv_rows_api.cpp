@@ -253,4 +253,46 @@ int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t inde
     return launched(call, gv::launch_lookup_grad(a, dev_workspace, (hipStream_t)stream));
 }
 
+static int check_select(const char *call, uint64_t queries, uint64_t rows, uint32_t beams, uint32_t best) {
+    if (queries > kMostQueries) return fail_call(GV_EINVAL, "%s: %llu queries: at most 2^16", call, (unsigned long long)queries);
+    if (rows > kMostRows) return fail_call(GV_EINVAL, "%s: %llu rows: at most 2^31", call, (unsigned long long)rows);
+    if (beams == 0 || beams > GV_MAX_BEAMS) return fail_call(GV_EINVAL, "%s: %u beams: 1..%u", call, beams, GV_MAX_BEAMS);
+    if (queries % beams) return fail_call(GV_EINVAL, "%s: %llu queries are no groups of %u beams", call, (unsigned long long)queries, beams);
+    if (best == 0 || best > GV_MAX_BEST) return fail_call(GV_EINVAL, "%s: the best %u: 1..%u", call, best, GV_MAX_BEST);
+    return GV_OK;
+}
+
+int gv_select_rows_workspace(uint64_t queries, uint64_t rows, uint32_t beams, uint32_t best, uint64_t *bytes) {
+    const char *call = "gv_select_rows_workspace";
+    GV_TRY(check_select(call, queries, rows, beams, best));
+    if (!bytes) return fail_call(GV_EINVAL, "%s: null output", call);
+    *bytes = gv::select_workspace(queries, rows, beams, best);
+    return GV_OK;
+}
+
+int gv_select_rows(uint64_t queries, uint64_t rows, int type, const void *dev_scores, uint64_t scores_stride, uint32_t beams,
+                   const float *dev_totals, const uint8_t *dev_done, uint64_t end, int log_softmax, uint32_t best, int64_t *dev_parent,
+                   int64_t *dev_row, float *dev_total, void *dev_workspace, uint64_t workspace_bytes, void *stream) {
+    const char *call = "gv_select_rows";
+    GV_TRY(check_select(call, queries, rows, beams, best));
+    if (type < GV_F32 || type > GV_F16) return fail_call(GV_EINVAL, "%s: bad type %d", call, type);
+    if (dev_done && end >= rows)
+        return fail_call(GV_EINVAL, "%s: end %llu: a row of %llu", call, (unsigned long long)end, (unsigned long long)rows);
+    if (queries == 0) return GV_OK;
+    if (rows > 0) GV_TRY(check_array(call, "scores", dev_scores, size_of(type)));
+    if (scores_stride < rows || scores_stride > kMostStride)
+        return fail_call(GV_EINVAL, "%s: stride %llu of scores: rows (%llu)..2^40", call, (unsigned long long)scores_stride,
+                         (unsigned long long)rows);
+    if (dev_totals) GV_TRY(check_array(call, "totals", dev_totals, 4));
+    GV_TRY(check_array(call, "parent", dev_parent, 8));
+    GV_TRY(check_array(call, "row", dev_row, 8));
+    GV_TRY(check_array(call, "total", dev_total, 4));
+    GV_TRY(check_workspace(call, dev_workspace, workspace_bytes, gv::select_workspace(queries, rows, beams, best)));
+    gv::SelectArgs a{};
+    a.scores = dev_scores, a.totals = dev_totals, a.done = dev_done, a.parent = dev_parent, a.row = dev_row, a.total = dev_total;
+    a.queries = queries, a.rows = rows, a.stride = scores_stride, a.beams = beams, a.best = best, a.end = (uint32_t)end, a.type = type;
+    a.log_softmax = log_softmax != 0;
+    return launched(call, gv::launch_select(a, dev_workspace, (hipStream_t)stream));
+}
+
 }  // extern "C"

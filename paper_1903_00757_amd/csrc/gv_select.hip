@@ -1,0 +1,541 @@
+// gfx950 kernels of the selection of the best rows over the scores of beams.
+//
+// A score s of beam b counts total[b] + (s - M) - log sum exp(s' - M), M the largest of the beam (or total[b] + s).  Within a beam
+// that is the order of the scores, so one pass over them is enough: every workgroup reads a part of a beam, keeps what may be among its best
+// in LDS and adds up the exponentials; a workgroup of each group joins the sums, and ranks what is left of the beams by what it counts.
+//
+// What may be among the best is told by a bound, a value that at least `best` scores seen so far reach.  The largest score of each
+// thread is one of them, and in a wave the k-th largest of its lanes' takes 32 steps of a ballot: with every wave's
+// ceil(best / waves)-th, the least of those is reached by `best` scores.  For scores in no special order some 1.3 `best` reach it.
+// Scores that do are few, and what few there are is kept; where they are more than there is room for, as with equal scores, the
+// bound is made exact by a search over the bits of (score, row), and `best` are left.
+#include "gv_row_pieces.hpp"
+#include "gv_rows.hpp"
+#include "gvhot.h"
+
+#include <algorithm>
+#include <type_traits>
+
+#pragma clang fp contract(off)
+
+namespace gv {
+namespace {
+
+constexpr int kThreads = 512, kWaves = kThreads / 64, kEach = 16;
+constexpr uint32_t kTile = kThreads * kEach, kSlots = 2048;  // scores of a turn; candidates that LDS has room for
+constexpr float kLowest = -3.402823466e38f;
+static_assert(GV_MAX_BEST <= kSlots / 2, "room for the best and as many");
+
+struct Candidate {
+    float score;
+    uint32_t row;
+};
+// What a workgroup leaves of its part.
+struct Part {
+    double sum;      // of exp(score - top)
+    float top;       // -inf: there is no score
+    float bound;     // at least `best` scores of the part reach it; -inf where that is not known
+    uint32_t count;  // of its candidates
+    uint32_t unused;
+};
+
+__device__ __forceinline__ float infinity() { return __builtin_inff(); }
+
+// Numbers in the order of the floats (no NaN; -0 comes as 0).
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t bits = __float_as_uint(x + 0.0f);
+    return bits ^ (bits >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t order) {
+    return __uint_as_float(order ^ (order >> 31 ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ __forceinline__ float next_above(float x) { return value_of(ordered(x) + 1); }  // NaN, which nothing reaches, above infinity
+
+// The k-th largest of the 64 lanes' numbers (1 <= k <= 64).
+__device__ __forceinline__ uint32_t kth_of_lanes(uint32_t x, uint32_t k) {
+    uint32_t found = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t to = found | 1u << bit;
+        if ((uint32_t)__popcll(__ballot(x >= to)) >= k) found = to;
+    }
+    return found;
+}
+
+// A bound that `best` of a workgroup's numbers reach, one from each thread: by every wave's ceil(best / waves)-th, or by the
+// best-th of one wave; 0 where there is none.
+template <int kOf>
+__device__ __forceinline__ uint32_t bound_of_threads(uint32_t x, uint32_t best, uint32_t (*scratch)[kOf]) {
+    const uint32_t wave = threadIdx.x / 64, each = (best + kOf - 1) / kOf;
+    if (each > 64) return 0;
+    const uint32_t spread = kth_of_lanes(x, each), alone = best <= 64 ? kth_of_lanes(x, best) : 0;
+    if (threadIdx.x % 64 == 0) scratch[0][wave] = spread, scratch[1][wave] = alone;
+    __syncthreads();
+    uint32_t least = 0xFFFFFFFFu, most = 0;
+#pragma unroll
+    for (int w = 0; w < kOf; ++w) {
+        least = std::min(least, scratch[0][w]);
+        most = std::max(most, scratch[1][w]);
+    }
+    __syncthreads();
+    return std::max(least, most);
+}
+
+template <int kOf>
+__device__ __forceinline__ double block_sum(double x, double *scratch) {
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) x += __shfl_xor(x, d);
+    if (threadIdx.x % 64 == 0) scratch[threadIdx.x / 64] = x;
+    __syncthreads();
+    double all = 0;
+#pragma unroll
+    for (int w = 0; w < kOf; ++w) all += scratch[w];
+    __syncthreads();
+    return all;
+}
+template <int kOf>
+__device__ __forceinline__ uint32_t block_largest(uint32_t x, uint32_t *scratch) {
+    x = largest_of_lanes<64>(x);
+    if (threadIdx.x % 64 == 0) scratch[threadIdx.x / 64] = x;
+    __syncthreads();
+    uint32_t all = 0;
+#pragma unroll
+    for (int w = 0; w < kOf; ++w) all = larger(all, scratch[w]);
+    __syncthreads();
+    return all;
+}
+
+struct Shared {
+    Candidate kept[kSlots];
+    uint32_t count, waves[2][kWaves];
+    double sums[kWaves];
+};
+
+__device__ __forceinline__ uint64_t key_of(float score, uint32_t row) { return (uint64_t)ordered(score) << 32 | (0xFFFFFFFFu - row); }
+
+// Leaves the `best` first of what is kept (n of it) and of the scores v of this turn that reach `least`; returns the last one's score.
+// There are at least `best` of them.
+__device__ __noinline__ float narrow(Shared &s, uint32_t n, uint32_t best, const float (&v)[kEach], float least, uint32_t row) {
+    constexpr int kOwn = kSlots / kThreads;
+    const auto row_of = [&](int i) { return row + (i / 8) * (kTile / 2) + i % 8; };
+    uint64_t own[kOwn];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        const uint32_t at = threadIdx.x + i * kThreads;
+        own[i] = at < n ? key_of(s.kept[at].score, s.kept[at].row) : 0;
+    }
+    uint64_t found = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+        const uint64_t to = found | 1ull << bit;
+        uint32_t reach = 0;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) reach += own[i] >= to;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) reach += v[i] >= least && key_of(v[i], row_of(i)) >= to;
+#pragma unroll
+        for (int d = 32; d > 0; d /= 2) reach += __shfl_xor(reach, d);
+        uint32_t *waves = s.waves[bit % 2];
+        if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = reach;
+        __syncthreads();
+        uint32_t all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all += waves[w];
+        if (all >= best) found = to;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) s.count = 0;
+    __syncthreads();
+    const auto keep = [&](uint64_t key) { s.kept[atomicAdd(&s.count, 1u)] = {value_of((uint32_t)(key >> 32)), 0xFFFFFFFFu - (uint32_t)key}; };
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+        if (own[i] >= found) keep(own[i]);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (v[i] >= least && key_of(v[i], row_of(i)) >= found) keep(key_of(v[i], row_of(i)));
+    __syncthreads();
+    return value_of((uint32_t)(found >> 32));
+}
+
+__device__ __forceinline__ bool offers(const SelectArgs &a, uint64_t beam, float &total) {
+    total = a.totals ? a.totals[beam] : 0.0f;
+    return fabsf(total) < infinity();
+}
+
+__device__ __forceinline__ void put_none(const SelectArgs &a, uint64_t group, uint32_t rank) {
+    const uint64_t at = group * a.best + rank;
+    a.parent[at] = -1;
+    a.row[at] = -1;
+    a.total[at] = -infinity();
+}
+// What a rank goes to; what counts -inf (finite scores beside infinity) goes behind all others, and is nothing.
+__device__ __forceinline__ void put(const SelectArgs &a, uint64_t group, uint32_t rank, uint64_t parent, uint32_t row, double total) {
+    if (total == -infinity()) return put_none(a, group, rank);
+    const uint64_t at = group * a.best + rank;
+    a.parent[at] = (int64_t)parent;
+    a.row[at] = row;
+    a.total[at] = (float)total;
+}
+
+// One part of one beam.  kAlone: groups of one beam in one part are finished here.
+template <class T, bool kLog, bool kAlone>
+__global__ __launch_bounds__(kThreads) void k_select_parts(SelectArgs a) {
+    __shared__ Shared s;
+    const uint64_t beam = blockIdx.x / a.parts;
+    const uint32_t part = blockIdx.x % a.parts, tid = threadIdx.x;
+    const uint64_t begin = (uint64_t)part * a.part_rows;
+    const uint32_t end = (uint32_t)std::min<uint64_t>(a.rows, begin + a.part_rows);
+    float base;
+    const bool some = offers(a, beam, base), ended = some && a.done && a.done[beam];
+    Part *to = (Part *)a.summaries + beam * a.parts + part;
+    if (!some || ended) {
+        if constexpr (kAlone) {
+            for (uint32_t r = tid; r < a.best; r += kThreads) {
+                if (ended && r == 0) put(a, beam, 0, beam, a.end, base);
+                else put_none(a, beam, r);
+            }
+        } else if (tid == 0) {
+            *to = Part{0.0, -infinity(), -infinity(), 0, 0};
+        }
+        return;
+    }
+    if (tid == 0) s.count = 0;
+    __syncthreads();
+    const T *scores = (const T *)a.scores + beam * a.stride;
+    float bound = -infinity(), least = kLowest, largest = -infinity(), top = -infinity();
+    double sum = 0.0;
+    uint32_t kept = 0, turn = 0;
+    for (uint64_t first = begin; first < end; first += kTile, ++turn) {
+        const uint32_t row = (uint32_t)first + 8 * tid;  // and half a turn on
+        float v[kEach];
+        {
+            Piece<T> p[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) p[h].load(scores, row + h * (kTile / 2), end);
+            const bool whole = first + kTile <= end;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const float x = (float)p[i / 8].at[i % 8];
+                v[i] = (whole || row + (i / 8) * (kTile / 2) + i % 8 < end) && x == x ? x : -infinity();
+            }
+        }
+        float most = v[0];
+#pragma unroll
+        for (int i = 1; i < kEach; ++i) most = fmaxf(most, v[i]);
+        if constexpr (kLog) {
+            // exponentials of differences from a score of this thread that is not far below its largest
+            if (most > top + 20.0f || top == -infinity()) {
+                if (most > top) {
+                    sum = top == -infinity() || most == infinity() ? 0.0 : sum * (double)__expf(top - most);
+                    top = most;
+                }
+            }
+            float terms[kEach];
+            if (top < infinity()) {
+                const float from = top == -infinity() ? 0.0f : top;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) terms[i] = __expf(v[i] - from);
+            } else {  // scores of infinity share everything
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) terms[i] = v[i] == infinity() ? 1.0f : 0.0f;
+            }
+#pragma unroll
+            for (int d = kEach / 2; d > 0; d /= 2)
+#pragma unroll
+                for (int i = 0; i < d; ++i) terms[i] += terms[i + d];
+            sum += (double)terms[0];
+        }
+        largest = fmaxf(largest, most);
+        if ((turn & (turn + 1)) == 0) {  // turns 0, 1, 3, 7, ...
+            const uint32_t found = bound_of_threads<kWaves>(ordered(largest), a.best, s.waves);
+            if (found > ordered(-infinity()) && value_of(found) > bound) {
+                // scores that are kept may lie below it; of those in later turns, equal ones come behind
+                bound = value_of(found);
+                least = std::max(least, bound);
+            }
+        }
+        bool full = false;
+        if (most >= least) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                if (v[i] < least) continue;
+                const uint32_t at = atomicAdd(&s.count, 1u);
+                if (at < kSlots) s.kept[at] = {v[i], row + (i / 8) * (kTile / 2) + i % 8};
+                else full = true;
+            }
+        }
+        if (__syncthreads_or(full)) {
+            bound = narrow(s, kept, a.best, v, least, row);
+            kept = a.best;
+        } else {
+            kept = s.count;
+        }
+        if (kept >= a.best && bound > -infinity()) least = std::max(least, next_above(bound));
+        __syncthreads();
+    }
+    double log_sum = 0.0;
+    float all_top = 0.0f;
+    if constexpr (kLog) {
+        const uint32_t found = block_largest<kWaves>(ordered(top), s.waves[0]);
+        all_top = value_of(found);
+        const double mine = top == -infinity() || (all_top == infinity() && top < all_top) ? 0.0
+                            : top == all_top ? sum : sum * exp((double)top - (double)all_top);
+        log_sum = block_sum<kWaves>(mine, s.sums);
+    }
+    const float none[kEach] = {};
+    const uint32_t most_kept = kAlone ? kSlots : a.slots;
+    if (kept > most_kept) {
+        bound = narrow(s, kept, a.best, none, infinity(), 0);
+        kept = a.best;
+    }
+    if constexpr (kAlone) {
+        log_sum = log(log_sum);
+        for (uint32_t i = tid; i < kept; i += kThreads) {
+            const uint64_t key = key_of(s.kept[i].score, s.kept[i].row);
+            uint32_t rank = 0;
+            for (uint32_t j = 0; j < kept; ++j) rank += key_of(s.kept[j].score, s.kept[j].row) > key;
+            if (rank >= a.best) continue;
+            const float score = s.kept[i].score;
+            const double total = !kLog ? (double)base + (double)score
+                                       : (double)base + (score == all_top ? 0.0 : (double)score - (double)all_top) - log_sum;
+            put(a, beam, rank, beam, s.kept[i].row, total);
+        }
+        for (uint32_t r = kept + tid; r < a.best; r += kThreads) put_none(a, beam, r);
+    } else {
+        if (tid == 0) *to = Part{log_sum, all_top, bound, kept, 0};
+        Candidate *out = (Candidate *)a.candidates + (beam * a.parts + part) * a.slots;
+        for (uint32_t i = tid; i < kept; i += kThreads) out[i] = s.kept[i];
+    }
+}
+
+// --- the beams of a group joined
+constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / 64;
+constexpr uint32_t kJoinSlots = 2 * kJoinThreads, kMostLists = 2048, kMostBeams = GV_MAX_BEAMS;
+static_assert(GV_MAX_BEST + kJoinThreads <= kJoinSlots, "room for the best and a turn");
+
+struct JoinShared {
+    double total[kJoinSlots];
+    float score[kJoinSlots];
+    uint32_t row[kJoinSlots], beam[kJoinSlots];
+    uint32_t ends[kMostLists];  // of the lists, counted together
+    double log_sum[kMostBeams];
+    float top[kMostBeams], base[kMostBeams];
+    uint32_t count, waves[2][kJoinWaves];
+};
+
+// Whether candidate i goes before candidate j: by total, beam, score and row.
+__device__ __forceinline__ bool before(const JoinShared &s, uint32_t i, uint32_t j) {
+    if (s.total[i] != s.total[j]) return s.total[i] > s.total[j];
+    if (s.beam[i] != s.beam[j]) return s.beam[i] < s.beam[j];
+    if (s.score[i] != s.score[j]) return s.score[i] > s.score[j];
+    return s.row[i] < s.row[j];
+}
+__device__ __forceinline__ uint32_t rank_of(const JoinShared &s, uint32_t i, uint32_t n) {
+    uint32_t rank = 0;
+    for (uint32_t j = 0; j < n; ++j) rank += before(s, j, i);
+    return rank;
+}
+
+template <bool kLog>
+__global__ __launch_bounds__(kJoinThreads) void k_select_join(SelectArgs a) {
+    __shared__ JoinShared s;
+    const uint32_t tid = threadIdx.x, lane = tid % 64, wave = tid / 64, lists = a.beams * a.parts;
+    const uint64_t group = blockIdx.x, first_beam = group * a.beams;
+    const Part *parts = (const Part *)a.summaries + first_beam * a.parts;
+    const Candidate *candidates = (const Candidate *)a.candidates + first_beam * a.parts * a.slots;
+    if (tid == 0) s.count = 0;
+    // what the scores of each beam count from
+    for (uint32_t beam = wave; beam < a.beams; beam += kJoinWaves) {
+        float base;
+        const bool some = offers(a, first_beam + beam, base);
+        if (lane == 0) s.base[beam] = some ? base : -infinity();
+        if constexpr (kLog) {
+            uint32_t top = 0;
+            for (uint32_t p = lane; p < a.parts; p += 64) top = larger(top, ordered(parts[beam * a.parts + p].top));
+            top = largest_of_lanes<64>(top);
+            const float all = value_of(top);
+            double sum = 0.0;
+            if (top > ordered(-infinity()))
+                for (uint32_t p = lane; p < a.parts; p += 64) {
+                    const Part part = parts[beam * a.parts + p];
+                    if (part.top == all) sum += part.sum;
+                    else if (all < infinity() && part.top > -infinity()) sum += part.sum * exp((double)part.top - (double)all);
+                }
+#pragma unroll
+            for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+            if (lane == 0) s.top[beam] = all, s.log_sum[beam] = log(sum);
+        }
+    }
+    // where each list ends
+    uint32_t mine[kMostLists / kJoinThreads], upto = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kMostLists / kJoinThreads; ++i) {
+        const uint32_t list = tid * (kMostLists / kJoinThreads) + i;
+        mine[i] = list < lists ? parts[list].count : 0;
+        upto += mine[i];
+    }
+    const uint32_t own = upto;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t other = __shfl_up(upto, d);
+        if (lane >= (uint32_t)d) upto += other;
+    }
+    if (lane == 63) s.waves[0][wave] = upto;
+    __syncthreads();
+    uint32_t all = 0, at = upto - own;
+#pragma unroll
+    for (uint32_t w = 0; w < kJoinWaves; ++w) {
+        at += w < wave ? s.waves[0][w] : 0;
+        all += s.waves[0][w];
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kMostLists / kJoinThreads; ++i) {
+        at += mine[i];
+        s.ends[tid * (kMostLists / kJoinThreads) + i] = at;
+    }
+    __syncthreads();
+    const auto total_of = [&](uint32_t beam, float score) {
+        const double base = (double)s.base[beam];
+        return !kLog ? base + (double)score : base + (score == s.top[beam] ? 0.0 : (double)score - (double)s.top[beam]) - s.log_sum[beam];
+    };
+    const auto take = [&](uint32_t i, uint32_t &beam, Candidate &c) {
+        uint32_t lo = 0, hi = lists - 1;  // the first list that ends behind i
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (s.ends[mid] > i) hi = mid;
+            else lo = mid + 1;
+        }
+        beam = lo / a.parts;
+        c = candidates[(uint64_t)lo * a.slots + (i - (lo ? s.ends[lo - 1] : 0))];
+        return total_of(beam, c.score);
+    };
+    // a bound of the totals, as in a part
+    double bound = -infinity();
+    if (all > 2 * a.best) {
+        double largest = -infinity();
+        for (uint32_t i = tid; i < all; i += kJoinThreads) {
+            uint32_t beam;
+            Candidate c;
+            largest = fmax(largest, take(i, beam, c));
+        }
+        const uint32_t found = bound_of_threads<kJoinWaves>(ordered((float)largest), a.best, s.waves);
+        // the float nearest to a total may lie above it: the one below does not
+        if (found > ordered(kLowest)) bound = (double)value_of(found - 1);
+    }
+    const auto keep = [&](double total, uint32_t beam, float score, uint32_t row) {
+        const uint32_t to = atomicAdd(&s.count, 1u);
+        if (to >= kJoinSlots) return true;
+        s.total[to] = total, s.beam[to] = beam, s.score[to] = score, s.row[to] = row;
+        return false;
+    };
+    bool full = false;
+    for (uint32_t beam = tid; a.done && beam < a.beams; beam += kJoinThreads)
+        if (a.done[first_beam + beam] && s.base[beam] > -infinity() && (double)s.base[beam] >= bound)
+            full |= keep((double)s.base[beam], beam, infinity(), a.end);
+    for (uint32_t i = tid; i < all; i += kJoinThreads) {
+        uint32_t beam;
+        Candidate c;
+        const double total = take(i, beam, c);
+        if (total >= bound) full |= keep(total, beam, c.score, c.row);
+    }
+    uint32_t n;
+    if (__syncthreads_or(full)) {
+        // more than there is room for: a turn at a time, and the best are left whenever the next may not fit
+        __syncthreads();
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        n = 0;
+        const uint32_t ended = a.done ? a.beams : 0;
+        for (uint32_t from = 0; from < ended + all; from += kJoinThreads) {
+            if (n + kJoinThreads > kJoinSlots) {
+                double total[2];
+                float score[2];
+                uint32_t row[2], beam[2], rank[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t i = tid + h * kJoinThreads;
+                    rank[h] = i < n ? rank_of(s, i, n) : a.best;
+                    if (i < n) total[h] = s.total[i], score[h] = s.score[i], row[h] = s.row[i], beam[h] = s.beam[i];
+                }
+                __syncthreads();
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (rank[h] < a.best)
+                        s.total[rank[h]] = total[h], s.score[rank[h]] = score[h], s.row[rank[h]] = row[h], s.beam[rank[h]] = beam[h];
+                if (tid == 0) s.count = std::min(n, a.best);
+                __syncthreads();
+                if (n >= a.best) bound = fmax(bound, s.total[a.best - 1]);
+            }
+            const uint32_t i = from + tid;
+            if (i < ended) {
+                if (a.done[first_beam + i] && s.base[i] > -infinity() && (double)s.base[i] >= bound)
+                    (void)keep((double)s.base[i], i, infinity(), a.end);
+            } else if (i < ended + all) {
+                uint32_t beam;
+                Candidate c;
+                const double total = take(i - ended, beam, c);
+                if (total >= bound) (void)keep(total, beam, c.score, c.row);
+            }
+            __syncthreads();
+            n = s.count;
+            __syncthreads();
+        }
+    } else {
+        n = s.count;
+    }
+    for (uint32_t i = tid; i < n; i += kJoinThreads) {
+        const uint32_t rank = rank_of(s, i, n);
+        if (rank < a.best) put(a, group, rank, first_beam + s.beam[i], s.row[i], s.total[i]);
+    }
+    for (uint32_t r = n + tid; r < a.best; r += kJoinThreads) put_none(a, group, r);
+}
+
+// How scores are cut: parts of whole turns, so many that a thousand workgroups are at work.
+struct Cut {
+    uint32_t parts, part_rows, slots;
+    bool alone;
+};
+Cut cut_of(uint64_t queries, uint64_t rows, uint32_t beams, uint32_t best) {
+    constexpr uint64_t kWanted = 1024;
+    const uint64_t tiles = std::max<uint64_t>(1, (rows + kTile - 1) / kTile);
+    uint64_t parts = std::min<uint64_t>(tiles, std::max<uint64_t>(1, kWanted / queries));
+    parts = std::min<uint64_t>(parts, kMostLists / beams);
+    if (beams == 1 && tiles <= 2) parts = 1;
+    const uint64_t each = (tiles + parts - 1) / parts;
+    parts = (tiles + each - 1) / each;
+    return {(uint32_t)parts, (uint32_t)(each * kTile), std::min<uint32_t>(kSlots, 512 + 4 * best), beams == 1 && parts == 1};
+}
+
+uint64_t summaries_of(uint64_t queries, const Cut &c) { return (queries * c.parts * sizeof(Part) + 15) & ~15ull; }
+
+}  // namespace
+
+uint64_t select_workspace(uint64_t queries, uint64_t rows, uint32_t beams, uint32_t best) {
+    if (queries == 0) return 0;
+    const Cut c = cut_of(queries, rows, beams, best);
+    return c.alone ? 0 : summaries_of(queries, c) + queries * c.parts * c.slots * sizeof(Candidate);
+}
+
+hipError_t launch_select(const SelectArgs &args, void *workspace, hipStream_t stream) {
+    SelectArgs a = args;
+    const Cut c = cut_of(a.queries, a.rows, a.beams, a.best);
+    a.parts = c.parts, a.part_rows = c.part_rows, a.slots = c.slots;
+    a.summaries = workspace;
+    a.candidates = (char *)workspace + summaries_of(a.queries, c);
+    const uint32_t blocks = (uint32_t)(a.queries * c.parts);
+    const auto first = [&](auto type) {
+        using T = decltype(type);
+        if (c.alone) {
+            return a.log_softmax ? launch(k_select_parts<T, true, true>, blocks, kThreads, 0, stream, a)
+                                 : launch(k_select_parts<T, false, true>, blocks, kThreads, 0, stream, a);
+        }
+        return a.log_softmax ? launch(k_select_parts<T, true, false>, blocks, kThreads, 0, stream, a)
+                             : launch(k_select_parts<T, false, false>, blocks, kThreads, 0, stream, a);
+    };
+    const hipError_t e = a.type == GV_F32 ? first(float()) : a.type == GV_BF16 ? first(__bf16()) : first(_Float16());
+    if (e != hipSuccess || c.alone) return e;
+    const uint32_t groups = (uint32_t)(a.queries / a.beams);
+    return a.log_softmax ? launch(k_select_join<true>, groups, kJoinThreads, 0, stream, a)
+                         : launch(k_select_join<false>, groups, kJoinThreads, 0, stream, a);
+}
+
+}  // namespace gv

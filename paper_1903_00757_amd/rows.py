@@ -18,7 +18,8 @@ import torch
 from .binding import GV_BF16, GV_F16, GV_F32, GV_I8, GV_I32, GV_I64, GV_OK, GvError, load
 
 __all__ = ["NormRows", "NormGrads", "gv_drop_rows", "gv_norm_rows", "gv_norm_rows_workspace", "gv_norm_rows_backward",
-           "gv_quantize_rows", "gv_score_rows", "gv_lookup_rows", "gv_lookup_rows_workspace", "gv_lookup_rows_backward"]
+           "gv_quantize_rows", "gv_score_rows", "gv_lookup_rows", "gv_lookup_rows_workspace", "gv_lookup_rows_backward",
+           "Selection", "gv_select_rows", "gv_select_rows_workspace"]
 
 _TYPES = {torch.float32: GV_F32, torch.bfloat16: GV_BF16, torch.float16: GV_F16}
 _TYPES_AND_BYTES = dict(_TYPES)
@@ -40,6 +41,13 @@ class NormGrads(NamedTuple):
     x: torch.Tensor
     residual: Optional[torch.Tensor]
     gain: Optional[torch.Tensor]   # float32[cols]
+
+
+class Selection(NamedTuple):
+    """What gv_select_rows gives, [groups][best]; -1 and -inf where there was nothing more to select."""
+    parent: torch.Tensor  # int64: the beam, counted over all queries
+    row: torch.Tensor     # int64
+    total: torch.Tensor   # float32
 
 
 def _refuse(text):
@@ -331,3 +339,43 @@ def gv_lookup_rows_backward(grad_out, index, rows, *, scale=1.0, out_type=None, 
     if passed:
         _written(out)
     return out
+
+
+@functools.lru_cache(maxsize=256)
+def gv_select_rows_workspace(queries, rows, beams, best):
+    """Bytes of scratch that a selection takes."""
+    n = C.c_uint64()
+    rc = load().gv_select_rows_workspace(queries, rows, beams, best, C.byref(n))
+    if rc != GV_OK:
+        raise GvError(rc, load().gv_last_error(None).decode())
+    return n.value
+
+
+def gv_select_rows(scores, best, *, beams=1, totals=None, done=None, end=0, log_softmax=True):
+    """The best rows over the scores of each group of `beams` queries: by totals + log softmax of the scores, or totals + scores.
+    done (bool): beams that have ended offer row `end` alone.  gv_lookup_rows(states, got.parent.view(-1)) gives the states that
+    belong to what was selected."""
+    kind = _TYPES.get(scores.dtype)
+    if kind is None or not scores.is_cuda:
+        _refuse(f"scores: {', '.join(map(str, _TYPES))} in device memory are asked for")
+    if scores.dim() != 2:
+        _refuse("scores: a 2-D tensor")
+    queries, rows = scores.shape
+    stride, step = scores.stride()
+    if step != 1 and rows > 1:
+        _refuse("scores: the scores of a query lie together")
+    gpu = scores.get_device()
+    totals_at = None if totals is None else _array("totals", totals, queries, _f32, gpu)
+    done_at = None if done is None else _array("done", done, queries, torch.bool, gpu)
+    if _recording() and (scores.requires_grad or (totals is not None and totals.requires_grad)):
+        _without_graph(scores, totals)
+    size = gv_select_rows_workspace(queries, rows, beams, best)
+    groups = queries // beams
+    at = torch.empty((2, groups, best), dtype=torch.int64, device=scores.device)
+    parent, row = at[0], at[1]
+    total = torch.empty((groups, best), dtype=_f32, device=scores.device)
+    space = torch.empty(size, dtype=_uint8, device=scores.device) if size else None
+    first = at.data_ptr()
+    _call(load().gv_select_rows, gpu, queries, rows, kind, scores.data_ptr(), stride if queries > 1 else rows, beams, totals_at, done_at, end,
+          bool(log_softmax), best, first, first + 8 * groups * best, total.data_ptr(), space.data_ptr() if size else None, size)
+    return Selection(parent, row, total)
