@@ -455,6 +455,31 @@ int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t inde
                             int type, const void *dev_grad, uint64_t grad_stride, float scale, int add, int out_type, void *dev_out,
                             uint64_t out_stride, void *dev_workspace, uint64_t workspace_bytes, void *stream);
 
+/* A layer: z = x weight^T + bias, out = residual + act(z); x has cols columns, weight outs rows of cols, bias outs values, and residual,
+ * pre and out have outs columns, all of `type` (GV_F32, GV_BF16, GV_F16).  bias, residual and pre may be NULL; pre receives z, which
+ * the backward pass takes.  GV_ACT_GELU is z (1 + erf(z / sqrt 2)) / 2, GV_ACT_SILU z / (1 + exp(-z)).  Sums are fp32 in an order that the
+ * sizes and the type decide, act is taken of the sum, and a result is rounded once.  out may be residual itself, but neither out nor
+ * pre may overlap x or weight.  1 <= outs <= GV_MAX_ROW_COLS.  dev_workspace points to workspace_bytes bytes (at least those of
+ * gv_dense_rows_workspace, which may be none; aligned to 16) that the call may overwrite.                               */
+enum { GV_ACT_NONE = 0, GV_ACT_RELU = 1, GV_ACT_GELU = 2, GV_ACT_SILU = 3 };
+int gv_dense_rows_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, uint64_t *bytes);
+int gv_dense_rows(uint64_t rows, uint32_t cols, uint32_t outs, int type, const void *dev_x, uint64_t x_stride, const void *dev_weight,
+                  uint64_t weight_stride, const void *dev_bias, int act, const void *dev_residual, uint64_t residual_stride,
+                  void *dev_pre, uint64_t pre_stride, void *dev_out, uint64_t out_stride, void *dev_workspace, uint64_t workspace_bytes,
+                  void *stream);
+/* Its gradients from grad_out (of out): with gz = grad_out * act'(pre) (relu: 0 where pre is 0),
+ *   grad_x = gz weight,  grad_weight = gz^T x,  grad_bias = sum over the rows of gz,
+ * each of `type` and each may be NULL (the residual's gradient is grad_out).  pre is what the forward pass left; without an activation
+ * it is not read.  The products take gz rounded to `type`, as they take their other operand; grad_bias adds up what is not rounded.
+ * grad_x and grad_weight may not overlap each other or what the call reads.  rows = 0 leaves grad_weight and grad_bias 0.  The workspace is that
+ * of gv_dense_rows_backward_workspace, which is told which gradients are asked for.                                  */
+int gv_dense_rows_backward_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, int act, int grad_x, int grad_weight,
+                                     int grad_bias, uint64_t *bytes);
+int gv_dense_rows_backward(uint64_t rows, uint32_t cols, uint32_t outs, int type, const void *dev_grad_out, uint64_t grad_out_stride,
+                           const void *dev_x, uint64_t x_stride, const void *dev_weight, uint64_t weight_stride, int act,
+                           const void *dev_pre, uint64_t pre_stride, void *dev_grad_x, uint64_t grad_x_stride, void *dev_grad_weight,
+                           uint64_t grad_weight_stride, void *dev_grad_bias, void *dev_workspace, uint64_t workspace_bytes, void *stream);
+
 /* The best rows over the scores of beams, as gv_score_rows gives them.  queries = groups x beams; the beams b of a group share a
  * selection of `best` out of all (b, i), row i of beam b counting
  *   totals[b] + scores[b][i] - log sum over i' of exp(scores[b][i'])    (log_softmax)

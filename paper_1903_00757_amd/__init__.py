@@ -8,6 +8,7 @@ from .binding import EXPORTS, LIB_PATH, GvError, load  # noqa: F401
 # of rows.py, which is imported with the first of them: it needs torch, which constants, the exports and the build do without
 _ROWS = ("NormRows", "NormGrads", "gv_drop_rows", "gv_norm_rows", "gv_norm_rows_workspace", "gv_norm_rows_backward",
          "gv_quantize_rows", "gv_score_rows", "gv_lookup_rows", "gv_lookup_rows_workspace", "gv_lookup_rows_backward",
+         "DenseRows", "DenseGrads", "gv_dense_rows", "gv_dense_rows_workspace", "gv_dense_rows_backward", "gv_dense_rows_backward_workspace",
          "Selection", "gv_select_rows", "gv_select_rows_workspace")
 __all__ = [name for name in globals() if not name.startswith("_") and name != "importlib"] + ["rows", *_ROWS]
 

@@ -23,6 +23,7 @@ GV_SHUFFLE_NONE, GV_SHUFFLE_PSEUDO = 0, 1
 GV_F32, GV_BF16, GV_F16, GV_I8, GV_I32, GV_I64 = 0, 1, 2, 3, 4, 5
 GV_MAX_ROW_COLS = 16384
 GV_MAX_BEAMS, GV_MAX_BEST = 512, 1024
+GV_ACT_NONE, GV_ACT_RELU, GV_ACT_GELU, GV_ACT_SILU = 0, 1, 2, 3
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgvhot.so")
 
@@ -36,6 +37,7 @@ EXPORTS = [
     "gv_build_walk_tables", "gv_augment_weighted", "gv_set_weighted_graph",
     "gv_drop_rows", "gv_norm_rows", "gv_norm_rows_workspace", "gv_norm_rows_backward", "gv_quantize_rows", "gv_score_rows",
     "gv_lookup_rows", "gv_lookup_rows_workspace", "gv_lookup_rows_backward",
+    "gv_dense_rows", "gv_dense_rows_workspace", "gv_dense_rows_backward", "gv_dense_rows_backward_workspace",
     "gv_select_rows", "gv_select_rows_workspace",
 ]
 
@@ -138,6 +140,10 @@ def load():
     L.gv_lookup_rows.argtypes = [u64, vp, u64, i32, u64, u32, i32, vp, u64, flt, i32, vp, u64, vp]
     L.gv_lookup_rows_workspace.argtypes = [u64, u64, u32, i32, u64p]
     L.gv_lookup_rows_backward.argtypes = [u64, vp, u64, i32, u64, u32, i32, vp, u64, flt, i32, i32, vp, u64, vp, u64, vp]
+    L.gv_dense_rows_workspace.argtypes = [u64, u32, u32, i32, u64p]
+    L.gv_dense_rows.argtypes = [u64, u32, u32, i32, vp, u64, vp, u64, vp, i32, vp, u64, vp, u64, vp, u64, vp, u64, vp]
+    L.gv_dense_rows_backward_workspace.argtypes = [u64, u32, u32, i32, i32, i32, i32, i32, u64p]
+    L.gv_dense_rows_backward.argtypes = [u64, u32, u32, i32, vp, u64, vp, u64, vp, u64, i32, vp, u64, vp, u64, vp, u64, vp, vp, u64, vp]
     L.gv_select_rows_workspace.argtypes = [u64, u64, u32, u32, u64p]
     L.gv_select_rows.argtypes = [u64, u64, i32, vp, u64, u32, vp, vp, u64, i32, u32, vp, vp, vp, vp, u64, vp]
     for name in EXPORTS:

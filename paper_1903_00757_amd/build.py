@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libgvhot.so")
 SOURCES = [("gv_kernels.hip", [], "gv_kernels.o"), ("gv_kernels.hip", ["-DGV_TRACK_LOSS=1"], "gv_kernels_tracked.o"),
            ("gv_api.cpp", [], "gv_api.o"), ("gv_plan.cpp", [], "gv_plan.o"), ("gv_augment.cpp", [], "gv_augment.o"),
            ("gv_rows.hip", [], "gv_rows.o"), ("gv_scores.hip", [], "gv_scores.o"), ("gv_lookup.hip", [], "gv_lookup.o"),
-           ("gv_select.hip", [], "gv_select.o"), ("gv_rows_api.cpp", [], "gv_rows_api.o")]
+           ("gv_dense.hip", [], "gv_dense.o"), ("gv_select.hip", [], "gv_select.o"), ("gv_rows_api.cpp", [], "gv_rows_api.o")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-munsafe-fp-atomics", "-Wall", "-Wextra", "-Wno-unused-parameter",
           # packed-fp32 instructions are kept out of the generated code on purpose

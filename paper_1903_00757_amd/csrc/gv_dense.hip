@@ -1,0 +1,465 @@
+// gfx950 kernels of a layer: out = residual + act(x weight^T + bias), and its gradients.
+//
+// All products are sums over k of A(m, k) B(n, k) on matrix instructions, with sums in fp32.  An operand lies with the values of one
+// row together (k runs along memory: x and weight in the forward pass), or with those of one k together (the gradients'
+// operands); the latter are transposed in registers on the way into LDS, so that there the tiles are all alike: rows of 128 bytes
+// of k, in eight pieces of 16 bytes, piece p of row r at place p ^ (r ^ r / 8) % 8.  Eight rows in a row then have a piece in eight
+// different places (what a matrix instruction's lanes read), and so have rows 4 i + j for eight i in a row (what is written transposed).
+#include "gv_row_pieces.hpp"
+#include "gv_rows.hpp"
+#include "gvhot.h"
+
+#include <algorithm>
+#include <type_traits>
+
+#pragma clang fp contract(off)
+
+namespace gv {
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+
+// act(z), and its slope
+__device__ __forceinline__ float act_of(int act, float z) {
+    if (act == GV_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if (act == GV_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    if (act == GV_ACT_SILU) return z / (1.0f + __expf(-z));
+    return z;
+}
+__device__ __forceinline__ float slope_of(int act, float z) {
+    if (act == GV_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (act == GV_ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * (0.39894228040143268f * __expf(-0.5f * z * z));
+    if (act == GV_ACT_SILU) {
+        const float s = 1.0f / (1.0f + __expf(-z));
+        return s * (1.0f + z * (1.0f - s));
+    }
+    return 1.0f;
+}
+
+// sums += 16 x 16 products over the k's of a piece of each lane: lane l has row l % 16 and the pieces of group l / 16.
+__device__ __forceinline__ void multiply(uint4 a, uint4 b, f4 &sums, float *) {
+    const float *x = (const float *)&a, *y = (const float *)&b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], sums, 0, 0, 0);
+}
+__device__ __forceinline__ void multiply(uint4 a, uint4 b, f4 &sums, __bf16 *) {
+    sums = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), sums, 0, 0, 0);
+}
+__device__ __forceinline__ void multiply(uint4 a, uint4 b, f4 &sums, _Float16 *) {
+    sums = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), sums, 0, 0, 0);
+}
+
+// N values from p, of which those before `left` are there; the others are 0.
+template <class T, int N>
+struct Values {
+    T at[N];
+    __device__ __forceinline__ void load(const T *p, uint32_t left) {
+        if (left >= (uint32_t)N) {
+            __builtin_memcpy(this, p, sizeof *this);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) at[i] = (uint32_t)i < left ? p[i] : (T)0.0f;
+        }
+    }
+    __device__ __forceinline__ void store(T *p, uint32_t left) const {
+        if (left >= (uint32_t)N) {
+            __builtin_memcpy(p, this, sizeof *this);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if ((uint32_t)i < left) p[i] = at[i];
+        }
+    }
+};
+__device__ __forceinline__ uint32_t left_of(uint32_t at, uint32_t all) { return at < all ? all - at : 0; }
+
+// What becomes of the four sums of row m from column n on.
+template <class T>
+__device__ __forceinline__ void finish(const DenseArgs &a, uint32_t m, uint32_t n, f4 sums) {
+    if (m >= a.rows || n >= a.outs) return;
+    const uint32_t left = a.outs - n;
+    float z[4] = {sums[0], sums[1], sums[2], sums[3]};
+    if (a.bias) {
+        Values<T, 4> b;
+        b.load((const T *)a.bias + n, left);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] += (float)b.at[i];
+    }
+    Values<T, 4> to;
+    if (a.pre) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to.at[i] = (T)z[i];
+        to.store((T *)a.pre + m * a.pre_stride + n, left);
+    }
+    if (a.act != GV_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = act_of(a.act, z[i]);
+    }
+    if (a.residual) {
+        Values<T, 4> r;
+        r.load((const T *)a.residual + m * a.residual_stride + n, left);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] += (float)r.at[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to.at[i] = (T)z[i];
+    to.store((T *)a.out + m * a.out_stride + n, left);
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of kTile x kTile, 2 kTile threads: eight, four or two waves side by side.  The next step's values are loaded into registers while this
+// step's are multiplied, and go to the other half of LDS.
+constexpr int kStep = 128;  // bytes of k
+
+template <class T>
+constexpr int kEach = 16 / (int)sizeof(T);  // values of a piece
+
+__device__ __forceinline__ uint32_t place_of(uint32_t row, uint32_t piece) { return row * kStep + (piece ^ ((row ^ row >> 3) & 7)) * 16; }
+
+// A thread's share of an operand's step: four pieces.
+template <class T, int kTile, bool kAlong>
+struct Share {
+    uint4 pieces[4];
+    // rows first .. first + kTile - 1 of `rows`, from k on of `count`
+    __device__ __forceinline__ void load(const T *p, uint64_t stride, uint32_t first, uint32_t rows, uint32_t k, uint32_t count) {
+        constexpr int N = kEach<T>;
+        if constexpr (kAlong) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t id = q * 2 * kTile + threadIdx.x, row = first + id / 8, at = k + id % 8 * N;
+                Values<T, N> v;
+                v.load(p + row * stride + at, row < rows ? left_of(at, count) : 0);
+                pieces[q] = __builtin_bit_cast(uint4, v);
+            }
+        } else {
+            const uint32_t row = first + 4 * (threadIdx.x % (kTile / 4)), at = k + threadIdx.x / (kTile / 4) * N;
+            const uint32_t left = left_of(row, rows);
+            Values<T, 4> v[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i].load(p + (at + i) * stride + row, at + i < count ? left : 0);
+            Values<T, N> turned;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) turned.at[i] = v[i].at[j];
+                pieces[j] = __builtin_bit_cast(uint4, turned);
+            }
+        }
+    }
+    __device__ __forceinline__ void put(char *tile) const {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint32_t row, piece;
+            if constexpr (kAlong) {
+                const uint32_t id = q * 2 * kTile + threadIdx.x;
+                row = id / 8, piece = id % 8;
+            } else {
+                row = 4 * (threadIdx.x % (kTile / 4)) + q, piece = threadIdx.x / (kTile / 4);
+            }
+            *(uint4 *)(tile + place_of(row, piece)) = pieces[q];
+        }
+    }
+};
+
+template <class T, int kTile, bool kAAlong, bool kBAlong>
+__global__ __launch_bounds__(2 * kTile) void k_product(DenseArgs a, uint32_t tiles_m, uint32_t tiles_n) {
+    // waves: kTile / 64 x 2 of 64 x kTile / 2 (m x n)
+    constexpr int kMs = 4, kNs = kTile / 32;
+    __shared__ __attribute__((aligned(16))) char tiles[2][2][kTile * kStep];
+    const uint32_t all = tiles_m * tiles_n, split = blockIdx.x / all;
+    uint32_t id = blockIdx.x % all;
+    // neighbours share rows in an L2: workgroup b runs on die b % 8, so a die takes tiles in a row, eight rows of tiles high
+    if (id < all / 8 * 8) id = id % 8 * (all / 8) + id / 8;
+    const uint32_t band = id / (8 * tiles_n), high = std::min(8u, tiles_m - 8 * band), in_band = id - 8 * band * tiles_n;
+    const uint32_t m0 = (8 * band + in_band % high) * kTile, n0 = in_band / high * kTile;
+    const uint32_t k_first = split * a.split_k, k_last = std::min<uint64_t>(a.cols, (uint64_t)k_first + a.split_k);
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, wm = wave / 2 * 64, wn = wave % 2 * (kTile / 2);
+    constexpr uint32_t kCount = kStep / sizeof(T);
+    f4 sums[kMs][kNs];
+#pragma unroll
+    for (int i = 0; i < kMs; ++i)
+#pragma unroll
+        for (int j = 0; j < kNs; ++j) sums[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    Share<T, kTile, kAAlong> share_a;
+    Share<T, kTile, kBAlong> share_b;
+    const T *pa = (const T *)a.x, *pb = (const T *)a.weight;
+    if (k_first < k_last) {
+        share_a.load(pa, a.x_stride, m0, a.rows, k_first, k_last);
+        share_b.load(pb, a.weight_stride, n0, a.outs, k_first, k_last);
+        share_a.put(tiles[0][0]);
+        share_b.put(tiles[0][1]);
+    }
+    __syncthreads();
+    uint32_t half = 0;
+    for (uint32_t k = k_first; k < k_last; k += kCount, half ^= 1) {
+        const bool more = k + kCount < k_last;
+        if (more) {
+            share_a.load(pa, a.x_stride, m0, a.rows, k + kCount, k_last);
+            share_b.load(pb, a.weight_stride, n0, a.outs, k + kCount, k_last);
+        }
+        const char *ta = tiles[half][0], *tb = tiles[half][1];
+#pragma unroll
+        for (uint32_t p = 0; p < 8; p += 4) {
+            uint4 ma[kMs], nb[kNs];
+#pragma unroll
+            for (int i = 0; i < kMs; ++i) ma[i] = *(const uint4 *)(ta + place_of(wm + 16 * i + lane % 16, p + lane / 16));
+#pragma unroll
+            for (int j = 0; j < kNs; ++j) nb[j] = *(const uint4 *)(tb + place_of(wn + 16 * j + lane % 16, p + lane / 16));
+#pragma unroll
+            for (int i = 0; i < kMs; ++i)
+#pragma unroll
+                for (int j = 0; j < kNs; ++j) multiply(nb[j], ma[i], sums[i][j], (T *)nullptr);
+        }
+        if (more) {
+            share_a.put(tiles[half ^ 1][0]);
+            share_b.put(tiles[half ^ 1][1]);
+        }
+        __syncthreads();
+    }
+    // a lane has four columns in a row of one row
+#pragma unroll
+    for (int i = 0; i < kMs; ++i)
+#pragma unroll
+        for (int j = 0; j < kNs; ++j) {
+            const uint32_t m = m0 + wm + 16 * i + lane % 16, n = n0 + wn + 16 * j + 4 * (lane / 16);
+            if (a.partial) {
+                if (m < a.rows && n < a.outs) {
+                    Values<float, 4> v = __builtin_bit_cast(decltype(v), sums[i][j]);
+                    v.store(a.partial + ((uint64_t)split * a.rows + m) * a.outs + n, a.outs - n);
+                }
+            } else {
+                finish<T>(a, m, n, sums[i][j]);
+            }
+        }
+}
+
+// The sums of the parts that a product's k was cut into, in their order.
+template <class T>
+__global__ __launch_bounds__(256) void k_join_product(DenseArgs a, uint32_t splits) {
+    const uint32_t each = (a.outs + 3) / 4;
+    const uint64_t all = (uint64_t)a.rows * each, step = (uint64_t)gridDim.x * 256;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += step) {
+        const uint32_t m = (uint32_t)(i / each), n = (uint32_t)(i % each) * 4;
+        f4 sums = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (uint32_t s = 0; s < splits; ++s) {
+            Values<float, 4> v;
+            v.load(a.partial + ((uint64_t)s * a.rows + m) * a.outs + n, a.outs - n);
+            sums += __builtin_bit_cast(f4, v);
+        }
+        finish<T>(a, m, n, sums);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Few rows of x: every value of the weight is read once, from memory straight into the matrix instruction's registers.  A workgroup takes
+// 16 columns of the result, its waves take steps of k in turn and are joined through LDS.
+constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
+
+template <class T, int kMs>
+__global__ __launch_bounds__(kFewThreads) void k_product_few(DenseArgs a) {
+    constexpr int N = kEach<T>, kAhead = 4;
+    __shared__ f4 joined[kFewWaves][kMs][64];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = blockIdx.x * 16 + lane % 16;
+    const T *weight = (const T *)a.weight + std::min(n, a.outs - 1) * a.weight_stride;  // rows past the end are not used
+    f4 sums[kMs];
+#pragma unroll
+    for (int i = 0; i < kMs; ++i) sums[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t k = wave * 4 * N; k < a.cols; k += kAhead * kFewWaves * 4 * N) {
+        Values<T, N> w[kAhead], x[kAhead][kMs];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t at = k + u * kFewWaves * 4 * N + lane / 16 * N, left = left_of(at, a.cols);
+            w[u].load(weight + at, left);
+#pragma unroll
+            for (int i = 0; i < kMs; ++i) {
+                const uint32_t m = 16 * i + lane % 16;
+                x[u][i].load((const T *)a.x + m * a.x_stride + at, m < a.rows ? left : 0);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int i = 0; i < kMs; ++i) multiply(__builtin_bit_cast(uint4, w[u]), __builtin_bit_cast(uint4, x[u][i]), sums[i], (T *)nullptr);
+    }
+#pragma unroll
+    for (int i = 0; i < kMs; ++i) joined[wave][i][lane] = sums[i];
+    __syncthreads();
+    if (wave >= (uint32_t)kMs) return;
+    f4 all = joined[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) all += joined[w][wave][lane];
+    finish<T>(a, 16 * wave + lane % 16, blockIdx.x * 16 + 4 * (lane / 16), all);
+}
+
+// ---------------------------------------------------------------------------
+// gz = grad * slope(pre), and the sums over its rows: a lane has eight columns, a wave 512, the waves of a workgroup take rows in turn.
+constexpr int kSlopeThreads = 256, kSlopeWaves = kSlopeThreads / 64;
+
+template <class T>
+__global__ __launch_bounds__(kSlopeThreads) void k_slope(DenseGradArgs a) {
+    __shared__ float joined[kSlopeWaves][512];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, parts = (a.outs + 511) / 512;
+    const uint32_t part = blockIdx.x % parts, chunk = blockIdx.x / parts, k = 512 * part + 8 * lane;
+    const uint64_t first = (uint64_t)chunk * a.chunk, last = std::min<uint64_t>(a.rows, first + a.chunk);
+    float sums[8] = {};
+    if (k < a.outs) {
+        for (uint64_t row = first + wave; row < last; row += kSlopeWaves) {
+            float g[8];
+            load_piece((const T *)a.grad + row * a.grad_stride, k, a.outs, g);
+            if (a.act != GV_ACT_NONE) {
+                float z[8];
+                load_piece((const T *)a.pre + row * a.pre_stride, k, a.outs, z);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] *= slope_of(a.act, z[i]);
+                if (a.gz) store_piece((T *)a.gz + row * a.outs, k, a.outs, g);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sums[i] += g[i];
+        }
+    }
+    if (!a.bias_partial) return;
+    __builtin_memcpy(&joined[wave][8 * lane], sums, sizeof sums);
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < 512 && 512 * part + c < a.outs; c += kSlopeThreads) {
+        float all = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kSlopeWaves; ++w) all += joined[w][c];
+        a.bias_partial[(uint64_t)chunk * a.outs + 512 * part + c] = all;
+    }
+}
+
+// 32 columns a workgroup, 32 threads to a column.
+template <class T>
+__global__ __launch_bounds__(1024) void k_join_bias(DenseGradArgs a, uint32_t chunks) {
+    __shared__ float scratch[32][33];
+    const uint32_t c = blockIdx.x * 32 + threadIdx.x % 32, first = threadIdx.x / 32;
+    float sum = 0.0f;
+    for (uint32_t p = first; p < chunks && c < a.outs; p += 32) sum += a.bias_partial[(uint64_t)p * a.outs + c];
+    scratch[first][threadIdx.x % 32] = sum;
+    __syncthreads();
+    sum = sum_lanes<32>(scratch[threadIdx.x % 32][first]);
+    if (threadIdx.x % 32 == 0 && blockIdx.x * 32 + first < a.outs) ((T *)a.grad_bias)[blockIdx.x * 32 + first] = (T)sum;
+}
+
+// ---------------------------------------------------------------------------
+
+template <class Run>
+hipError_t by_type(int type, Run &&run) {
+    if (type == GV_F32) return run((float *)nullptr);
+    if (type == GV_BF16) return run((__bf16 *)nullptr);
+    return run((_Float16 *)nullptr);
+}
+
+// How a product of rows x outs over `cols` k's is cut.
+struct Cut {
+    uint32_t tile, tiles_m, tiles_n, splits, split_k;
+};
+constexpr uint32_t kFewRows = 64;
+
+Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type) {
+    constexpr uint64_t kWanted = 256;
+    const uint64_t step = kStep / (type == GV_F32 ? 4 : 2), steps = (cols + step - 1) / step;
+    const auto tiles = [&](uint64_t t) { return ((rows + t - 1) / t) * ((outs + t - 1) / t); };
+    const uint64_t tile = tiles(256) >= kWanted ? 256 : tiles(128) * std::min<uint64_t>(steps / 8 + 1, 8) >= kWanted ? 128 : 64;
+    const uint64_t all = std::max<uint64_t>(1, tiles(tile));
+    uint64_t splits = std::max<uint64_t>(1, std::min<uint64_t>((2 * kWanted) / all, steps / 8));
+    const uint64_t each = std::max<uint64_t>(1, (steps + splits - 1) / splits);
+    splits = std::max<uint64_t>(1, (steps + each - 1) / each);
+    return {(uint32_t)tile, (uint32_t)((rows + tile - 1) / tile), (uint32_t)((outs + tile - 1) / tile), (uint32_t)splits, (uint32_t)(each * step)};
+}
+uint64_t partial_of(const Cut &c, uint64_t rows, uint64_t outs) { return c.splits > 1 ? 4ull * c.splits * rows * outs : 0; }
+
+template <class T, bool kAAlong, bool kBAlong>
+hipError_t product(DenseArgs a, void *workspace, hipStream_t stream) {
+    if (a.rows == 0 || a.outs == 0) return hipSuccess;
+    const Cut c = cut_of(a.rows, a.cols, a.outs, a.type);
+    a.split_k = c.split_k;
+    a.partial = c.splits > 1 ? (float *)workspace : nullptr;
+    const uint32_t blocks = c.tiles_m * c.tiles_n * c.splits;
+    const hipError_t e = c.tile == 256   ? launch(k_product<T, 256, kAAlong, kBAlong>, blocks, 512, 0, stream, a, c.tiles_m, c.tiles_n)
+                         : c.tile == 128 ? launch(k_product<T, 128, kAAlong, kBAlong>, blocks, 256, 0, stream, a, c.tiles_m, c.tiles_n)
+                                         : launch(k_product<T, 64, kAAlong, kBAlong>, blocks, 128, 0, stream, a, c.tiles_m, c.tiles_n);
+    if (e != hipSuccess || c.splits == 1) return e;
+    const uint64_t pieces = (uint64_t)a.rows * ((a.outs + 3) / 4);
+    return launch(k_join_product<T>, (uint32_t)std::min<uint64_t>((pieces + 255) / 256, 1 << 16), 256, 0, stream, a, c.splits);
+}
+
+// The parts of the gradients' workspace, in bytes.
+struct GradPlan {
+    uint64_t gz, bias, product, bytes;
+    uint32_t chunk, chunks;
+};
+GradPlan grad_plan_of(uint64_t rows, uint32_t cols, uint32_t outs, int type, int act, bool want_x, bool want_weight, bool want_bias) {
+    GradPlan p{};
+    const uint64_t parts = (outs + 511) / 512, most = std::max<uint64_t>(1, 2048 / parts);
+    p.chunk = (uint32_t)std::max<uint64_t>(4 * kSlopeWaves, (rows + most - 1) / most);
+    p.chunks = (uint32_t)((rows + p.chunk - 1) / p.chunk);
+    uint64_t at = 0;
+    const auto take = [&](uint64_t bytes) {
+        const uint64_t here = at;
+        at += (bytes + 15) & ~15ull;
+        return here;
+    };
+    p.gz = take(act != GV_ACT_NONE && (want_x || want_weight) ? rows * outs * (type == GV_F32 ? 4 : 2) : 0);
+    p.bias = take(want_bias ? 4ull * p.chunks * outs : 0);
+    p.product = take(std::max(want_x ? partial_of(cut_of(rows, outs, cols, type), rows, cols) : 0,
+                              want_weight ? partial_of(cut_of(outs, rows, cols, type), outs, cols) : 0));
+    p.bytes = at;
+    return p;
+}
+
+}  // namespace
+
+uint64_t dense_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type) {
+    return rows <= kFewRows ? 0 : partial_of(cut_of(rows, cols, outs, type), rows, outs);
+}
+
+hipError_t launch_dense(const DenseArgs &a, void *workspace, hipStream_t stream) {
+    return by_type(a.type, [&](auto *t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        if (a.rows > kFewRows) return product<T, true, true>(a, workspace, stream);
+        const uint32_t blocks = (a.outs + 15) / 16;
+        if (a.rows <= 16) return launch(k_product_few<T, 1>, blocks, kFewThreads, 0, stream, a);
+        if (a.rows <= 32) return launch(k_product_few<T, 2>, blocks, kFewThreads, 0, stream, a);
+        return launch(k_product_few<T, 4>, blocks, kFewThreads, 0, stream, a);
+    });
+}
+
+uint64_t dense_grad_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, int act, bool want_x, bool want_weight, bool want_bias) {
+    return grad_plan_of(rows, cols, outs, type, act, want_x, want_weight, want_bias).bytes;
+}
+
+hipError_t launch_dense_grad(const DenseGradArgs &args, void *workspace, hipStream_t stream) {
+    return by_type(args.type, [&](auto *t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        DenseGradArgs a = args;
+        const bool products = a.grad_x || a.grad_weight;
+        const GradPlan p = grad_plan_of(a.rows, a.cols, a.outs, a.type, a.act, a.grad_x, a.grad_weight, a.grad_bias);
+        a.chunk = p.chunk;
+        a.gz = a.act != GV_ACT_NONE && products ? (char *)workspace + p.gz : nullptr;
+        a.bias_partial = a.grad_bias ? (float *)((char *)workspace + p.bias) : nullptr;
+        void *space = (char *)workspace + p.product;
+        hipError_t e = hipSuccess;
+        if ((a.gz || a.grad_bias) && a.rows > 0) e = launch(k_slope<T>, p.chunks * ((a.outs + 511) / 512), kSlopeThreads, 0, stream, a);
+        if (e == hipSuccess && a.grad_bias) e = launch(k_join_bias<T>, (a.outs + 31) / 32, 1024, 0, stream, a, p.chunks);
+        const void *gz = a.gz ? a.gz : a.grad;
+        const uint64_t gz_stride = a.gz ? a.outs : a.grad_stride;
+        if (e == hipSuccess && a.grad_x) {
+            DenseArgs d{};
+            d.x = gz, d.weight = a.weight, d.out = a.grad_x, d.x_stride = gz_stride, d.weight_stride = a.weight_stride;
+            d.out_stride = a.grad_x_stride, d.rows = (uint32_t)a.rows, d.cols = a.outs, d.outs = a.cols, d.type = a.type;
+            e = product<T, true, false>(d, space, stream);
+        }
+        if (e == hipSuccess && a.grad_weight) {
+            DenseArgs d{};
+            d.x = gz, d.weight = a.x, d.out = a.grad_weight, d.x_stride = gz_stride, d.weight_stride = a.x_stride;
+            d.out_stride = a.grad_weight_stride, d.rows = a.outs, d.cols = (uint32_t)a.rows, d.outs = a.cols, d.type = a.type;
+            e = product<T, false, false>(d, space, stream);
+        }
+        return e;
+    });
+}
+
+}  // namespace gv

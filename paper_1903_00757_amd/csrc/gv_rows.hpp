@@ -1,5 +1,6 @@
 // Internal interface between the checks of the operators on rows (gv_rows_api.cpp) and their kernels
-// (gv_rows.hip, gv_scores.hip, gv_lookup.hip, gv_select.hip).  Not part of the C boundary.
+// (gv_rows.hip, gv_scores.hip, gv_lookup.hip, gv_dense.hip,
+// gv_select.hip).  Not part of the C boundary.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -110,6 +111,28 @@ struct LookupGradArgs {
     uint32_t lanes, chunk, chunks;
 };
 
+// rows x outs sums over cols products of x and weight, and what becomes of them
+struct DenseArgs {
+    const void *x, *weight, *bias, *residual;  // bias and residual may be null
+    void *pre, *out;                           // pre may be null
+    uint64_t x_stride, weight_stride, residual_stride, pre_stride, out_stride;
+    uint32_t rows, cols, outs;
+    int type, act;
+    float *partial;    // where cols are cut
+    uint32_t split_k;  // and how many are taken together
+};
+
+struct DenseGradArgs {
+    const void *grad, *x, *weight, *pre;         // pre may be null, without an activation
+    void *grad_x, *grad_weight, *grad_bias;      // may be null
+    uint64_t rows, grad_stride, x_stride, weight_stride, pre_stride, grad_x_stride, grad_weight_stride;
+    uint32_t cols, outs;
+    int type, act;
+    void *gz;             // of the workspace
+    float *bias_partial;  // likewise
+    uint32_t chunk;       // rows of each of its parts
+};
+
 struct SelectArgs {
     const void *scores;
     const float *totals;   // may be null
@@ -147,6 +170,10 @@ hipError_t launch_quantize(const QuantizeArgs &a, hipStream_t stream);
 hipError_t launch_score(const ScoreArgs &a, hipStream_t stream);
 hipError_t launch_lookup(const LookupArgs &a, hipStream_t stream);
 uint64_t lookup_grad_workspace(uint64_t count, uint64_t rows, uint32_t cols, bool add);
+uint64_t dense_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type);
+hipError_t launch_dense(const DenseArgs &a, void *workspace, hipStream_t stream);
+uint64_t dense_grad_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, int act, bool want_x, bool want_weight, bool want_bias);
+hipError_t launch_dense_grad(const DenseGradArgs &a, void *workspace, hipStream_t stream);
 uint64_t select_workspace(uint64_t queries, uint64_t rows, uint32_t beams, uint32_t best);
 hipError_t launch_select(const SelectArgs &a, void *workspace, hipStream_t stream);
 hipError_t launch_lookup_grad(const LookupGradArgs &a, void *workspace, hipStream_t stream);

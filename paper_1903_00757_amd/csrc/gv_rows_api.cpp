@@ -69,10 +69,10 @@ int check_index(const char *call, const gv::Index &index, uint64_t count, uint64
 }
 
 // Whether two matrices share memory.
-bool overlap(const Matrix &a, uint64_t a_rows, const Matrix &b, uint64_t b_rows, uint32_t cols) {
+bool overlap(const Matrix &a, uint64_t a_rows, uint32_t a_cols, const Matrix &b, uint64_t b_rows, uint32_t b_cols) {
     if (a_rows == 0 || b_rows == 0) return false;
-    const uintptr_t a_end = (uintptr_t)a.at + ((a_rows - 1) * a.stride + cols) * size_of(a.type);
-    const uintptr_t b_end = (uintptr_t)b.at + ((b_rows - 1) * b.stride + cols) * size_of(b.type);
+    const uintptr_t a_end = (uintptr_t)a.at + ((a_rows - 1) * a.stride + a_cols) * size_of(a.type);
+    const uintptr_t b_end = (uintptr_t)b.at + ((b_rows - 1) * b.stride + b_cols) * size_of(b.type);
     return (uintptr_t)a.at < b_end && (uintptr_t)b.at < a_end;
 }
 
@@ -219,7 +219,7 @@ int gv_lookup_rows(uint64_t count, const void *dev_index, uint64_t index_stride,
     const Matrix table{"table", dev_table, table_stride, type}, out{"out", dev_out, out_stride, out_type};
     if (rows > 0) GV_TRY(check_matrices(call, cols, {table}));
     GV_TRY(check_matrices(call, cols, {out}));
-    if (overlap(table, rows, out, count, cols)) return fail_call(GV_EINVAL, "%s: out overlaps the table", call);
+    if (overlap(table, rows, cols, out, count, cols)) return fail_call(GV_EINVAL, "%s: out overlaps the table", call);
     return launched(call, gv::launch_lookup({index, dev_table, dev_out, count, table_stride, out_stride, (uint32_t)rows, cols, type, out_type,
                                              scale}, (hipStream_t)stream));
 }
@@ -245,12 +245,103 @@ int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t inde
     const Matrix grad{"grad", dev_grad, grad_stride, type}, out{"out", dev_out, out_stride, out_type};
     if (count > 0) GV_TRY(check_matrices(call, cols, {grad}));
     GV_TRY(check_matrices(call, cols, {out}));
-    if (overlap(grad, count, out, rows, cols)) return fail_call(GV_EINVAL, "%s: out overlaps grad", call);
+    if (overlap(grad, count, cols, out, rows, cols)) return fail_call(GV_EINVAL, "%s: out overlaps grad", call);
     GV_TRY(check_workspace(call, dev_workspace, workspace_bytes, gv::lookup_grad_workspace(count, rows, cols, add != 0)));
     gv::LookupGradArgs a{};
     a.index = index, a.grad = dev_grad, a.out = dev_out, a.count = count, a.grad_stride = grad_stride, a.out_stride = out_stride;
     a.rows = (uint32_t)rows, a.cols = cols, a.type = type, a.out_type = out_type, a.scale = scale, a.add = add != 0;
     return launched(call, gv::launch_lookup_grad(a, dev_workspace, (hipStream_t)stream));
+}
+
+static int check_dense(const char *call, uint64_t rows, uint32_t cols, uint32_t outs, int type, int act) {
+    GV_TRY(check_shape(call, rows, cols, type, false));
+    if (outs == 0 || outs > GV_MAX_ROW_COLS) return fail_call(GV_EINVAL, "%s: %u columns of out: 1..%u", call, outs, GV_MAX_ROW_COLS);
+    if (act < GV_ACT_NONE || act > GV_ACT_SILU) return fail_call(GV_EINVAL, "%s: bad activation %d", call, act);
+    return GV_OK;
+}
+
+// A matrix of a layer, as far as it goes.
+struct Sized {
+    Matrix matrix;
+    uint64_t rows;
+    uint32_t cols;
+};
+static int check_apart(const char *call, std::initializer_list<Sized> written, std::initializer_list<Sized> read) {
+    for (const Sized &w : written)
+        for (const Sized &r : read)
+            if (w.matrix.at && r.matrix.at && overlap(w.matrix, w.rows, w.cols, r.matrix, r.rows, r.cols))
+                return fail_call(GV_EINVAL, "%s: %s overlaps %s", call, w.matrix.name, r.matrix.name);
+    return GV_OK;
+}
+
+int gv_dense_rows_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, uint64_t *bytes) {
+    const char *call = "gv_dense_rows_workspace";
+    GV_TRY(check_dense(call, rows, cols, outs, type, GV_ACT_NONE));
+    if (!bytes) return fail_call(GV_EINVAL, "%s: null output", call);
+    *bytes = gv::dense_workspace(rows, cols, outs, type);
+    return GV_OK;
+}
+
+int gv_dense_rows(uint64_t rows, uint32_t cols, uint32_t outs, int type, const void *dev_x, uint64_t x_stride, const void *dev_weight,
+                  uint64_t weight_stride, const void *dev_bias, int act, const void *dev_residual, uint64_t residual_stride,
+                  void *dev_pre, uint64_t pre_stride, void *dev_out, uint64_t out_stride, void *dev_workspace, uint64_t workspace_bytes,
+                  void *stream) {
+    const char *call = "gv_dense_rows";
+    GV_TRY(check_dense(call, rows, cols, outs, type, act));
+    if (rows == 0) return GV_OK;
+    const Sized x{{"x", dev_x, x_stride, type}, rows, cols}, weight{{"weight", dev_weight, weight_stride, type}, outs, cols};
+    const Sized pre{{"pre", dev_pre, pre_stride, type}, rows, outs}, out{{"out", dev_out, out_stride, type}, rows, outs};
+    GV_TRY(check_matrices(call, cols, {x.matrix, weight.matrix}));
+    GV_TRY(check_matrices(call, outs, {out.matrix}));
+    if (dev_bias) GV_TRY(check_array(call, "bias", dev_bias, size_of(type)));
+    if (dev_residual) GV_TRY(check_matrices(call, outs, {{"residual", dev_residual, residual_stride, type}}));
+    if (dev_pre) GV_TRY(check_matrices(call, outs, {pre.matrix}));
+    GV_TRY(check_apart(call, {out, pre}, {x, weight}));
+    GV_TRY(check_workspace(call, dev_workspace, workspace_bytes, gv::dense_workspace(rows, cols, outs, type)));
+    gv::DenseArgs a{};
+    a.x = dev_x, a.weight = dev_weight, a.bias = dev_bias, a.residual = dev_residual, a.pre = dev_pre, a.out = dev_out;
+    a.x_stride = x_stride, a.weight_stride = weight_stride, a.residual_stride = residual_stride, a.pre_stride = pre_stride;
+    a.out_stride = out_stride, a.rows = (uint32_t)rows, a.cols = cols, a.outs = outs, a.type = type, a.act = act;
+    return launched(call, gv::launch_dense(a, dev_workspace, (hipStream_t)stream));
+}
+
+int gv_dense_rows_backward_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, int act, int grad_x, int grad_weight,
+                                     int grad_bias, uint64_t *bytes) {
+    const char *call = "gv_dense_rows_backward_workspace";
+    GV_TRY(check_dense(call, rows, cols, outs, type, act));
+    if (!bytes) return fail_call(GV_EINVAL, "%s: null output", call);
+    *bytes = gv::dense_grad_workspace(rows, cols, outs, type, act, grad_x != 0, grad_weight != 0, grad_bias != 0);
+    return GV_OK;
+}
+
+int gv_dense_rows_backward(uint64_t rows, uint32_t cols, uint32_t outs, int type, const void *dev_grad_out, uint64_t grad_out_stride,
+                           const void *dev_x, uint64_t x_stride, const void *dev_weight, uint64_t weight_stride, int act,
+                           const void *dev_pre, uint64_t pre_stride, void *dev_grad_x, uint64_t grad_x_stride, void *dev_grad_weight,
+                           uint64_t grad_weight_stride, void *dev_grad_bias, void *dev_workspace, uint64_t workspace_bytes, void *stream) {
+    const char *call = "gv_dense_rows_backward";
+    GV_TRY(check_dense(call, rows, cols, outs, type, act));
+    const Sized grad{{"grad_out", dev_grad_out, grad_out_stride, type}, rows, outs}, x{{"x", dev_x, x_stride, type}, rows, cols};
+    const Sized weight{{"weight", dev_weight, weight_stride, type}, outs, cols}, pre{{"pre", dev_pre, pre_stride, type}, rows, outs};
+    const Sized grad_x{{"grad_x", dev_grad_x, grad_x_stride, type}, rows, cols};
+    const Sized grad_weight{{"grad_weight", dev_grad_weight, grad_weight_stride, type}, outs, cols};
+    if (rows > 0) {
+        GV_TRY(check_matrices(call, outs, {grad.matrix}));
+        if (act != GV_ACT_NONE) GV_TRY(check_matrices(call, outs, {pre.matrix}));
+        if (dev_grad_x) GV_TRY(check_matrices(call, cols, {weight.matrix, grad_x.matrix}));
+        if (dev_grad_weight) GV_TRY(check_matrices(call, cols, {x.matrix}));
+    }
+    if (dev_grad_weight) GV_TRY(check_matrices(call, cols, {grad_weight.matrix}));
+    if (dev_grad_bias) GV_TRY(check_array(call, "grad_bias", dev_grad_bias, size_of(type)));
+    GV_TRY(check_apart(call, {grad_x, grad_weight}, {grad, x, weight, pre}));
+    GV_TRY(check_apart(call, {grad_x}, {grad_weight}));
+    GV_TRY(check_workspace(call, dev_workspace, workspace_bytes,
+                           gv::dense_grad_workspace(rows, cols, outs, type, act, dev_grad_x, dev_grad_weight, dev_grad_bias)));
+    gv::DenseGradArgs a{};
+    a.grad = dev_grad_out, a.x = dev_x, a.weight = dev_weight, a.pre = dev_pre, a.grad_x = rows > 0 ? dev_grad_x : nullptr;
+    a.grad_weight = dev_grad_weight, a.grad_bias = dev_grad_bias, a.rows = rows, a.grad_stride = grad_out_stride, a.x_stride = x_stride;
+    a.weight_stride = weight_stride, a.pre_stride = pre_stride, a.grad_x_stride = grad_x_stride;
+    a.grad_weight_stride = grad_weight_stride, a.cols = cols, a.outs = outs, a.type = type, a.act = act;
+    return launched(call, gv::launch_dense_grad(a, dev_workspace, (hipStream_t)stream));
 }
 
 static int check_select(const char *call, uint64_t queries, uint64_t rows, uint32_t beams, uint32_t best) {

@@ -15,10 +15,11 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from .binding import GV_BF16, GV_F16, GV_F32, GV_I8, GV_I32, GV_I64, GV_OK, GvError, load
+from .binding import GV_ACT_NONE, GV_BF16, GV_F16, GV_F32, GV_I8, GV_I32, GV_I64, GV_OK, GvError, load
 
 __all__ = ["NormRows", "NormGrads", "gv_drop_rows", "gv_norm_rows", "gv_norm_rows_workspace", "gv_norm_rows_backward",
            "gv_quantize_rows", "gv_score_rows", "gv_lookup_rows", "gv_lookup_rows_workspace", "gv_lookup_rows_backward",
+           "DenseRows", "DenseGrads", "gv_dense_rows", "gv_dense_rows_workspace", "gv_dense_rows_backward", "gv_dense_rows_backward_workspace",
            "Selection", "gv_select_rows", "gv_select_rows_workspace"]
 
 _TYPES = {torch.float32: GV_F32, torch.bfloat16: GV_BF16, torch.float16: GV_F16}
@@ -41,6 +42,18 @@ class NormGrads(NamedTuple):
     x: torch.Tensor
     residual: Optional[torch.Tensor]
     gain: Optional[torch.Tensor]   # float32[cols]
+
+
+class DenseRows(NamedTuple):
+    out: torch.Tensor
+    pre: Optional[torch.Tensor]
+
+
+class DenseGrads(NamedTuple):
+    """Of a layer; None where it was not asked for.  The residual's is the gradient that came in."""
+    x: Optional[torch.Tensor]
+    weight: Optional[torch.Tensor]
+    bias: Optional[torch.Tensor]
 
 
 class Selection(NamedTuple):
@@ -339,6 +352,82 @@ def gv_lookup_rows_backward(grad_out, index, rows, *, scale=1.0, out_type=None, 
     if passed:
         _written(out)
     return out
+
+
+@functools.lru_cache(maxsize=256)
+def gv_dense_rows_workspace(rows, cols, outs, type):
+    """Bytes of scratch that a layer takes."""
+    n = C.c_uint64()
+    rc = load().gv_dense_rows_workspace(rows, cols, outs, type, C.byref(n))
+    if rc != GV_OK:
+        raise GvError(rc, load().gv_last_error(None).decode())
+    return n.value
+
+
+def gv_dense_rows(x, weight, bias=None, residual=None, *, act=GV_ACT_NONE, keep_pre=False, out=None):
+    """residual + act(x weight^T + bias).  weight is [outs][cols], all are of x's type.  keep_pre keeps what the activation is taken
+    of, for gv_dense_rows_backward.  out may be passed, and may be residual."""
+    at, stride, rows, cols, kind, gpu = _first("x", x)
+    dtype = x.dtype
+    if weight.dim() != 2:
+        _refuse("weight: a 2-D tensor")
+    outs = weight.shape[0]
+    weight_at, weight_stride = _rows("weight", weight, outs, cols, dtype, gpu)
+    bias_at = None if bias is None else _array("bias", bias, outs, dtype, gpu)
+    res_at, res_stride = (None, 0) if residual is None else _rows("residual", residual, rows, outs, dtype, gpu)
+    passed = out is not None
+    if passed:
+        out_at, out_stride = _rows("out", out, rows, outs, dtype, gpu)
+    else:
+        out = x.new_empty((rows, outs))
+        out_at, out_stride = out.data_ptr(), outs
+    if _recording() and (passed or x.requires_grad or weight.requires_grad or bias is not None or residual is not None):
+        _without_graph(x, weight, bias, residual, out)
+    pre = x.new_empty((rows, outs)) if keep_pre else None
+    size = gv_dense_rows_workspace(rows, cols, outs, kind)
+    space = torch.empty(size, dtype=_uint8, device=x.device) if size else None
+    _call(load().gv_dense_rows, gpu, rows, cols, outs, kind, at, stride, weight_at, weight_stride, bias_at, act, res_at, res_stride,
+          pre.data_ptr() if keep_pre else None, outs, out_at, out_stride, space.data_ptr() if size else None, size)
+    if passed:
+        _written(out)
+    return DenseRows(out, pre)
+
+
+@functools.lru_cache(maxsize=256)
+def gv_dense_rows_backward_workspace(rows, cols, outs, type, act, keep_x=True, keep_weight=True, keep_bias=False):
+    """Bytes of scratch that the gradients of a layer take."""
+    n = C.c_uint64()
+    rc = load().gv_dense_rows_backward_workspace(rows, cols, outs, type, act, keep_x, keep_weight, keep_bias, C.byref(n))
+    if rc != GV_OK:
+        raise GvError(rc, load().gv_last_error(None).decode())
+    return n.value
+
+
+def gv_dense_rows_backward(grad_out, x, weight, pre=None, *, act=GV_ACT_NONE, keep_x=True, keep_weight=True, keep_bias=False):
+    """Gradients of gv_dense_rows for x, weight and bias; the residual's is grad_out.  pre is what the layer kept, where it has an
+    activation."""
+    at, stride, rows, outs, kind, gpu = _first("grad_out", grad_out)
+    dtype = grad_out.dtype
+    if x.dim() != 2:
+        _refuse("x: a 2-D tensor")
+    cols = x.shape[1]
+    x_at, x_stride = _rows("x", x, rows, cols, dtype, gpu)
+    weight_at, weight_stride = _rows("weight", weight, outs, cols, dtype, gpu)
+    pre_at, pre_stride = (None, 0) if pre is None else _rows("pre", pre, rows, outs, dtype, gpu)
+    if pre is None and act != GV_ACT_NONE:
+        _refuse("pre: an activation's gradient is taken of it")
+    if _recording() and (grad_out.requires_grad or x.requires_grad or weight.requires_grad or pre is not None):
+        _without_graph(grad_out, x, weight, pre)
+    keep_x, keep_weight, keep_bias = bool(keep_x), bool(keep_weight), bool(keep_bias)
+    grad_x = grad_out.new_empty((rows, cols)) if keep_x else None
+    grad_weight = grad_out.new_empty((outs, cols)) if keep_weight else None
+    grad_bias = grad_out.new_empty(outs) if keep_bias else None
+    size = gv_dense_rows_backward_workspace(rows, cols, outs, kind, act, keep_x, keep_weight, keep_bias)
+    space = torch.empty(size, dtype=_uint8, device=grad_out.device) if size else None
+    _call(load().gv_dense_rows_backward, gpu, rows, cols, outs, kind, at, stride, x_at, x_stride, weight_at, weight_stride, act, pre_at,
+          pre_stride, grad_x.data_ptr() if keep_x else None, cols, grad_weight.data_ptr() if keep_weight else None, cols,
+          grad_bias.data_ptr() if keep_bias else None, space.data_ptr() if size else None, size)
+    return DenseGrads(grad_x, grad_weight, grad_bias)
 
 
 @functools.lru_cache(maxsize=256)
