@@ -235,6 +235,195 @@ __global__ __launch_bounds__(2 * kTile) void k_product(DenseArgs a, uint32_t til
         }
 }
 
+// ---------------------------------------------------------------------------
+// The same for 16-bit types whose rows are whole pieces (of 8 values, aligned): a step's 64 k's go from memory straight into LDS, where
+// an operand lies as it does in memory, and what lies with the values of a k together is turned by the loads that transpose.
+// A wave's values of half a step are read while those of the half before are multiplied; one barrier a step says that the next
+// step has arrived and that this one's place is free for the step after that.
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s4v LdsFour;
+typedef __attribute__((address_space(3))) void LdsAny;
+
+constexpr uint32_t kWide = 64;                 // k's of a step
+constexpr uint64_t kWideStride = 1ull << 21;   // a tile's rows lie within 2^31 bytes
+
+template <int kTile, bool kAlong>
+struct Operand {
+    static constexpr uint32_t kThreads = 2 * kTile, kLoads = kTile * 128 / 16 / kThreads, kUnits = kTile / 16;
+    static constexpr uint32_t kRows = kThreads / (kAlong ? 8 : kTile / 8);  // that the workgroup loads at once
+    const char *at, *end;  // the tile's first value of the next step, and of the matrix behind its last
+    uint64_t step, rows;   // bytes to the next step, and to the next rows
+    uint32_t from[2];      // of this lane in the first rows and in the second (the third's are the first's), in bytes
+    // A piece's place: along k rows of 128 bytes, piece p of row r at p ^ r % 8; otherwise rows of kTile values of one k, in units of 16
+    // values, unit u of row k at u ^ turn(k): what 16 lanes read together, four k's, and the four groups of lanes are different units.
+    static __device__ __forceinline__ uint32_t turn(uint32_t k) { return ((k & 3) | (k >> 3 & 3) << 2) & (kUnits - 1); }
+    // value k (and first row) of a matrix of `lines` lines of `length` values
+    __device__ __forceinline__ void begin(const void *p, uint64_t stride, uint64_t lines, uint64_t length, uint32_t first, uint32_t k) {
+        at = (const char *)p + 2 * (kAlong ? first * stride + k : k * stride + first);
+        end = (const char *)p + 2 * ((lines - 1) * stride + length);
+        step = kAlong ? 2 * kWide : 2 * kWide * stride;
+        rows = 2 * kRows * stride;
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+            const uint32_t id = j * kThreads + threadIdx.x, row = threadIdx.x / (kThreads / kRows);
+            if constexpr (kAlong) from[j] = 2 * (row * (uint32_t)stride + (id ^ id / 8) % 8 * 8);
+            else from[j] = 2 * (row * (uint32_t)stride + 16 * (id % (kTile / 8) / 2 ^ turn(id / (kTile / 8))) + id % 2 * 8);
+        }
+    }
+    // Asks for the next step.  Nothing is read behind the matrix's end; what lies behind its rows and columns is not used.
+    __device__ __forceinline__ void fetch(char *tile) {
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63u);
+        const char *p = at;
+#pragma unroll
+        for (uint32_t j = 0; j < kLoads; ++j, p += rows) {
+            const uint32_t bytes = p < end ? (uint32_t)std::min<uint64_t>(end - p, 0xFFFFFFFFu) : 0;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000),
+                                                     (LdsAny *)(tile + (j * kThreads + wave) * 16), 16, from[j % 2], 0, 0, 0);
+        }
+        at += step;
+    }
+    // a step of `left` k's, `steps` steps on, and zeros behind them
+    __device__ __forceinline__ void fetch_some(char *tile, uint32_t steps, uint32_t left) const {
+        const char *p = at + steps * step;
+#pragma unroll
+        for (uint32_t j = 0; j < kLoads; ++j, p += rows) {
+            const uint32_t id = j * kThreads + threadIdx.x;
+            const uint32_t k = kAlong ? (id ^ id / 8) % 8 * 8 : id / (kTile / 8);
+            uint4 v = {};
+            if (k < left && p + from[j % 2] < end) __builtin_memcpy(&v, p + from[j % 2], 16);  // whole pieces: 8 k's of a row, or 8 rows of a k
+            *(uint4 *)(tile + id * 16) = v;
+        }
+    }
+};
+
+// How a lane reads eight k's (piece 4 half + its group of a step) of 16 rows from row + 16 i on, for the matrix instruction.
+template <int kTile, bool kAlong>
+struct Reader {
+    uint32_t base;  // in a tile, for half 0 and i 0
+    __device__ __forceinline__ void begin(uint32_t row) {
+        const uint32_t lane = threadIdx.x % 64, group = lane / 16;
+        if constexpr (kAlong) {
+            base = (row + lane % 16) * 128 + (group ^ lane % 8) * 16;
+        } else {
+            const uint32_t four = lane % 16 / 4;  // turn() of the k's that this lane points to
+            base = (8 * group + four) * (2 * kTile) + ((row / 16) ^ ((four | group << 2) & (kTile / 16 - 1))) * 32 + lane % 4 * 8;
+        }
+    }
+    __device__ __forceinline__ uint4 read(const char *tile, int half, int i) const {
+        if constexpr (kAlong) {
+            return *(const uint4 *)(tile + (base ^ 64 * half) + 2048 * i);
+        } else {
+            const char *at = tile + (base ^ 32 * i) + half * (32 * 2 * kTile);
+            const s4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsFour *)at);
+            const s4v high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsFour *)(at + 8 * kTile));
+            const uint2 x = __builtin_bit_cast(uint2, low), y = __builtin_bit_cast(uint2, high);
+            return uint4{x.x, x.y, y.x, y.y};
+        }
+    }
+};
+
+template <class T, int kTile, bool kAAlong, bool kBAlong>
+__global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint32_t tiles_m, uint32_t tiles_n) {
+    // waves: 2 x kTile / 64, of kTile / 2 x 64
+    constexpr int kMs = kTile / 32, kNs = 4;
+    constexpr uint32_t kBytes = kTile * 128;
+    // of one step and of the next; they are apart so that the compiler sees that what is read is not what is being fetched
+    __shared__ __attribute__((aligned(16))) char a0[kBytes], a1[kBytes], b0[kBytes], b1[kBytes];
+    const uint32_t all = tiles_m * tiles_n, split = blockIdx.x / all;
+    uint32_t id = blockIdx.x % all;
+    if (id < all / 8 * 8) id = id % 8 * (all / 8) + id / 8;
+    const uint32_t band = id / (8 * tiles_n), high = std::min(8u, tiles_m - 8 * band), in_band = id - 8 * band * tiles_n;
+    const uint32_t m0 = (8 * band + in_band % high) * kTile, n0 = in_band / high * kTile;
+    const uint32_t k_first = split * a.split_k, k_last = std::min<uint64_t>(a.cols, (uint64_t)k_first + a.split_k);
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, wm = wave % 2 * (kTile / 2), wn = wave / 2 * 64;
+    f4 sums[kMs][kNs];
+#pragma unroll
+    for (int i = 0; i < kMs; ++i)
+#pragma unroll
+        for (int j = 0; j < kNs; ++j) sums[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    Operand<kTile, kAAlong> of_a;
+    Operand<kTile, kBAlong> of_b;
+    of_a.begin(a.x, a.x_stride, kAAlong ? a.rows : a.cols, kAAlong ? a.cols : a.rows, m0, k_first);
+    of_b.begin(a.weight, a.weight_stride, kBAlong ? a.outs : a.cols, kBAlong ? a.cols : a.outs, n0, k_first);
+    // Steps go in pairs.  What is left of k behind the whole steps goes first, and a step of zeros makes the number even.
+    uint32_t whole = (k_last - k_first) / kWide;
+    const uint32_t left = (k_last - k_first) % kWide, odd = (whole + (left ? 1 : 0)) % 2;
+    const auto fetch = [&](char *ta, char *tb) {
+        if (whole == 0) return;
+        of_a.fetch(ta);
+        of_b.fetch(tb);
+        --whole;
+    };
+    const auto arrived = [] {
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    Reader<kTile, kAAlong> read_a;
+    Reader<kTile, kBAlong> read_b;
+    read_a.begin(wm);
+    read_b.begin(wn);
+    uint4 ma[kMs], nb[2][kNs];
+    // the products of half a step; the values of the next half, of these tiles, replace those that are done with
+    const auto products = [&](auto now, const char *ta, const char *tb) {
+        constexpr int kHalf = decltype(now)::value, kNext = kHalf ^ 1;
+#pragma unroll
+        for (int j = 0; j < kNs; ++j) nb[kNext][j] = read_b.read(tb, kNext, j);
+#pragma unroll
+        for (int i = 0; i < kMs; ++i) {
+#pragma unroll
+            for (int j = 0; j < kNs; ++j) multiply(nb[kHalf][j], ma[i], sums[i][j], (T *)nullptr);
+            ma[i] = read_a.read(ta, kNext, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    constexpr std::integral_constant<int, 0> kFirst;
+    constexpr std::integral_constant<int, 1> kSecond;
+    const uint32_t pairs = (whole + (left ? 1 : 0) + odd) / 2;
+    if (left || odd) {
+        of_a.fetch_some(a0, whole, left);
+        of_b.fetch_some(b0, whole, left);
+    } else {
+        fetch(a0, b0);
+    }
+    if (left && odd) {
+        of_a.fetch_some(a1, 0, 0);
+        of_b.fetch_some(b1, 0, 0);
+        arrived();
+    } else {
+        arrived();
+        fetch(a1, b1);
+    }
+#pragma unroll
+    for (int i = 0; i < kMs; ++i) ma[i] = read_a.read(a0, 0, i);
+#pragma unroll
+    for (int j = 0; j < kNs; ++j) nb[0][j] = read_b.read(b0, 0, j);
+    for (uint32_t pair = 0; pair < pairs; ++pair) {
+        products(kFirst, a0, b0);
+        arrived();
+        fetch(a0, b0);
+        products(kSecond, a1, b1);
+        products(kFirst, a1, b1);
+        arrived();
+        fetch(a1, b1);
+        products(kSecond, a0, b0);
+    }
+#pragma unroll
+    for (int i = 0; i < kMs; ++i)
+#pragma unroll
+        for (int j = 0; j < kNs; ++j) {
+            const uint32_t m = m0 + wm + 16 * i + lane % 16, n = n0 + wn + 16 * j + 4 * (lane / 16);
+            if (a.partial) {
+                if (m < a.rows && n < a.outs) {
+                    Values<float, 4> v = __builtin_bit_cast(decltype(v), sums[i][j]);
+                    v.store(a.partial + ((uint64_t)split * a.rows + m) * a.outs + n, a.outs - n);
+                }
+            } else {
+                finish<T>(a, m, n, sums[i][j]);
+            }
+        }
+}
+
 // The sums of the parts that a product's k was cut into, in their order.
 template <class T>
 __global__ __launch_bounds__(256) void k_join_product(DenseArgs a, uint32_t splits) {
@@ -378,7 +567,18 @@ hipError_t product(DenseArgs a, void *workspace, hipStream_t stream) {
     a.split_k = c.split_k;
     a.partial = c.splits > 1 ? (float *)workspace : nullptr;
     const uint32_t blocks = c.tiles_m * c.tiles_n * c.splits;
-    const hipError_t e = c.tile == 256   ? launch(k_product<T, 256, kAAlong, kBAlong>, blocks, 512, 0, stream, a, c.tiles_m, c.tiles_n)
+    bool wide = false;
+    hipError_t e = hipSuccess;
+    if constexpr (sizeof(T) == 2) {
+        const auto whole = [](const void *p, uint64_t stride, uint64_t together) {
+            return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && together % 8 == 0 && together > 0 && stride < kWideStride;
+        };
+        wide = c.tile >= 128 && whole(a.x, a.x_stride, kAAlong ? a.cols : a.rows) && whole(a.weight, a.weight_stride, kBAlong ? a.cols : a.outs);
+        if (wide)
+            e = c.tile == 256 ? launch(k_product_wide<T, 256, kAAlong, kBAlong>, blocks, 512, 0, stream, a, c.tiles_m, c.tiles_n)
+                              : launch(k_product_wide<T, 128, kAAlong, kBAlong>, blocks, 256, 0, stream, a, c.tiles_m, c.tiles_n);
+    }
+    if (!wide) e = c.tile == 256   ? launch(k_product<T, 256, kAAlong, kBAlong>, blocks, 512, 0, stream, a, c.tiles_m, c.tiles_n)
                          : c.tile == 128 ? launch(k_product<T, 128, kAAlong, kBAlong>, blocks, 256, 0, stream, a, c.tiles_m, c.tiles_n)
                                          : launch(k_product<T, 64, kAAlong, kBAlong>, blocks, 128, 0, stream, a, c.tiles_m, c.tiles_n);
     if (e != hipSuccess || c.splits == 1) return e;
