@@ -21,18 +21,36 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 
+// The normal distribution's Phi(z) and, on the way, exp(-z^2 / 2).  Phi(-|z|) = (a1 t + ... + a5 t^5) exp(-z^2 / 2) / 2 with
+// t = 1 / (1 + 0.3275911 |z| / sqrt 2): formula 7.1.26 of Abramowitz and Stegun's Handbook, within 1.5e-7 / 2 of the true value, which is a
+// unit of fp32 near 1; where Phi is small the factor exp(-z^2 / 2) keeps it so.  erff takes three times the instructions: 65536 x 512 x
+// 2048 with gelu took 520 us by it.
+__device__ __forceinline__ float normal(float z, float &bell) {
+    const float x = fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(x, 0.23164190f, 1.0f));
+    bell = __expf(-0.5f * z * z);
+    const float poly = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
+    const float tail = 0.5f * t * poly * bell;
+    return z < 0.0f ? tail : 1.0f - tail;
+}
 // act(z), and its slope
 __device__ __forceinline__ float act_of(int act, float z) {
     if (act == GV_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (act == GV_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    if (act == GV_ACT_SILU) return z / (1.0f + __expf(-z));
+    if (act == GV_ACT_GELU) {
+        float bell;
+        return z * normal(z, bell);
+    }
+    if (act == GV_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));
     return z;
 }
 __device__ __forceinline__ float slope_of(int act, float z) {
     if (act == GV_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if (act == GV_ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * (0.39894228040143268f * __expf(-0.5f * z * z));
+    if (act == GV_ACT_GELU) {
+        float bell;
+        const float phi = normal(z, bell);
+        return fmaf(z * 0.39894228040143268f, bell, phi);
+    }
     if (act == GV_ACT_SILU) {
-        const float s = 1.0f / (1.0f + __expf(-z));
+        const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
         return s * (1.0f + z * (1.0f - s));
     }
     return 1.0f;
@@ -63,6 +81,20 @@ struct Values {
             for (int i = 0; i < N; ++i) at[i] = (uint32_t)i < left ? p[i] : (T)0.0f;
         }
     }
+    __device__ __forceinline__ void round(const float (&v)[N]) {
+        if constexpr (sizeof(T) == 2) {  // two at a time: the machine rounds pairs
+            typedef float f2 __attribute__((ext_vector_type(2)));
+            typedef T t2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+            for (int i = 0; i < N; i += 2) {
+                const t2 pair = __builtin_convertvector((f2{v[i], v[i + 1]}), t2);
+                at[i] = pair[0], at[i + 1] = pair[1];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) at[i] = (T)v[i];
+        }
+    }
     __device__ __forceinline__ void store(T *p, uint32_t left) const {
         if (left >= (uint32_t)N) {
             __builtin_memcpy(p, this, sizeof *this);
@@ -75,36 +107,38 @@ struct Values {
 };
 __device__ __forceinline__ uint32_t left_of(uint32_t at, uint32_t all) { return at < all ? all - at : 0; }
 
-// What becomes of the four sums of row m from column n on.
-template <class T>
-__device__ __forceinline__ void finish(const DenseArgs &a, uint32_t m, uint32_t n, f4 sums) {
+// What becomes of the N sums of row m from column n on.
+template <class T, int N>
+__device__ __forceinline__ void finish(const DenseArgs &a, uint32_t m, uint32_t n, uint32_t split, float (&z)[N]) {
     if (m >= a.rows || n >= a.outs) return;
     const uint32_t left = a.outs - n;
-    float z[4] = {sums[0], sums[1], sums[2], sums[3]};
+    if (a.partial) {
+        Values<float, N> v = __builtin_bit_cast(decltype(v), z);
+        v.store(a.partial + ((uint64_t)split * a.rows + m) * a.outs + n, left);
+        return;
+    }
     if (a.bias) {
-        Values<T, 4> b;
+        Values<T, N> b;
         b.load((const T *)a.bias + n, left);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] += (float)b.at[i];
+        for (int i = 0; i < N; ++i) z[i] += (float)b.at[i];
     }
-    Values<T, 4> to;
+    Values<T, N> to;
     if (a.pre) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) to.at[i] = (T)z[i];
+        to.round(z);
         to.store((T *)a.pre + m * a.pre_stride + n, left);
     }
     if (a.act != GV_ACT_NONE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = act_of(a.act, z[i]);
+        for (int i = 0; i < N; ++i) z[i] = act_of(a.act, z[i]);
     }
     if (a.residual) {
-        Values<T, 4> r;
+        Values<T, N> r;
         r.load((const T *)a.residual + m * a.residual_stride + n, left);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] += (float)r.at[i];
+        for (int i = 0; i < N; ++i) z[i] += (float)r.at[i];
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) to.at[i] = (T)z[i];
+    to.round(z);
     to.store((T *)a.out + m * a.out_stride + n, left);
 }
 
@@ -223,15 +257,8 @@ __global__ __launch_bounds__(2 * kTile) void k_product(DenseArgs a, uint32_t til
     for (int i = 0; i < kMs; ++i)
 #pragma unroll
         for (int j = 0; j < kNs; ++j) {
-            const uint32_t m = m0 + wm + 16 * i + lane % 16, n = n0 + wn + 16 * j + 4 * (lane / 16);
-            if (a.partial) {
-                if (m < a.rows && n < a.outs) {
-                    Values<float, 4> v = __builtin_bit_cast(decltype(v), sums[i][j]);
-                    v.store(a.partial + ((uint64_t)split * a.rows + m) * a.outs + n, a.outs - n);
-                }
-            } else {
-                finish<T>(a, m, n, sums[i][j]);
-            }
+            float z[4] = {sums[i][j][0], sums[i][j][1], sums[i][j][2], sums[i][j][3]};
+            finish<T>(a, m0 + wm + 16 * i + lane % 16, n0 + wn + 16 * j + 4 * (lane / 16), split, z);
         }
 }
 
@@ -247,16 +274,22 @@ typedef __attribute__((address_space(3))) void LdsAny;
 constexpr uint32_t kWide = 64;                 // k's of a step
 constexpr uint64_t kWideStride = 1ull << 21;   // a tile's rows lie within 2^31 bytes
 
-template <int kTile, bool kAlong>
+// kSpread: of B.  The matrix instruction's row 4 g + r of tile j of a wave's 64 rows of B is row 16 g + 4 j + r of them, so that the lanes of
+// group g end with 16 columns of the result in a row, which four of them write as a whole line.
+template <int kTile, bool kAlong, bool kSpread>
 struct Operand {
     static constexpr uint32_t kThreads = 2 * kTile, kLoads = kTile * 128 / 16 / kThreads, kUnits = kTile / 16;
-    static constexpr uint32_t kRows = kThreads / (kAlong ? 8 : kTile / 8);  // that the workgroup loads at once
+    static constexpr uint32_t kLine = kAlong ? 8 : kTile / 8;  // pieces
+    static constexpr uint32_t kRows = kThreads / kLine;        // that the workgroup loads at once
     const char *at, *end;  // the tile's first value of the next step, and of the matrix behind its last
     uint64_t step, rows;   // bytes to the next step, and to the next rows
     uint32_t from[2];      // of this lane in the first rows and in the second (the third's are the first's), in bytes
-    // A piece's place: along k rows of 128 bytes, piece p of row r at p ^ r % 8; otherwise rows of kTile values of one k, in units of 16
-    // values, unit u of row k at u ^ turn(k): what 16 lanes read together, four k's, and the four groups of lanes are different units.
-    static __device__ __forceinline__ uint32_t turn(uint32_t k) { return ((k & 3) | (k >> 3 & 3) << 2) & (kUnits - 1); }
+    // A piece's place: along k rows of 128 bytes, piece p of row r at p ^ turn(r); otherwise rows of kTile values of one k, piece p of
+    // row k at p ^ turn(k): what lanes read together lies in different banks.
+    static __device__ __forceinline__ uint32_t turn(uint32_t row) {
+        if constexpr (kAlong) return kSpread ? (row & 3) | (row >> 4 & 1) << 2 : row & 7;
+        else return kSpread ? (row & 1) | (row >> 1 & 1) << 3 : 2 * (((row & 3) | (row >> 3 & 3) << 2) & (kUnits - 1));
+    }
     // value k (and first row) of a matrix of `lines` lines of `length` values
     __device__ __forceinline__ void begin(const void *p, uint64_t stride, uint64_t lines, uint64_t length, uint32_t first, uint32_t k) {
         at = (const char *)p + 2 * (kAlong ? first * stride + k : k * stride + first);
@@ -265,9 +298,8 @@ struct Operand {
         rows = 2 * kRows * stride;
 #pragma unroll
         for (uint32_t j = 0; j < 2; ++j) {
-            const uint32_t id = j * kThreads + threadIdx.x, row = threadIdx.x / (kThreads / kRows);
-            if constexpr (kAlong) from[j] = 2 * (row * (uint32_t)stride + (id ^ id / 8) % 8 * 8);
-            else from[j] = 2 * (row * (uint32_t)stride + 16 * (id % (kTile / 8) / 2 ^ turn(id / (kTile / 8))) + id % 2 * 8);
+            const uint32_t id = j * kThreads + threadIdx.x, row = threadIdx.x / kLine;
+            from[j] = 2 * (row * (uint32_t)stride + (id % kLine ^ turn(id / kLine)) * 8);
         }
     }
     // Asks for the next step.  Nothing is read behind the matrix's end; what lies behind its rows and columns is not used.
@@ -288,7 +320,7 @@ struct Operand {
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; ++j, p += rows) {
             const uint32_t id = j * kThreads + threadIdx.x;
-            const uint32_t k = kAlong ? (id ^ id / 8) % 8 * 8 : id / (kTile / 8);
+            const uint32_t k = kAlong ? (id % kLine ^ turn(id / kLine)) * 8 : id / kLine;
             uint4 v = {};
             if (k < left && p + from[j % 2] < end) __builtin_memcpy(&v, p + from[j % 2], 16);  // whole pieces: 8 k's of a row, or 8 rows of a k
             *(uint4 *)(tile + id * 16) = v;
@@ -296,24 +328,28 @@ struct Operand {
     }
 };
 
-// How a lane reads eight k's (piece 4 half + its group of a step) of 16 rows from row + 16 i on, for the matrix instruction.
-template <int kTile, bool kAlong>
+// How a lane reads eight k's (piece 4 half + its group of a step) of tile i of the wave's rows, for the matrix instruction.
+template <int kTile, bool kAlong, bool kSpread>
 struct Reader {
-    uint32_t base;  // in a tile, for half 0 and i 0
+    uint32_t base;  // in a step, for half 0 and tile 0
     __device__ __forceinline__ void begin(uint32_t row) {
-        const uint32_t lane = threadIdx.x % 64, group = lane / 16;
+        using Of = Operand<kTile, kAlong, kSpread>;
+        const uint32_t lane = threadIdx.x % 64, group = lane / 16, at = lane % 16;
         if constexpr (kAlong) {
-            base = (row + lane % 16) * 128 + (group ^ lane % 8) * 16;
+            row += kSpread ? at / 4 * 16 + at % 4 : at;  // tiles are 4 or 16 rows apart
+            base = row * 128 + (group ^ Of::turn(row)) * 16;
         } else {
-            const uint32_t four = lane % 16 / 4;  // turn() of the k's that this lane points to
-            base = (8 * group + four) * (2 * kTile) + ((row / 16) ^ ((four | group << 2) & (kTile / 16 - 1))) * 32 + lane % 4 * 8;
+            // lanes point to four rows of one k each, and get four k's of one row
+            const uint32_t k = 8 * group + at / 4, piece = kSpread ? row / 8 + at % 4 * 2 : row / 8 + at % 4 / 2;
+            base = k * (2 * kTile) + (piece ^ Of::turn(k)) * 16 + (kSpread ? 0 : at % 2 * 8);
         }
     }
     __device__ __forceinline__ uint4 read(const char *tile, int half, int i) const {
         if constexpr (kAlong) {
-            return *(const uint4 *)(tile + (base ^ 64 * half) + 2048 * i);
+            // turn() of rows that are 16 apart is the same; of rows 4 i apart as well
+            return *(const uint4 *)(tile + (base ^ 64 * half) + (kSpread ? 512 : 2048) * i);
         } else {
-            const char *at = tile + (base ^ 32 * i) + half * (32 * 2 * kTile);
+            const char *at = tile + (kSpread ? (base ^ 16 * (i / 2)) + 8 * (i % 2) : base ^ 32 * i) + half * (32 * 2 * kTile);
             const s4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsFour *)at);
             const s4v high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsFour *)(at + 8 * kTile));
             const uint2 x = __builtin_bit_cast(uint2, low), y = __builtin_bit_cast(uint2, high);
@@ -341,8 +377,8 @@ __global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint
     for (int i = 0; i < kMs; ++i)
 #pragma unroll
         for (int j = 0; j < kNs; ++j) sums[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    Operand<kTile, kAAlong> of_a;
-    Operand<kTile, kBAlong> of_b;
+    Operand<kTile, kAAlong, false> of_a;
+    Operand<kTile, kBAlong, true> of_b;
     of_a.begin(a.x, a.x_stride, kAAlong ? a.rows : a.cols, kAAlong ? a.cols : a.rows, m0, k_first);
     of_b.begin(a.weight, a.weight_stride, kBAlong ? a.outs : a.cols, kBAlong ? a.cols : a.outs, n0, k_first);
     // Steps go in pairs.  What is left of k behind the whole steps goes first, and a step of zeros makes the number even.
@@ -359,8 +395,8 @@ __global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint
         __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
     };
-    Reader<kTile, kAAlong> read_a;
-    Reader<kTile, kBAlong> read_b;
+    Reader<kTile, kAAlong, false> read_a;
+    Reader<kTile, kBAlong, true> read_b;
     read_a.begin(wm);
     read_b.begin(wn);
     uint4 ma[kMs], nb[2][kNs];
@@ -408,19 +444,15 @@ __global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint
         fetch(a1, b1);
         products(kSecond, a0, b0);
     }
+    // a lane has 16 columns in a row of each of its rows
 #pragma unroll
     for (int i = 0; i < kMs; ++i)
 #pragma unroll
-        for (int j = 0; j < kNs; ++j) {
-            const uint32_t m = m0 + wm + 16 * i + lane % 16, n = n0 + wn + 16 * j + 4 * (lane / 16);
-            if (a.partial) {
-                if (m < a.rows && n < a.outs) {
-                    Values<float, 4> v = __builtin_bit_cast(decltype(v), sums[i][j]);
-                    v.store(a.partial + ((uint64_t)split * a.rows + m) * a.outs + n, a.outs - n);
-                }
-            } else {
-                finish<T>(a, m, n, sums[i][j]);
-            }
+        for (int h = 0; h < 2; ++h) {
+            float z[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) z[c] = sums[i][2 * h + c / 4][c % 4];
+            finish<T>(a, m0 + wm + 16 * i + lane % 16, n0 + wn + 16 * (lane / 16) + 8 * h, split, z);
         }
 }
 
@@ -437,7 +469,10 @@ __global__ __launch_bounds__(256) void k_join_product(DenseArgs a, uint32_t spli
             v.load(a.partial + ((uint64_t)s * a.rows + m) * a.outs + n, a.outs - n);
             sums += __builtin_bit_cast(f4, v);
         }
-        finish<T>(a, m, n, sums);
+        float z[4] = {sums[0], sums[1], sums[2], sums[3]};
+        DenseArgs whole = a;
+        whole.partial = nullptr;
+        finish<T>(whole, m, n, 0, z);
     }
 }
 
@@ -479,7 +514,8 @@ __global__ __launch_bounds__(kFewThreads) void k_product_few(DenseArgs a) {
     f4 all = joined[0][wave][lane];
 #pragma unroll
     for (int w = 1; w < kFewWaves; ++w) all += joined[w][wave][lane];
-    finish<T>(a, 16 * wave + lane % 16, blockIdx.x * 16 + 4 * (lane / 16), all);
+    float z[4] = {all[0], all[1], all[2], all[3]};
+    finish<T>(a, 16 * wave + lane % 16, blockIdx.x * 16 + 4 * (lane / 16), 0, z);
 }
 
 // ---------------------------------------------------------------------------

@@ -156,7 +156,9 @@ def test_refusals_of_tensors(gv):
 
 SHAPES = [(1, 1, 1, 0, 0), (1, 512, 2048, 0, 0), (3, 77, 19, 1, 1), (16, 4096, 100, 0, 0), (17, 130, 33, 3, 1), (33, 1001, 65, 0, 0), (64, 357, 500, 2, 0),
           (65, 357, 501, 0, 0), (100, 64, 64, 8, 0), (257, 40, 300, 1, 1), (1021, 357, 500, 0, 0), (2, 16384, 3, 0, 0), (130, 5, 16384, 0, 0),
-          (300, 8200, 130, 0, 0), (2048, 256, 1100, 0, 0), (4100, 33, 4100, 0, 0)]
+          (300, 8200, 130, 0, 0), (2048, 256, 1100, 0, 0), (4100, 33, 4100, 0, 0),
+          # whole pieces, in all kinds of whole and broken steps, with few and many tiles
+          (4104, 520, 1032, 0, 0), (8200, 72, 2056, 0, 0), (1000, 2056, 2048, 8, 8), (3000, 136, 3000, 0, 0), (4100, 200, 4104, 24, 0), (70, 8, 16384, 0, 0)]
 
 
 @gpu
