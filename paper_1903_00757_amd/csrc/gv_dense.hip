@@ -274,21 +274,22 @@ typedef __attribute__((address_space(3))) void LdsAny;
 constexpr uint32_t kWide = 64;                 // k's of a step
 constexpr uint64_t kWideStride = 1ull << 21;   // a tile's rows lie within 2^31 bytes
 
-// kSpread: of B.  The matrix instruction's row 4 g + r of tile j of a wave's 64 rows of B is row 16 g + 4 j + r of them, so that the lanes of
-// group g end with 16 columns of the result in a row, which four of them write as a whole line.
+// kSpread: row 4 g + r of tile j of the matrix instruction is row 16 g + 4 j + r of 64 rows, and tiles 4 to 7 are of the next 64.  For B that
+// leaves the lanes of group g with 16 columns of the result in a row, which four of them write as a whole line; operands that
+// are turned are read at fewer different addresses.
 template <int kTile, bool kAlong, bool kSpread>
 struct Operand {
-    static constexpr uint32_t kThreads = 2 * kTile, kLoads = kTile * 128 / 16 / kThreads, kUnits = kTile / 16;
+    static constexpr uint32_t kThreads = 2 * kTile, kLoads = kTile * 128 / 16 / kThreads;
     static constexpr uint32_t kLine = kAlong ? 8 : kTile / 8;  // pieces
     static constexpr uint32_t kRows = kThreads / kLine;        // that the workgroup loads at once
     const char *at, *end;  // the tile's first value of the next step, and of the matrix behind its last
     uint64_t step, rows;   // bytes to the next step, and to the next rows
-    uint32_t from[2];      // of this lane in the first rows and in the second (the third's are the first's), in bytes
+    uint32_t from;         // of this lane in the first rows (and in the others likewise), in bytes
     // A piece's place: along k rows of 128 bytes, piece p of row r at p ^ turn(r); otherwise rows of kTile values of one k, piece p of
     // row k at p ^ turn(k): what lanes read together lies in different banks.
     static __device__ __forceinline__ uint32_t turn(uint32_t row) {
         if constexpr (kAlong) return kSpread ? (row & 3) | (row >> 4 & 1) << 2 : row & 7;
-        else return kSpread ? (row & 1) | (row >> 1 & 1) << 3 : 2 * (((row & 3) | (row >> 3 & 3) << 2) & (kUnits - 1));
+        else return (row & 1) | (row >> 1 & 1) << 3;
     }
     // value k (and first row) of a matrix of `lines` lines of `length` values
     __device__ __forceinline__ void begin(const void *p, uint64_t stride, uint64_t lines, uint64_t length, uint32_t first, uint32_t k) {
@@ -296,11 +297,7 @@ struct Operand {
         end = (const char *)p + 2 * ((lines - 1) * stride + length);
         step = kAlong ? 2 * kWide : 2 * kWide * stride;
         rows = 2 * kRows * stride;
-#pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) {
-            const uint32_t id = j * kThreads + threadIdx.x, row = threadIdx.x / kLine;
-            from[j] = 2 * (row * (uint32_t)stride + (id % kLine ^ turn(id / kLine)) * 8);
-        }
+        from = 2 * (threadIdx.x / kLine * (uint32_t)stride + (threadIdx.x % kLine ^ turn(threadIdx.x / kLine)) * 8);
     }
     // Asks for the next step.  Nothing is read behind the matrix's end; what lies behind its rows and columns is not used.
     __device__ __forceinline__ void fetch(char *tile) {
@@ -310,7 +307,7 @@ struct Operand {
         for (uint32_t j = 0; j < kLoads; ++j, p += rows) {
             const uint32_t bytes = p < end ? (uint32_t)std::min<uint64_t>(end - p, 0xFFFFFFFFu) : 0;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000),
-                                                     (LdsAny *)(tile + (j * kThreads + wave) * 16), 16, from[j % 2], 0, 0, 0);
+                                                     (LdsAny *)(tile + (j * kThreads + wave) * 16), 16, from, 0, 0, 0);
         }
         at += step;
     }
@@ -322,7 +319,7 @@ struct Operand {
             const uint32_t id = j * kThreads + threadIdx.x;
             const uint32_t k = kAlong ? (id % kLine ^ turn(id / kLine)) * 8 : id / kLine;
             uint4 v = {};
-            if (k < left && p + from[j % 2] < end) __builtin_memcpy(&v, p + from[j % 2], 16);  // whole pieces: 8 k's of a row, or 8 rows of a k
+            if (k < left && p + from < end) __builtin_memcpy(&v, p + from, 16);  // whole pieces: 8 k's of a row, or 8 rows of a k
             *(uint4 *)(tile + id * 16) = v;
         }
     }
@@ -340,8 +337,8 @@ struct Reader {
             base = row * 128 + (group ^ Of::turn(row)) * 16;
         } else {
             // lanes point to four rows of one k each, and get four k's of one row
-            const uint32_t k = 8 * group + at / 4, piece = kSpread ? row / 8 + at % 4 * 2 : row / 8 + at % 4 / 2;
-            base = k * (2 * kTile) + (piece ^ Of::turn(k)) * 16 + (kSpread ? 0 : at % 2 * 8);
+            const uint32_t k = 8 * group + at / 4;
+            base = k * (2 * kTile) + ((row / 8 + at % 4 * 2) ^ Of::turn(k)) * 16;
         }
     }
     __device__ __forceinline__ uint4 read(const char *tile, int half, int i) const {
@@ -349,7 +346,8 @@ struct Reader {
             // turn() of rows that are 16 apart is the same; of rows 4 i apart as well
             return *(const uint4 *)(tile + (base ^ 64 * half) + (kSpread ? 512 : 2048) * i);
         } else {
-            const char *at = tile + (kSpread ? (base ^ 16 * (i / 2)) + 8 * (i % 2) : base ^ 32 * i) + half * (32 * 2 * kTile);
+            static_assert(kSpread, "what is turned is spread");
+            const char *at = tile + (base ^ (16 * (i % 4 / 2) + 128 * (i / 4))) + 8 * (i % 2) + half * (32 * 2 * kTile);
             const s4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsFour *)at);
             const s4v high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsFour *)(at + 8 * kTile));
             const uint2 x = __builtin_bit_cast(uint2, low), y = __builtin_bit_cast(uint2, high);
@@ -377,7 +375,7 @@ __global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint
     for (int i = 0; i < kMs; ++i)
 #pragma unroll
         for (int j = 0; j < kNs; ++j) sums[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    Operand<kTile, kAAlong, false> of_a;
+    Operand<kTile, kAAlong, !kAAlong> of_a;
     Operand<kTile, kBAlong, true> of_b;
     of_a.begin(a.x, a.x_stride, kAAlong ? a.rows : a.cols, kAAlong ? a.cols : a.rows, m0, k_first);
     of_b.begin(a.weight, a.weight_stride, kBAlong ? a.outs : a.cols, kBAlong ? a.cols : a.outs, n0, k_first);
@@ -395,7 +393,7 @@ __global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint
         __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
     };
-    Reader<kTile, kAAlong, false> read_a;
+    Reader<kTile, kAAlong, !kAAlong> read_a;
     Reader<kTile, kBAlong, true> read_b;
     read_a.begin(wm);
     read_b.begin(wn);
@@ -452,7 +450,8 @@ __global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint
             float z[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) z[c] = sums[i][2 * h + c / 4][c % 4];
-            finish<T>(a, m0 + wm + 16 * i + lane % 16, n0 + wn + 16 * (lane / 16) + 8 * h, split, z);
+            const uint32_t m = kAAlong ? 16 * i + lane % 16 : 64 * (i / 4) + 4 * (i % 4) + lane % 16 / 4 * 16 + lane % 4;
+            finish<T>(a, m0 + wm + m, n0 + wn + 16 * (lane / 16) + 8 * h, split, z);
         }
 }
 
@@ -589,7 +588,7 @@ Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type) {
     const auto tiles = [&](uint64_t t) { return ((rows + t - 1) / t) * ((outs + t - 1) / t); };
     const uint64_t tile = tiles(256) >= kWanted ? 256 : tiles(128) * std::min<uint64_t>(steps / 8 + 1, 8) >= kWanted ? 128 : 64;
     const uint64_t all = std::max<uint64_t>(1, tiles(tile));
-    uint64_t splits = std::max<uint64_t>(1, std::min<uint64_t>((2 * kWanted) / all, steps / 8));
+    uint64_t splits = all >= kWanted ? 1 : std::max<uint64_t>(1, std::min<uint64_t>((2 * kWanted) / all, steps / 8));
     const uint64_t each = std::max<uint64_t>(1, (steps + splits - 1) / splits);
     splits = std::max<uint64_t>(1, (steps + each - 1) / each);
     return {(uint32_t)tile, (uint32_t)((rows + tile - 1) / tile), (uint32_t)((outs + tile - 1) / tile), (uint32_t)splits, (uint32_t)(each * step)};
