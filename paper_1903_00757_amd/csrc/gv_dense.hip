@@ -10,6 +10,7 @@
 #include "gvhot.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #pragma clang fp contract(off)
@@ -143,7 +144,7 @@ __device__ __forceinline__ void finish(const DenseArgs &a, uint32_t m, uint32_t 
 }
 
 // ---------------------------------------------------------------------------
-// Tiles of kTile x kTile, 2 kTile threads: eight, four or two waves side by side.  The next step's values are loaded into registers while this
+// Tiles of kTile x kTile, 2 kTile threads: eight or four waves side by side.  The next step's values are loaded into registers while this
 // step's are multiplied, and go to the other half of LDS.
 constexpr int kStep = 128;  // bytes of k
 
@@ -260,6 +261,106 @@ __global__ __launch_bounds__(2 * kTile) void k_product(DenseArgs a, uint32_t til
             float z[4] = {sums[i][j][0], sums[i][j][1], sums[i][j][2], sums[i][j][3]};
             finish<T>(a, m0 + wm + 16 * i + lane % 16, n0 + wn + 16 * j + 4 * (lane / 16), split, z);
         }
+}
+
+// ---------------------------------------------------------------------------
+// Small products, of any type and alignment: tiles of 32 x 64, four waves with 16 x 32 of it each, so that there are many workgroups, and
+// values asked for three steps ahead, since a step's products take a quarter of what its loads take.
+constexpr int kSmallM = 32, kSmallN = 64, kSmallThreads = 256, kSmallAhead = 3;
+
+template <class T, int kRows, bool kAlong>
+struct SmallShare {
+    static constexpr int N = kEach<T>, kPieces = kRows * 8 / kSmallThreads;
+    Values<T, N> pieces[kPieces];
+    // k's k .. k + 8 N - 1, of which `left` are there (kWhole: all)
+    template <bool kWhole>
+    __device__ __forceinline__ void load(const T *p, uint64_t stride, uint32_t first, uint32_t rows, uint32_t k, uint32_t left) {
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) {
+            const uint32_t id = q * kSmallThreads + threadIdx.x;
+            if constexpr (kAlong) {
+                const uint32_t row = std::min(first + id / 8, rows - 1), at = id % 8 * N;  // rows past the end are not used
+                const T *from = p + row * stride + k + at;
+                if constexpr (kWhole) __builtin_memcpy(&pieces[q], from, 16);
+                else pieces[q].load(from, left_of(at, left));
+            } else {
+                const uint32_t row = std::min(first + id % kRows, rows - 1), at = id / kRows * N;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const uint32_t to = kWhole ? at + i : std::min(at + i, left - 1);
+                    const T v = p[(uint64_t)(k + to) * stride + row];
+                    pieces[q].at[i] = kWhole || at + i < left ? v : (T)0.0f;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void put(char *tile) const {
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) {
+            const uint32_t id = q * kSmallThreads + threadIdx.x, row = kAlong ? id / 8 : id % kRows, piece = kAlong ? id % 8 : id / kRows;
+            *(uint4 *)(tile + row * kStep + (piece ^ (row & 7)) * 16) = __builtin_bit_cast(uint4, pieces[q]);
+        }
+    }
+};
+
+template <class T, bool kAAlong, bool kBAlong>
+__global__ __launch_bounds__(kSmallThreads) void k_product_small(DenseArgs a, uint32_t tiles_m, uint32_t tiles_n) {
+    constexpr uint32_t kCount = kStep / sizeof(T);
+    __shared__ __attribute__((aligned(16))) char tiles[2][(kSmallM + kSmallN) * kStep];
+    const uint32_t all = tiles_m * tiles_n, split = blockIdx.x / all, id = blockIdx.x % all;
+    const uint32_t m0 = id / tiles_n * kSmallM, n0 = id % tiles_n * kSmallN;
+    const uint32_t k_first = split * a.split_k, k_last = std::min<uint64_t>(a.cols, (uint64_t)k_first + a.split_k);
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, wm = wave % 2 * 16, wn = wave / 2 * 32;
+    f4 sums[2] = {};
+    SmallShare<T, kSmallM, kAAlong> of_a[kSmallAhead];
+    SmallShare<T, kSmallN, kBAlong> of_b[kSmallAhead];
+    const T *pa = (const T *)a.x, *pb = (const T *)a.weight;
+    const auto load = [&](auto stage, uint32_t k) {
+        constexpr int kStage = decltype(stage)::value;
+        if (k + kCount <= k_last) {
+            of_a[kStage].template load<true>(pa, a.x_stride, m0, a.rows, k, kCount);
+            of_b[kStage].template load<true>(pb, a.weight_stride, n0, a.outs, k, kCount);
+        } else if (k < k_last) {
+            of_a[kStage].template load<false>(pa, a.x_stride, m0, a.rows, k, k_last - k);
+            of_b[kStage].template load<false>(pb, a.weight_stride, n0, a.outs, k, k_last - k);
+        }
+    };
+    uint32_t half = 0;
+    const auto step = [&](auto stage, uint32_t k) {
+        constexpr int kStage = decltype(stage)::value;
+        char *tile = tiles[half];
+        of_a[kStage].put(tile);
+        of_b[kStage].put(tile + kSmallM * kStep);
+        load(stage, k + kSmallAhead * kCount);
+        __syncthreads();  // one a step: the other half is written next, and was read before this
+#pragma unroll
+        for (uint32_t p = 0; p < 8; p += 4) {
+            const uint32_t at = ((p + lane / 16) ^ (lane & 7)) * 16;
+            const uint4 ma = *(const uint4 *)(tile + (wm + lane % 16) * kStep + at);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                multiply(*(const uint4 *)(tile + (kSmallM + wn + 16 * j + lane % 16) * kStep + at), ma, sums[j], (T *)nullptr);
+        }
+        half ^= 1;
+    };
+    constexpr std::integral_constant<int, 0> kFirst;
+    constexpr std::integral_constant<int, 1> kSecond;
+    constexpr std::integral_constant<int, 2> kThird;
+    load(kFirst, k_first);
+    load(kSecond, k_first + kCount);
+    load(kThird, k_first + 2 * kCount);
+    for (uint32_t k = k_first; k < k_last; k += 3 * kCount) {
+        step(kFirst, k);
+        if (k + kCount >= k_last) break;
+        step(kSecond, k + kCount);
+        if (k + 2 * kCount >= k_last) break;
+        step(kThird, k + 2 * kCount);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        float z[4] = {sums[j][0], sums[j][1], sums[j][2], sums[j][3]};
+        finish<T>(a, m0 + wm + lane % 16, n0 + wn + 16 * j + 4 * (lane / 16), split, z);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -576,46 +677,68 @@ hipError_t by_type(int type, Run &&run) {
     return run((_Float16 *)nullptr);
 }
 
-// How a product of rows x outs over `cols` k's is cut.
+// How a product of rows x outs over `cols` k's is cut: the way that is the shortest by what steps were measured to take.  Larger tiles ask
+// for fewer values (8192 x 4096 x 4096 in bfloat16: 214 us by tiles of 256, 256 by 128; 65536 x 512 x 2048 202, 227 and 413 by the small
+// ones), smaller ones are more workgroups (1000 x 1000 x 1000: 32, 22 and 10 us), and a long k is cut where there are few (a weight's
+// gradient of 65536 x 128 x 512: 50 us in 64 parts of 128 tiles, 203 in 8).
 struct Cut {
     uint32_t tile, tiles_m, tiles_n, splits, split_k;
 };
 constexpr uint32_t kFewRows = 64;
 
-Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type) {
-    constexpr uint64_t kWanted = 256;
-    const uint64_t step = kStep / (type == GV_F32 ? 4 : 2), steps = (cols + step - 1) / step;
-    const auto tiles = [&](uint64_t t) { return ((rows + t - 1) / t) * ((outs + t - 1) / t); };
-    const uint64_t tile = tiles(256) >= kWanted ? 256 : tiles(128) * std::min<uint64_t>(steps / 8 + 1, 8) >= kWanted ? 128 : 64;
-    const uint64_t all = std::max<uint64_t>(1, tiles(tile));
-    uint64_t splits = all >= kWanted ? 1 : std::max<uint64_t>(1, std::min<uint64_t>((2 * kWanted) / all, steps / 8));
-    const uint64_t each = std::max<uint64_t>(1, (steps + splits - 1) / splits);
-    splits = std::max<uint64_t>(1, (steps + each - 1) / each);
-    return {(uint32_t)tile, (uint32_t)((rows + tile - 1) / tile), (uint32_t)((outs + tile - 1) / tile), (uint32_t)splits, (uint32_t)(each * step)};
+Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide) {
+    const uint64_t step = kStep / (type == GV_F32 ? 4 : 2), steps = std::max<uint64_t>(1, (cols + step - 1) / step);
+    // tiles, workgroups that run at once, and what a step of theirs takes then, in microseconds
+    struct Way {
+        uint32_t m, n;
+        double at_once, each;
+    };
+    const bool f32 = type == GV_F32;
+    const Way ways[3] = {{256, 256, 256, f32 ? 7.5 : wide ? 2.1 : 5.0}, {128, 128, 512, f32 ? 4.0 : wide ? 1.2 : 2.6}, {kSmallM, kSmallN, 1024, f32 ? 1.0 : 0.8}};
+    Cut best{};
+    double least = 1e300;
+    for (const Way &w : ways) {
+        const uint64_t m = (rows + w.m - 1) / w.m, n = (outs + w.n - 1) / w.n;
+        for (uint64_t splits = 1; splits <= 64 && (splits == 1 || steps >= 4 * splits); splits *= 2) {
+            const uint64_t each = (steps + splits - 1) / splits, cut = (steps + each - 1) / each;
+            const double rounds = (double)(m * n * cut) / w.at_once, alone = 0.3 + 0.7 * std::min(1.0, rounds);
+            const double time = std::ceil(rounds) * ((double)each * w.each * alone + 3.0) + (cut > 1 ? 4.0 + (double)(cut * rows * outs) * 2e-6 : 0.0);
+            if (time < least) {
+                least = time;
+                best = {w.m, (uint32_t)m, (uint32_t)n, (uint32_t)cut, (uint32_t)(each * step)};
+            }
+        }
+    }
+    return best;
 }
 uint64_t partial_of(const Cut &c, uint64_t rows, uint64_t outs) { return c.splits > 1 ? 4ull * c.splits * rows * outs : 0; }
+
+// with what an alignment may ask for
+uint64_t most_partial_of(uint64_t rows, uint64_t cols, uint64_t outs, int type) {
+    const uint64_t some = partial_of(cut_of(rows, cols, outs, type, false), rows, outs);
+    return type == GV_F32 ? some : std::max(some, partial_of(cut_of(rows, cols, outs, type, true), rows, outs));
+}
 
 template <class T, bool kAAlong, bool kBAlong>
 hipError_t product(DenseArgs a, void *workspace, hipStream_t stream) {
     if (a.rows == 0 || a.outs == 0) return hipSuccess;
-    const Cut c = cut_of(a.rows, a.cols, a.outs, a.type);
+    const auto whole = [](const void *p, uint64_t stride, uint64_t together) {
+        return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && together % 8 == 0 && together > 0 && stride < kWideStride;
+    };
+    const bool wide = sizeof(T) == 2 && whole(a.x, a.x_stride, kAAlong ? a.cols : a.rows) && whole(a.weight, a.weight_stride, kBAlong ? a.cols : a.outs);
+    const Cut c = cut_of(a.rows, a.cols, a.outs, a.type, wide);
     a.split_k = c.split_k;
     a.partial = c.splits > 1 ? (float *)workspace : nullptr;
     const uint32_t blocks = c.tiles_m * c.tiles_n * c.splits;
-    bool wide = false;
+    const auto run = [&](auto kernel, uint32_t threads) { return launch(kernel, blocks, threads, 0, stream, a, c.tiles_m, c.tiles_n); };
     hipError_t e = hipSuccess;
-    if constexpr (sizeof(T) == 2) {
-        const auto whole = [](const void *p, uint64_t stride, uint64_t together) {
-            return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && together % 8 == 0 && together > 0 && stride < kWideStride;
-        };
-        wide = c.tile >= 128 && whole(a.x, a.x_stride, kAAlong ? a.cols : a.rows) && whole(a.weight, a.weight_stride, kBAlong ? a.cols : a.outs);
-        if (wide)
-            e = c.tile == 256 ? launch(k_product_wide<T, 256, kAAlong, kBAlong>, blocks, 512, 0, stream, a, c.tiles_m, c.tiles_n)
-                              : launch(k_product_wide<T, 128, kAAlong, kBAlong>, blocks, 256, 0, stream, a, c.tiles_m, c.tiles_n);
+    if (c.tile == kSmallM) {
+        e = run(k_product_small<T, kAAlong, kBAlong>, kSmallThreads);
+    } else if (!wide) {
+        e = c.tile == 256 ? run(k_product<T, 256, kAAlong, kBAlong>, 512) : run(k_product<T, 128, kAAlong, kBAlong>, 256);
+    } else if constexpr (sizeof(T) == 2) {
+        e = c.tile == 256 ? run(k_product_wide<T, 256, kAAlong, kBAlong>, 512) : run(k_product_wide<T, 128, kAAlong, kBAlong>, 256);
     }
-    if (!wide) e = c.tile == 256   ? launch(k_product<T, 256, kAAlong, kBAlong>, blocks, 512, 0, stream, a, c.tiles_m, c.tiles_n)
-                         : c.tile == 128 ? launch(k_product<T, 128, kAAlong, kBAlong>, blocks, 256, 0, stream, a, c.tiles_m, c.tiles_n)
-                                         : launch(k_product<T, 64, kAAlong, kBAlong>, blocks, 128, 0, stream, a, c.tiles_m, c.tiles_n);
     if (e != hipSuccess || c.splits == 1) return e;
     const uint64_t pieces = (uint64_t)a.rows * ((a.outs + 3) / 4);
     return launch(k_join_product<T>, (uint32_t)std::min<uint64_t>((pieces + 255) / 256, 1 << 16), 256, 0, stream, a, c.splits);
@@ -639,8 +762,8 @@ GradPlan grad_plan_of(uint64_t rows, uint32_t cols, uint32_t outs, int type, int
     };
     p.gz = take(act != GV_ACT_NONE && (want_x || want_weight) ? rows * outs * (type == GV_F32 ? 4 : 2) : 0);
     p.bias = take(want_bias ? 4ull * p.chunks * outs : 0);
-    p.product = take(std::max(want_x ? partial_of(cut_of(rows, outs, cols, type), rows, cols) : 0,
-                              want_weight ? partial_of(cut_of(outs, rows, cols, type), outs, cols) : 0));
+    p.product = take(std::max(want_x ? most_partial_of(rows, outs, cols, type) : 0,
+                              want_weight ? most_partial_of(outs, rows, cols, type) : 0));
     p.bytes = at;
     return p;
 }
@@ -648,7 +771,7 @@ GradPlan grad_plan_of(uint64_t rows, uint32_t cols, uint32_t outs, int type, int
 }  // namespace
 
 uint64_t dense_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type) {
-    return rows <= kFewRows ? 0 : partial_of(cut_of(rows, cols, outs, type), rows, outs);
+    return rows <= kFewRows ? 0 : most_partial_of(rows, cols, outs, type);
 }
 
 hipError_t launch_dense(const DenseArgs &a, void *workspace, hipStream_t stream) {
