@@ -21,7 +21,7 @@
 namespace gv {
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64, kEach = 16;
+constexpr int kThreads = 512, kWaves = kThreads / 64, kEach = 32, kPieces = kEach / 8;
 constexpr uint32_t kTile = kThreads * kEach, kSlots = 2048;  // scores of a turn; candidates that LDS has room for
 constexpr float kLowest = -3.402823466e38f;
 static_assert(GV_MAX_BEST <= kSlots / 2, "room for the best and as many");
@@ -51,15 +51,15 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 }
 __device__ __forceinline__ float next_above(float x) { return value_of(ordered(x) + 1); }  // NaN, which nothing reaches, above infinity
 
-// The k-th largest of the 64 lanes' numbers (1 <= k <= 64).
-__device__ __forceinline__ uint32_t kth_of_lanes(uint32_t x, uint32_t k) {
-    uint32_t found = 0;
+// The k-th and the l-th largest of the 64 lanes' numbers (at least 1; 0 for more than 64).
+__device__ __forceinline__ void some_of_lanes(uint32_t x, uint32_t k, uint32_t l, uint32_t &kth, uint32_t &lth) {
+    kth = lth = 0;
 #pragma unroll
     for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t to = found | 1u << bit;
-        if ((uint32_t)__popcll(__ballot(x >= to)) >= k) found = to;
+        const uint32_t a = kth | 1u << bit, b = lth | 1u << bit;
+        if ((uint32_t)__popcll(__ballot(x >= a)) >= k) kth = a;
+        if ((uint32_t)__popcll(__ballot(x >= b)) >= l) lth = b;
     }
-    return found;
 }
 
 // A bound that `best` of a workgroup's numbers reach, one from each thread: by every wave's ceil(best / waves)-th, or by the
@@ -68,7 +68,8 @@ template <int kOf>
 __device__ __forceinline__ uint32_t bound_of_threads(uint32_t x, uint32_t best, uint32_t (*scratch)[kOf]) {
     const uint32_t wave = threadIdx.x / 64, each = (best + kOf - 1) / kOf;
     if (each > 64) return 0;
-    const uint32_t spread = kth_of_lanes(x, each), alone = best <= 64 ? kth_of_lanes(x, best) : 0;
+    uint32_t spread, alone;
+    some_of_lanes(x, each, best, spread, alone);
     if (threadIdx.x % 64 == 0) scratch[0][wave] = spread, scratch[1][wave] = alone;
     __syncthreads();
     uint32_t least = 0xFFFFFFFFu, most = 0;
@@ -113,11 +114,28 @@ struct Shared {
 
 __device__ __forceinline__ uint64_t key_of(float score, uint32_t row) { return (uint64_t)ordered(score) << 32 | (0xFFFFFFFFu - row); }
 
-// Leaves the `best` first of what is kept (n of it) and of the scores v of this turn that reach `least`; returns the last one's score.
-// There are at least `best` of them.
-__device__ __noinline__ float narrow(Shared &s, uint32_t n, uint32_t best, const float (&v)[kEach], float least, uint32_t row) {
+// This thread's scores of a turn from row `first` on; what is not there, and NaN, as -inf.
+template <class T>
+__device__ __forceinline__ void load_turn(const T *scores, uint32_t first, uint32_t end, float (&v)[kEach]) {
+    const uint32_t row = first + 8 * threadIdx.x;  // and so on in every quarter of the turn
+    Piece<T> p[kPieces];
+    if (first + kTile <= end) {
+#pragma unroll
+        for (int h = 0; h < kPieces; ++h) __builtin_memcpy(&p[h], scores + row + h * (kTile / kPieces), sizeof p[h]);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] = fmaxf((float)p[i / 8].at[i % 8], -infinity());
+    } else {
+#pragma unroll
+        for (int h = 0; h < kPieces; ++h) p[h].load(scores, row + h * (kTile / kPieces), end);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            v[i] = row + (i / 8) * (kTile / kPieces) + i % 8 < end ? fmaxf((float)p[i / 8].at[i % 8], -infinity()) : -infinity();
+    }
+}
+
+// Leaves the `best` first of the n kept (at least as many); returns the last one's score.
+__device__ __forceinline__ float narrow(Shared &s, uint32_t n, uint32_t best) {
     constexpr int kOwn = kSlots / kThreads;
-    const auto row_of = [&](int i) { return row + (i / 8) * (kTile / 2) + i % 8; };
     uint64_t own[kOwn];
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
@@ -125,15 +143,12 @@ __device__ __noinline__ float narrow(Shared &s, uint32_t n, uint32_t best, const
         own[i] = at < n ? key_of(s.kept[at].score, s.kept[at].row) : 0;
     }
     uint64_t found = 0;
+#pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
         const uint64_t to = found | 1ull << bit;
         uint32_t reach = 0;
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) reach += own[i] >= to;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) reach += v[i] >= least && key_of(v[i], row_of(i)) >= to;
-#pragma unroll
-        for (int d = 32; d > 0; d /= 2) reach += __shfl_xor(reach, d);
+        for (int i = 0; i < kOwn; ++i) reach += (uint32_t)__popcll(__ballot(own[i] >= to));
         uint32_t *waves = s.waves[bit % 2];
         if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = reach;
         __syncthreads();
@@ -145,16 +160,40 @@ __device__ __noinline__ float narrow(Shared &s, uint32_t n, uint32_t best, const
     __syncthreads();
     if (threadIdx.x == 0) s.count = 0;
     __syncthreads();
-    const auto keep = [&](uint64_t key) { s.kept[atomicAdd(&s.count, 1u)] = {value_of((uint32_t)(key >> 32)), 0xFFFFFFFFu - (uint32_t)key}; };
 #pragma unroll
     for (int i = 0; i < kOwn; ++i)
-        if (own[i] >= found) keep(own[i]);
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-        if (v[i] >= least && key_of(v[i], row_of(i)) >= found) keep(key_of(v[i], row_of(i)));
+        if (own[i] >= found) s.kept[atomicAdd(&s.count, 1u)] = {value_of((uint32_t)(own[i] >> 32)), 0xFFFFFFFFu - (uint32_t)own[i]};
     __syncthreads();
     return value_of((uint32_t)(found >> 32));
 }
+
+// A turn with more candidates than there is room for: `kept` of the turns before, and the turn's scores that reach `least`, two of each thread at
+// a time, narrowed whenever the next may not fit.  Returns how many are kept; `bound` is raised to what `best` of them reach.
+template <class T>
+__device__ __forceinline__ uint32_t take_slowly(Shared &s, uint32_t kept, uint32_t best, const T *scores, uint32_t first, uint32_t end, float least,
+                                                float &bound) {
+    if (threadIdx.x == 0) s.count = kept;
+    __syncthreads();
+#pragma unroll 1
+    for (int i = kEach - 2; i >= 0; i -= 2) {  // the last first: scores that rise are done with soonest
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+            const uint32_t row = first + 8 * threadIdx.x + i / 8 * (kTile / kPieces) + i % 8 + o;
+            const float x = row < end ? (float)scores[row] : -infinity();
+            if (x >= least) s.kept[atomicAdd(&s.count, 1u)] = {x, row};
+        }
+        __syncthreads();
+        kept = s.count;
+        __syncthreads();
+        if (kept + 2 * kThreads > kSlots) {
+            bound = std::max(bound, narrow(s, kept, best));
+            least = std::max(least, bound);
+            kept = best;
+        }
+    }
+    return kept;
+}
+static_assert(GV_MAX_BEST + 2 * kThreads <= kSlots, "narrowed, the next fit");
 
 __device__ __forceinline__ bool offers(const SelectArgs &a, uint64_t beam, float &total) {
     total = a.totals ? a.totals[beam] : 0.0f;
@@ -178,7 +217,7 @@ __device__ __forceinline__ void put(const SelectArgs &a, uint64_t group, uint32_
 
 // One part of one beam.  kAlone: groups of one beam in one part are finished here.
 template <class T, bool kLog, bool kAlone>
-__global__ __launch_bounds__(kThreads) void k_select_parts(SelectArgs a) {
+__global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
     __shared__ Shared s;
     const uint64_t beam = blockIdx.x / a.parts;
     const uint32_t part = blockIdx.x % a.parts, tid = threadIdx.x;
@@ -205,19 +244,9 @@ __global__ __launch_bounds__(kThreads) void k_select_parts(SelectArgs a) {
     double sum = 0.0;
     uint32_t kept = 0, turn = 0;
     for (uint64_t first = begin; first < end; first += kTile, ++turn) {
-        const uint32_t row = (uint32_t)first + 8 * tid;  // and half a turn on
+        const uint32_t row = (uint32_t)first + 8 * tid;  // and so on in every quarter of the turn
         float v[kEach];
-        {
-            Piece<T> p[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) p[h].load(scores, row + h * (kTile / 2), end);
-            const bool whole = first + kTile <= end;
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const float x = (float)p[i / 8].at[i % 8];
-                v[i] = (whole || row + (i / 8) * (kTile / 2) + i % 8 < end) && x == x ? x : -infinity();
-            }
-        }
+        load_turn(scores, (uint32_t)first, end, v);
         float most = v[0];
 #pragma unroll
         for (int i = 1; i < kEach; ++i) most = fmaxf(most, v[i]);
@@ -229,23 +258,19 @@ __global__ __launch_bounds__(kThreads) void k_select_parts(SelectArgs a) {
                     top = most;
                 }
             }
-            float terms[kEach];
+            float terms[4] = {};
             if (top < infinity()) {
                 const float from = top == -infinity() ? 0.0f : top;
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) terms[i] = __expf(v[i] - from);
+                for (int i = 0; i < kEach; ++i) terms[i % 4] += __expf(v[i] - from);
             } else {  // scores of infinity share everything
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) terms[i] = v[i] == infinity() ? 1.0f : 0.0f;
+                for (int i = 0; i < kEach; ++i) terms[i % 4] += v[i] == infinity() ? 1.0f : 0.0f;
             }
-#pragma unroll
-            for (int d = kEach / 2; d > 0; d /= 2)
-#pragma unroll
-                for (int i = 0; i < d; ++i) terms[i] += terms[i + d];
-            sum += (double)terms[0];
+            sum += (double)((terms[0] + terms[1]) + (terms[2] + terms[3]));
         }
         largest = fmaxf(largest, most);
-        if ((turn & (turn + 1)) == 0) {  // turns 0, 1, 3, 7, ...
+        if ((turn & (turn + 1)) == 0 || first + kTile >= end) {  // turns 0, 1, 3, 7, ..., and the last
             const uint32_t found = bound_of_threads<kWaves>(ordered(largest), a.best, s.waves);
             if (found > ordered(-infinity()) && value_of(found) > bound) {
                 // scores that are kept may lie below it; of those in later turns, equal ones come behind
@@ -259,13 +284,12 @@ __global__ __launch_bounds__(kThreads) void k_select_parts(SelectArgs a) {
             for (int i = 0; i < kEach; ++i) {
                 if (v[i] < least) continue;
                 const uint32_t at = atomicAdd(&s.count, 1u);
-                if (at < kSlots) s.kept[at] = {v[i], row + (i / 8) * (kTile / 2) + i % 8};
+                if (at < kSlots) s.kept[at] = {v[i], row + (i / 8) * (kTile / kPieces) + i % 8};
                 else full = true;
             }
         }
         if (__syncthreads_or(full)) {
-            bound = narrow(s, kept, a.best, v, least, row);
-            kept = a.best;
+            kept = take_slowly(s, kept, a.best, scores, (uint32_t)first, end, least, bound);
         } else {
             kept = s.count;
         }
@@ -281,10 +305,9 @@ __global__ __launch_bounds__(kThreads) void k_select_parts(SelectArgs a) {
                             : top == all_top ? sum : sum * exp((double)top - (double)all_top);
         log_sum = block_sum<kWaves>(mine, s.sums);
     }
-    const float none[kEach] = {};
     const uint32_t most_kept = kAlone ? kSlots : a.slots;
     if (kept > most_kept) {
-        bound = narrow(s, kept, a.best, none, infinity(), 0);
+        bound = narrow(s, kept, a.best);
         kept = a.best;
     }
     if constexpr (kAlone) {
@@ -301,9 +324,16 @@ __global__ __launch_bounds__(kThreads) void k_select_parts(SelectArgs a) {
         }
         for (uint32_t r = kept + tid; r < a.best; r += kThreads) put_none(a, beam, r);
     } else {
-        if (tid == 0) *to = Part{log_sum, all_top, bound, kept, 0};
         Candidate *out = (Candidate *)a.candidates + (beam * a.parts + part) * a.slots;
-        for (uint32_t i = tid; i < kept; i += kThreads) out[i] = s.kept[i];
+        __syncthreads();
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        for (uint32_t i = tid; i < kept; i += kThreads) {
+            const Candidate c = s.kept[i];
+            if (c.score >= bound) out[atomicAdd(&s.count, 1u)] = c;  // some were kept before the bound rose
+        }
+        __syncthreads();
+        if (tid == 0) *to = Part{log_sum, all_top, bound, s.count, 0};
     }
 }
 
@@ -322,16 +352,24 @@ struct JoinShared {
     uint32_t count, waves[2][kJoinWaves];
 };
 
-// Whether candidate i goes before candidate j: by total, beam, score and row.
-__device__ __forceinline__ bool before(const JoinShared &s, uint32_t i, uint32_t j) {
-    if (s.total[i] != s.total[j]) return s.total[i] > s.total[j];
-    if (s.beam[i] != s.beam[j]) return s.beam[i] < s.beam[j];
-    if (s.score[i] != s.score[j]) return s.score[i] > s.score[j];
-    return s.row[i] < s.row[j];
-}
+// How many of n candidates go before candidate i: by total, beam, score and row.
 __device__ __forceinline__ uint32_t rank_of(const JoinShared &s, uint32_t i, uint32_t n) {
-    uint32_t rank = 0;
-    for (uint32_t j = 0; j < n; ++j) rank += before(s, j, i);
+    const double total = s.total[i];
+    uint32_t rank = 0, equal = 0;
+#pragma unroll 8
+    for (uint32_t j = 0; j < n; ++j) {
+        const double other = s.total[j];
+        rank += other > total;
+        equal += other == total;
+    }
+    if (equal > 1) {
+        const uint32_t beam = s.beam[i], row = s.row[i];
+        const float score = s.score[i];
+        for (uint32_t j = 0; j < n; ++j) {
+            if (s.total[j] != total || j == i) continue;
+            rank += s.beam[j] != beam ? s.beam[j] < beam : s.score[j] != score ? s.score[j] > score : s.row[j] < row;
+        }
+    }
     return rank;
 }
 
@@ -408,11 +446,23 @@ __global__ __launch_bounds__(kJoinThreads) void k_select_join(SelectArgs a) {
         c = candidates[(uint64_t)lo * a.slots + (i - (lo ? s.ends[lo - 1] : 0))];
         return total_of(beam, c.score);
     };
+    // Candidates are read once, as far as registers hold them: four a thread, asked for together.
+    constexpr uint32_t kHeld = 4;
+    double held_total[kHeld];
+    Candidate held[kHeld];
+    uint32_t held_beam[kHeld];
+    double largest = -infinity();
+#pragma unroll
+    for (uint32_t h = 0; h < kHeld; ++h) {
+        held_total[h] = -infinity();
+        if (tid + h * kJoinThreads < all) held_total[h] = take(tid + h * kJoinThreads, held_beam[h], held[h]);
+    }
+#pragma unroll
+    for (uint32_t h = 0; h < kHeld; ++h) largest = fmax(largest, held_total[h]);
     // a bound of the totals, as in a part
     double bound = -infinity();
     if (all > 2 * a.best) {
-        double largest = -infinity();
-        for (uint32_t i = tid; i < all; i += kJoinThreads) {
+        for (uint32_t i = tid + kHeld * kJoinThreads; i < all; i += kJoinThreads) {
             uint32_t beam;
             Candidate c;
             largest = fmax(largest, take(i, beam, c));
@@ -431,7 +481,10 @@ __global__ __launch_bounds__(kJoinThreads) void k_select_join(SelectArgs a) {
     for (uint32_t beam = tid; a.done && beam < a.beams; beam += kJoinThreads)
         if (a.done[first_beam + beam] && s.base[beam] > -infinity() && (double)s.base[beam] >= bound)
             full |= keep((double)s.base[beam], beam, infinity(), a.end);
-    for (uint32_t i = tid; i < all; i += kJoinThreads) {
+#pragma unroll
+    for (uint32_t h = 0; h < kHeld; ++h)
+        if (tid + h * kJoinThreads < all && held_total[h] >= bound) full |= keep(held_total[h], held_beam[h], held[h].score, held[h].row);
+    for (uint32_t i = tid + kHeld * kJoinThreads; i < all; i += kJoinThreads) {
         uint32_t beam;
         Candidate c;
         const double total = take(i, beam, c);
@@ -499,7 +552,6 @@ Cut cut_of(uint64_t queries, uint64_t rows, uint32_t beams, uint32_t best) {
     const uint64_t tiles = std::max<uint64_t>(1, (rows + kTile - 1) / kTile);
     uint64_t parts = std::min<uint64_t>(tiles, std::max<uint64_t>(1, kWanted / queries));
     parts = std::min<uint64_t>(parts, kMostLists / beams);
-    if (beams == 1 && tiles <= 2) parts = 1;
     const uint64_t each = (tiles + parts - 1) / parts;
     parts = (tiles + each - 1) / each;
     return {(uint32_t)parts, (uint32_t)(each * kTile), std::min<uint32_t>(kSlots, 512 + 4 * best), beams == 1 && parts == 1};
