@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kThreads = 512, kWaves = kThreads / 64, kEach = 32, kPieces = kEach / 8;
 constexpr uint32_t kTile = kThreads * kEach, kSlots = 2048;  // scores of a turn; candidates that LDS has room for
+constexpr uint32_t kFewToRank = 256;  // each compared with all others; more are narrowed first
 constexpr float kLowest = -3.402823466e38f;
 static_assert(GV_MAX_BEST <= kSlots / 2, "room for the best and as many");
 
@@ -51,30 +52,41 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 }
 __device__ __forceinline__ float next_above(float x) { return value_of(ordered(x) + 1); }  // NaN, which nothing reaches, above infinity
 
-// The k-th and the l-th largest of the 64 lanes' numbers (at least 1; 0 for more than 64).
-__device__ __forceinline__ void some_of_lanes(uint32_t x, uint32_t k, uint32_t l, uint32_t &kth, uint32_t &lth) {
-    kth = lth = 0;
+// The k-th largest of the kOf numbers of each of the 64 lanes (1 <= k <= 64 kOf).
+template <int kOf>
+__device__ __forceinline__ uint32_t kth_of_lanes(const uint32_t (&x)[kOf], uint32_t k) {
+    uint32_t found = 0;
 #pragma unroll
     for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t a = kth | 1u << bit, b = lth | 1u << bit;
-        if ((uint32_t)__popcll(__ballot(x >= a)) >= k) kth = a;
-        if ((uint32_t)__popcll(__ballot(x >= b)) >= l) lth = b;
+        const uint32_t to = found | 1u << bit;
+        uint32_t reach = 0;
+#pragma unroll
+        for (int i = 0; i < kOf; ++i) reach += (uint32_t)__popcll(__ballot(x[i] >= to));
+        if (reach >= k) found = to;
     }
+    return found;
 }
 
-// A bound that `best` of a workgroup's numbers reach, one from each thread: by every wave's ceil(best / waves)-th, or by the
-// best-th of one wave; 0 where there is none.
-template <int kOf>
-__device__ __forceinline__ uint32_t bound_of_threads(uint32_t x, uint32_t best, uint32_t (*scratch)[kOf]) {
-    const uint32_t wave = threadIdx.x / 64, each = (best + kOf - 1) / kOf;
-    if (each > 64) return 0;
-    uint32_t spread, alone;
-    some_of_lanes(x, each, best, spread, alone);
+// A bound that `best` of a workgroup's numbers reach: by every wave's ceil(best / waves)-th, or by the best-th of one wave.  A few are
+// looked for among the threads' largest, many among all kOf numbers of each.
+template <int kWavesOf, int kOf>
+__device__ __forceinline__ uint32_t bound_of_threads(const uint32_t (&x)[kOf], uint32_t best, uint32_t (*scratch)[kWavesOf]) {
+    const uint32_t wave = threadIdx.x / 64, each = (best + kWavesOf - 1) / kWavesOf;
+    uint32_t spread = 0, alone = 0;
+    if (best <= 64) {
+        uint32_t largest[1] = {x[0]};
+#pragma unroll
+        for (int i = 1; i < kOf; ++i) largest[0] = larger(largest[0], x[i]);
+        spread = kth_of_lanes(largest, each);
+        alone = kth_of_lanes(largest, best);
+    } else if (each <= 64 * kOf) {
+        spread = kth_of_lanes(x, each);
+    }
     if (threadIdx.x % 64 == 0) scratch[0][wave] = spread, scratch[1][wave] = alone;
     __syncthreads();
     uint32_t least = 0xFFFFFFFFu, most = 0;
 #pragma unroll
-    for (int w = 0; w < kOf; ++w) {
+    for (int w = 0; w < kWavesOf; ++w) {
         least = std::min(least, scratch[0][w]);
         most = std::max(most, scratch[1][w]);
     }
@@ -106,11 +118,6 @@ __device__ __forceinline__ uint32_t block_largest(uint32_t x, uint32_t *scratch)
     return all;
 }
 
-struct Shared {
-    Candidate kept[kSlots];
-    uint32_t count, waves[2][kWaves];
-    double sums[kWaves];
-};
 
 __device__ __forceinline__ uint64_t key_of(float score, uint32_t row) { return (uint64_t)ordered(score) << 32 | (0xFFFFFFFFu - row); }
 
@@ -133,7 +140,65 @@ __device__ __forceinline__ void load_turn(const T *scores, uint32_t first, uint3
     }
 }
 
-// Leaves the `best` first of the n kept (at least as many); returns the last one's score.
+template <int kWavesOf>
+struct SearchShared {
+    uint64_t some, differ[kWavesOf];
+    uint32_t reach[2][kWavesOf];
+};
+// How many of a workgroup's conditions hold.
+template <int kWavesOf, int kOf>
+__device__ __forceinline__ uint32_t block_count(const bool (&x)[kOf], uint32_t (&scratch)[kWavesOf]) {
+    uint32_t own = 0;
+#pragma unroll
+    for (int i = 0; i < kOf; ++i) own += (uint32_t)__popcll(__ballot(x[i]));
+    if (threadIdx.x % 64 == 0) scratch[threadIdx.x / 64] = own;
+    __syncthreads();
+    uint32_t all = 0;
+#pragma unroll
+    for (int w = 0; w < kWavesOf; ++w) all += scratch[w];
+    return all;
+}
+// A number that exactly the k largest of a workgroup's reach, unless several equal the k-th: then that.  0 is none; there are k others.
+template <int kWavesOf, int kOf>
+__device__ __forceinline__ uint64_t block_kth(const uint64_t (&x)[kOf], uint32_t k, SearchShared<kWavesOf> &s) {
+    uint64_t one = 0, differ = 0;
+#pragma unroll
+    for (int i = 0; i < kOf; ++i) one = x[i] ? x[i] : one;
+    if (one) s.some = one;  // whichever of them: bits that all share need no look
+    __syncthreads();
+    one = s.some;
+#pragma unroll
+    for (int i = 0; i < kOf; ++i) differ |= x[i] ? x[i] ^ one : 0;
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) differ |= __shfl_xor(differ, d);
+    if (threadIdx.x % 64 == 0) s.differ[threadIdx.x / 64] = differ;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWavesOf; ++w) differ |= s.differ[w];
+    const int bits = differ ? 64 - __builtin_clzll(differ) : 0;
+    uint64_t found = bits == 64 ? 0 : one >> bits << bits;
+#pragma unroll 1
+    for (int bit = bits - 1; bit >= 0; --bit) {
+        const uint64_t to = found | 1ull << bit;
+        bool reach[kOf];
+#pragma unroll
+        for (int i = 0; i < kOf; ++i) reach[i] = x[i] >= to;
+        const uint32_t all = block_count(reach, s.reach[bit % 2]);
+        if (all >= k) found = to;
+        if (all == k) break;
+    }
+    __syncthreads();
+    return found;
+}
+
+struct Shared {
+    Candidate kept[kSlots];
+    uint32_t count, waves[2][kWaves];
+    double sums[kWaves];
+    SearchShared<kWaves> search;
+};
+
+// Leaves the `best` first of the n kept (at least as many); returns a score that they reach.
 __device__ __forceinline__ float narrow(Shared &s, uint32_t n, uint32_t best) {
     constexpr int kOwn = kSlots / kThreads;
     uint64_t own[kOwn];
@@ -142,27 +207,12 @@ __device__ __forceinline__ float narrow(Shared &s, uint32_t n, uint32_t best) {
         const uint32_t at = threadIdx.x + i * kThreads;
         own[i] = at < n ? key_of(s.kept[at].score, s.kept[at].row) : 0;
     }
-    uint64_t found = 0;
-#pragma unroll 1
-    for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t to = found | 1ull << bit;
-        uint32_t reach = 0;
-#pragma unroll
-        for (int i = 0; i < kOwn; ++i) reach += (uint32_t)__popcll(__ballot(own[i] >= to));
-        uint32_t *waves = s.waves[bit % 2];
-        if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = reach;
-        __syncthreads();
-        uint32_t all = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) all += waves[w];
-        if (all >= best) found = to;
-    }
-    __syncthreads();
+    const uint64_t found = block_kth(own, best, s.search);
     if (threadIdx.x == 0) s.count = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kOwn; ++i)
-        if (own[i] >= found) s.kept[atomicAdd(&s.count, 1u)] = {value_of((uint32_t)(own[i] >> 32)), 0xFFFFFFFFu - (uint32_t)own[i]};
+        if (own[i] >= found && own[i]) s.kept[atomicAdd(&s.count, 1u)] = {value_of((uint32_t)(own[i] >> 32)), 0xFFFFFFFFu - (uint32_t)own[i]};
     __syncthreads();
     return value_of((uint32_t)(found >> 32));
 }
@@ -240,16 +290,25 @@ __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
     if (tid == 0) s.count = 0;
     __syncthreads();
     const T *scores = (const T *)a.scores + beam * a.stride;
-    float bound = -infinity(), least = kLowest, largest = -infinity(), top = -infinity();
+    float bound = -infinity(), least = kLowest, top = -infinity();
+    float largest[kPieces];  // so far, of each piece's places
+#pragma unroll
+    for (int h = 0; h < kPieces; ++h) largest[h] = -infinity();
     double sum = 0.0;
     uint32_t kept = 0, turn = 0;
     for (uint64_t first = begin; first < end; first += kTile, ++turn) {
         const uint32_t row = (uint32_t)first + 8 * tid;  // and so on in every quarter of the turn
         float v[kEach];
         load_turn(scores, (uint32_t)first, end, v);
-        float most = v[0];
+        float most = -infinity();
 #pragma unroll
-        for (int i = 1; i < kEach; ++i) most = fmaxf(most, v[i]);
+        for (int h = 0; h < kPieces; ++h) {
+            float some = v[8 * h];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) some = fmaxf(some, v[8 * h + i]);
+            largest[h] = fmaxf(largest[h], some);
+            most = fmaxf(most, some);
+        }
         if constexpr (kLog) {
             // exponentials of differences from a score of this thread that is not far below its largest
             if (most > top + 20.0f || top == -infinity()) {
@@ -269,9 +328,11 @@ __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
             }
             sum += (double)((terms[0] + terms[1]) + (terms[2] + terms[3]));
         }
-        largest = fmaxf(largest, most);
         if ((turn & (turn + 1)) == 0 || first + kTile >= end) {  // turns 0, 1, 3, 7, ..., and the last
-            const uint32_t found = bound_of_threads<kWaves>(ordered(largest), a.best, s.waves);
+            uint32_t order[kPieces];
+#pragma unroll
+            for (int h = 0; h < kPieces; ++h) order[h] = ordered(largest[h]);
+            const uint32_t found = bound_of_threads<kWaves>(order, a.best, s.waves);
             if (found > ordered(-infinity()) && value_of(found) > bound) {
                 // scores that are kept may lie below it; of those in later turns, equal ones come behind
                 bound = value_of(found);
@@ -289,6 +350,11 @@ __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
             }
         }
         if (__syncthreads_or(full)) {
+            if (kept >= a.best) {  // scores that equal the last of those come behind
+                bound = std::max(bound, narrow(s, kept, a.best));
+                least = std::max(least, next_above(bound));
+                kept = a.best;
+            }
             kept = take_slowly(s, kept, a.best, scores, (uint32_t)first, end, least, bound);
         } else {
             kept = s.count;
@@ -305,7 +371,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
                             : top == all_top ? sum : sum * exp((double)top - (double)all_top);
         log_sum = block_sum<kWaves>(mine, s.sums);
     }
-    const uint32_t most_kept = kAlone ? kSlots : a.slots;
+    const uint32_t most_kept = kAlone ? std::max(a.best, kFewToRank) : a.slots;
     if (kept > most_kept) {
         bound = narrow(s, kept, a.best);
         kept = a.best;
@@ -350,7 +416,61 @@ struct JoinShared {
     double log_sum[kMostBeams];
     float top[kMostBeams], base[kMostBeams];
     uint32_t count, waves[2][kJoinWaves];
+    SearchShared<kJoinWaves> search;
 };
+
+__device__ __forceinline__ uint64_t ordered(double x) {
+    const uint64_t bits = (uint64_t)__double_as_longlong(x + 0.0);
+    return bits ^ (bits >> 63 ? ~0ull : 1ull << 63);
+}
+
+// Leaves the `best` first of n candidates (n > best): by total; of those that equal the last one by beam and score; of those by row.
+__device__ __forceinline__ void narrow(JoinShared &s, uint32_t n, uint32_t best) {
+    double total[2];
+    float score[2];
+    uint32_t row[2], beam[2];
+    uint64_t key[2];
+    bool stays[2], above[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t i = threadIdx.x + h * kJoinThreads;
+        key[h] = 0;
+        if (i < n) total[h] = s.total[i], score[h] = s.score[i], row[h] = s.row[i], beam[h] = s.beam[i], key[h] = ordered(total[h]);
+        stays[h] = false;
+    }
+    uint32_t need = best;
+#pragma unroll
+    for (int round = 0; round < 3; ++round) {
+        const uint64_t found = block_kth(key, need, s.search);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) above[h] = key[h] > found;
+        const uint32_t more = block_count(above, s.search.reach[0]);
+        bool reach[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) reach[h] = key[h] >= found && key[h];
+        const uint32_t all = block_count(reach, s.search.reach[1]);
+        __syncthreads();
+        // all that reach it, where those are as many as are asked for; else those above, and the others by what comes next
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            stays[h] |= all == need ? reach[h] : above[h];
+            const bool open = all > need && key[h] == found;
+            key[h] = !open ? 0 : round == 0 ? (uint64_t)(0xFFFFFFFFu - beam[h]) << 32 | ordered(score[h]) : 0xFFFFFFFFu - row[h];
+        }
+        if (all == need) break;
+        need -= more;
+    }
+    if (threadIdx.x == 0) s.count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (!stays[h]) continue;
+        const uint32_t to = atomicAdd(&s.count, 1u);
+        s.total[to] = total[h], s.score[to] = score[h], s.row[to] = row[h], s.beam[to] = beam[h];
+    }
+    __syncthreads();
+}
+
 
 // How many of n candidates go before candidate i: by total, beam, score and row.
 __device__ __forceinline__ uint32_t rank_of(const JoinShared &s, uint32_t i, uint32_t n) {
@@ -457,8 +577,6 @@ __global__ __launch_bounds__(kJoinThreads) void k_select_join(SelectArgs a) {
         held_total[h] = -infinity();
         if (tid + h * kJoinThreads < all) held_total[h] = take(tid + h * kJoinThreads, held_beam[h], held[h]);
     }
-#pragma unroll
-    for (uint32_t h = 0; h < kHeld; ++h) largest = fmax(largest, held_total[h]);
     // a bound of the totals, as in a part
     double bound = -infinity();
     if (all > 2 * a.best) {
@@ -467,7 +585,10 @@ __global__ __launch_bounds__(kJoinThreads) void k_select_join(SelectArgs a) {
             Candidate c;
             largest = fmax(largest, take(i, beam, c));
         }
-        const uint32_t found = bound_of_threads<kJoinWaves>(ordered((float)largest), a.best, s.waves);
+        uint32_t order[1 + kHeld] = {ordered((float)largest)};
+#pragma unroll
+        for (uint32_t h = 0; h < kHeld; ++h) order[1 + h] = ordered((float)held_total[h]);
+        const uint32_t found = bound_of_threads<kJoinWaves>(order, a.best, s.waves);
         // the float nearest to a total may lie above it: the one below does not
         if (found > ordered(kLowest)) bound = (double)value_of(found - 1);
     }
@@ -500,23 +621,14 @@ __global__ __launch_bounds__(kJoinThreads) void k_select_join(SelectArgs a) {
         const uint32_t ended = a.done ? a.beams : 0;
         for (uint32_t from = 0; from < ended + all; from += kJoinThreads) {
             if (n + kJoinThreads > kJoinSlots) {
-                double total[2];
-                float score[2];
-                uint32_t row[2], beam[2], rank[2];
+                if (n > a.best) narrow(s, n, a.best);
+                if (n >= a.best) {
+                    double least = infinity();
+                    for (uint32_t i = lane; i < a.best; i += 64) least = fmin(least, s.total[i]);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t i = tid + h * kJoinThreads;
-                    rank[h] = i < n ? rank_of(s, i, n) : a.best;
-                    if (i < n) total[h] = s.total[i], score[h] = s.score[i], row[h] = s.row[i], beam[h] = s.beam[i];
+                    for (int d = 32; d > 0; d /= 2) least = fmin(least, __shfl_xor(least, d));
+                    bound = fmax(bound, least);
                 }
-                __syncthreads();
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (rank[h] < a.best)
-                        s.total[rank[h]] = total[h], s.score[rank[h]] = score[h], s.row[rank[h]] = row[h], s.beam[rank[h]] = beam[h];
-                if (tid == 0) s.count = std::min(n, a.best);
-                __syncthreads();
-                if (n >= a.best) bound = fmax(bound, s.total[a.best - 1]);
             }
             const uint32_t i = from + tid;
             if (i < ended) {
@@ -534,6 +646,10 @@ __global__ __launch_bounds__(kJoinThreads) void k_select_join(SelectArgs a) {
         }
     } else {
         n = s.count;
+    }
+    if (n > std::max(a.best, kFewToRank)) {
+        narrow(s, n, a.best);
+        n = a.best;
     }
     for (uint32_t i = tid; i < n; i += kJoinThreads) {
         const uint32_t rank = rank_of(s, i, n);
