@@ -585,9 +585,8 @@ __global__ __launch_bounds__(kJoinThreads) void k_select_join(SelectArgs a) {
             Candidate c;
             largest = fmax(largest, take(i, beam, c));
         }
-        uint32_t order[1 + kHeld] = {ordered((float)largest)};
-#pragma unroll
-        for (uint32_t h = 0; h < kHeld; ++h) order[1 + h] = ordered((float)held_total[h]);
+        const uint32_t order[kHeld] = {ordered((float)fmax(largest, held_total[0])), ordered((float)held_total[1]), ordered((float)held_total[2]),
+                                       ordered((float)held_total[3])};
         const uint32_t found = bound_of_threads<kJoinWaves>(order, a.best, s.waves);
         // the float nearest to a total may lie above it: the one below does not
         if (found > ordered(kLowest)) bound = (double)value_of(found - 1);
@@ -658,7 +657,9 @@ __global__ __launch_bounds__(kJoinThreads) void k_select_join(SelectArgs a) {
     for (uint32_t r = n + tid; r < a.best; r += kJoinThreads) put_none(a, group, r);
 }
 
-// How scores are cut: parts of whole turns, so many that a thousand workgroups are at work.
+// How scores are cut: parts of whole turns, so many that a thousand workgroups are at work, but no more than leave the join with
+// candidates that its registers hold (some 1.3 `best` a part; one query, 4 x 10^6 scores, best 100: 245 parts took 99 us), as far as the
+// chip is filled once.
 struct Cut {
     uint32_t parts, part_rows, slots;
     bool alone;
@@ -667,6 +668,7 @@ Cut cut_of(uint64_t queries, uint64_t rows, uint32_t beams, uint32_t best) {
     constexpr uint64_t kWanted = 1024;
     const uint64_t tiles = std::max<uint64_t>(1, (rows + kTile - 1) / kTile);
     uint64_t parts = std::min<uint64_t>(tiles, std::max<uint64_t>(1, kWanted / queries));
+    parts = std::min<uint64_t>(parts, std::max<uint64_t>({1, 3 * kJoinThreads / ((uint64_t)best * beams), std::min<uint64_t>(32, kWanted / 2 / queries)}));
     parts = std::min<uint64_t>(parts, kMostLists / beams);
     const uint64_t each = (tiles + parts - 1) / parts;
     parts = (tiles + each - 1) / each;
