@@ -63,19 +63,31 @@ __global__ __launch_bounds__(kLookupThreads) void k_copy_rows(LookupArgs a, Walk
 // The gradient.  A row takes `lanes` lanes (a power of two up to 64), a piece of eight columns each, and one part of 512 columns
 // after the other where it is longer.
 
+// Rows of eight columns and more (kWide) have no broken piece: the last one lies back so far that it is whole, and two lanes of a group
+// have the columns that it shares with the one before, and the same sums of them.  (A piece that may be broken is loaded in so many parts
+// that a step of the sums waits for each of them: 2^20 rows of 128 took 240 us instead of 120.)  They are the same wave's, so that
+// with add both have read what was there before either writes.
+template <bool kWide>
+__device__ __forceinline__ uint32_t first_of(uint32_t k, uint32_t cols) {
+    return kWide ? std::min(k, cols - 8) : k;
+}
+template <bool kWide>
+__device__ __forceinline__ uint32_t cols_of(uint32_t k, uint32_t cols) {
+    return kWide ? k + 8 : cols;
+}
 // A finished sum goes to its row.
-template <class Out>
+template <class Out, bool kWide>
 __device__ __forceinline__ void put_sum(const LookupGradArgs &a, uint32_t row, uint32_t k, float (&v)[8]) {
     Out *to = (Out *)a.out + row * a.out_stride;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= a.scale;
     if (a.add) {
         float there[8];
-        load_piece(to, k, a.cols, there);
+        load_piece(to, k, cols_of<kWide>(k, a.cols), there);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = there[i] + v[i];
     }
-    store_piece(to, k, a.cols, v);
+    store_piece(to, k, cols_of<kWide>(k, a.cols), v);
 }
 
 // Sums over the groups of a workgroup, in their order, for group 0: lane l of a group has piece l of them.
@@ -94,7 +106,7 @@ __device__ __forceinline__ void join_groups(float (&v)[8], float (*scratch)[8], 
 // names adds up all places of that row; others end.  Workgroups behind those write zeros to the rows that are not named.
 constexpr uint32_t kFew = 1024, kFillRows = 4096;
 
-template <class In, class Out>
+template <class In, class Out, bool kWide>
 __global__ __launch_bounds__(kGradThreads) void k_grad_few(LookupGradArgs a, uint32_t parts, uint32_t fill_blocks, uint32_t fill_rows) {
     constexpr int kEach = kFew / kGradThreads;
     __shared__ float scratch[kGradThreads][8];
@@ -155,14 +167,16 @@ __global__ __launch_bounds__(kGradThreads) void k_grad_few(LookupGradArgs a, uin
     for (int i = 0; i < kEach; ++i)
         if (found >> i & 1) same[to++] = (uint16_t)(kEach * tid + i);
     __syncthreads();
-    const uint32_t lanes = a.lanes, lane = tid % lanes, groups = kGradThreads / lanes, k = 512 * part + 8 * lane;
+    const uint32_t lanes = a.lanes, lane = tid % lanes, groups = kGradThreads / lanes;
+    const bool used = 512 * part + 8 * lane < a.cols;
+    const uint32_t k = first_of<kWide>(512 * part + 8 * lane, a.cols);
     float sum[8] = {};
-    if (k < a.cols) {
+    if (used) {
         for (uint32_t j = tid / lanes; j < all; j += 4 * groups) {
             Piece<In> p[4];
 #pragma unroll
             for (uint32_t u = 0; u < 4; ++u)
-                if (j + u * groups < all) p[u].load((const In *)a.grad + same[j + u * groups] * a.grad_stride, k, a.cols);
+                if (j + u * groups < all) p[u].load((const In *)a.grad + same[j + u * groups] * a.grad_stride, k, cols_of<kWide>(k, a.cols));
 #pragma unroll
             for (uint32_t u = 0; u < 4; ++u) {
                 if (j + u * groups >= all) continue;
@@ -174,10 +188,10 @@ __global__ __launch_bounds__(kGradThreads) void k_grad_few(LookupGradArgs a, uin
         }
     }
     join_groups(sum, scratch, lanes);
-    if (tid < lanes && k < a.cols) put_sum<Out>(a, row, k, sum);
+    if (tid < lanes && used) put_sum<Out, kWide>(a, row, k, sum);
 }
 
-// --- the order of the places by row.  keys: the rows, sorted (`rows` for places without one, at the end); order: the places.
+// --- the order of the places by row: pairs of a row (`rows` for places without one, at the end) and a place, sorted.
 
 // Some thousand places: the place of each is how many go before it.  A workgroup of 16 waves takes 64 places, each wave a
 // sixteenth of those that they are compared with.
@@ -209,8 +223,7 @@ __global__ __launch_bounds__(kRankThreads) void k_rank(LookupGradArgs a) {
     if (wave > 0 || t >= count) return;
 #pragma unroll
     for (int w = 1; w < kRankThreads / 64; ++w) rank += ranks[w][lane];
-    a.keys[rank] = mine;
-    a.order[rank] = t;
+    a.sorted[rank] = uint2{mine, t};
 }
 
 // Sets the flag of every row that is named.
@@ -224,28 +237,28 @@ __global__ __launch_bounds__(256) void k_clear_flags(uint8_t *flags, uint64_t ro
 
 // More: digits of up to 11 bits, the lowest first; places with equal digits keep their order.  Three launches a digit: how often
 // each workgroup's places have each digit, where those begin, and the places moved there.
-constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64, kSortSteps = 16;
+constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64, kSortSteps = 8;
 constexpr uint32_t kSortTile = kSortThreads * kSortSteps, kMostDigits = 1u << 11;
 
 struct Digit {
-    const uint32_t *keys, *order;  // null: as the batch has them
-    uint32_t *to_keys, *to_order;
+    const uint2 *from;  // null: as the batch has them
+    uint2 *to;
     uint32_t shift, bits, tiles;
-    uint8_t *set_flags;            // of the last digit, or null
+    uint8_t *set_flags;  // of the last digit, or null
 };
 
 __global__ __launch_bounds__(kSortThreads) void k_count_digits(LookupGradArgs a, Digit d) {
     __shared__ uint32_t counts[kMostDigits];
     const uint32_t digits = 1u << d.bits;
     for (uint32_t i = threadIdx.x; i < digits; i += kSortThreads) counts[i] = 0;
-    if (!d.keys) clear_flags(a.flags, a.rows);
+    if (!d.from) clear_flags(a.flags, a.rows);
     __syncthreads();
     const uint64_t first = (uint64_t)blockIdx.x * kSortTile;
 #pragma unroll
     for (int s = 0; s < kSortSteps; ++s) {
         const uint64_t t = first + s * kSortThreads + threadIdx.x;
         if (t >= a.count) continue;
-        const uint32_t key = d.keys ? d.keys[t] : row_at(a.index, t, a.rows);
+        const uint32_t key = d.from ? d.from[t].x : row_at(a.index, t, a.rows);
         atomicAdd(&counts[key >> d.shift & (digits - 1)], 1u);
     }
     __syncthreads();
@@ -301,19 +314,20 @@ __global__ __launch_bounds__(kSortThreads) void k_place_digits(LookupGradArgs a,
         if (digit < digits) base[digit] = upto + a.digit_counts[(uint64_t)digit * d.tiles + blockIdx.x];
         upto += total[i];
     }
-    // a wave takes 1024 places in a row, and counts those with the same digit before each
-    uint32_t key[kSortSteps], rank[kSortSteps];
+    // a wave takes 512 places in a row, and counts those with the same digit before each
+    uint2 pair[kSortSteps];
+    uint32_t rank[kSortSteps];
     const uint64_t first = (uint64_t)blockIdx.x * kSortTile + wave * (64 * kSortSteps) + lane;
 #pragma unroll
     for (int s = 0; s < kSortSteps; ++s) {
         const uint64_t t = first + 64 * s;
-        key[s] = t < a.count ? d.keys ? d.keys[t] : row_at(a.index, t, a.rows) : 0;
+        pair[s] = t >= a.count ? uint2{0, 0} : d.from ? d.from[t] : uint2{row_at(a.index, t, a.rows), (uint32_t)t};
     }
     volatile uint16_t *mine_of = counts[wave];
 #pragma unroll
     for (int s = 0; s < kSortSteps; ++s) {
         const bool there = first + 64 * s < a.count;
-        const uint32_t digit = key[s] >> d.shift & (digits - 1);
+        const uint32_t digit = pair[s].x >> d.shift & (digits - 1);
         uint64_t same = __ballot(there);
         for (uint32_t b = 0; b < d.bits; ++b) {
             const bool one = digit >> b & 1;
@@ -343,107 +357,195 @@ __global__ __launch_bounds__(kSortThreads) void k_place_digits(LookupGradArgs a,
     for (int s = 0; s < kSortSteps; ++s) {
         const uint64_t t = first + 64 * s;
         if (t >= a.count) continue;
-        const uint32_t digit = key[s] >> d.shift & (digits - 1);
+        const uint32_t digit = pair[s].x >> d.shift & (digits - 1);
         const uint32_t to = base[digit] + counts[wave][digit] + rank[s];
-        d.to_keys[to] = key[s];
-        d.to_order[to] = d.order ? d.order[t] : (uint32_t)t;
-        if (d.set_flags && key[s] < a.rows) d.set_flags[key[s]] = 1;
+        d.to[to] = pair[s];
+        if (d.set_flags && pair[s].x < a.rows) d.set_flags[pair[s].x] = 1;
     }
 }
 
 // --- the sums over the sorted places
 
-// A group of lanes goes along `chunk` sorted places.  A run of equal rows that lies within them is finished; one that goes on
-// behind them leaves partial[2 c + 1] where it begins here, and partial[2 c] where it began before (whether it ends here or not).
-// Workgroups behind those write zeros to the rows that are not named.
-template <class In, class Out>
-__global__ __launch_bounds__(kGradThreads) void k_sum_runs(LookupGradArgs a, uint32_t sum_blocks) {
+// A workgroup takes `chunk` sorted places, whose runs of equal rows its groups of lanes take in turn; long ones are taken by all groups together.
+// A run that begins there and ends within chunk / 4 places behind them is finished, and the workgroup of the next chunk leaves it out.  A
+// longer one leaves partial[2 c + 1] where it begins, and partial[2 c] where it began before (whether it ends there or not).  So the many
+// short runs are summed and written once, and only the few long ones pass through memory.  Workgroups behind those write zeros to the
+// rows that are not named.
+constexpr uint32_t kMostChunk = 1024, kLong = 32;
+
+__device__ __forceinline__ uint32_t key_at(const LookupGradArgs &a, uint64_t p) { return p < a.count ? a.sorted[p].x : 0xFFFFFFFFu; }
+// whether the run of `key` that goes on behind `border`, the first border that it passes, ends soon
+__device__ __forceinline__ bool ends_soon(const LookupGradArgs &a, uint64_t border, uint32_t key) { return key_at(a, border + a.chunk / 4) != key; }
+
+template <class In, class Out, bool kWide>
+__global__ __launch_bounds__(kGradThreads) void k_sum_runs(LookupGradArgs a, Walk fill, uint32_t sum_blocks) {
+    constexpr uint32_t kEach = kMostChunk / kGradThreads;
+    __shared__ uint2 pairs[kMostChunk + kMostChunk / 4 + 1];
+    __shared__ uint16_t begins[kMostChunk + 1], longs[kMostChunk / kLong + 2];
+    __shared__ uint32_t counts[kGradThreads / 64], found_longs;
+    __shared__ float scratch[kGradThreads][8];
     if (blockIdx.x >= sum_blocks) {
-        const uint64_t pieces = (a.cols + 7) / 8;
-        const uint64_t step = (uint64_t)(gridDim.x - sum_blocks) * kGradThreads;
-        for (uint64_t i = (uint64_t)(blockIdx.x - sum_blocks) * kGradThreads + threadIdx.x; i < a.rows * pieces; i += step) {
-            const uint64_t row = i / pieces;
-            if (a.flags[row]) continue;
+        walk_items(fill, [&](uint64_t row, uint32_t piece) {
+            if (a.flags[row]) return;
             const float zeros[8] = {};
-            store_piece((Out *)a.out + row * a.out_stride, 8 * (uint32_t)(i % pieces), a.cols, zeros);
-        }
+            store_piece((Out *)a.out + row * a.out_stride, 8 * piece, a.cols, zeros);
+        }, blockIdx.x - sum_blocks);
         return;
     }
-    constexpr int kAhead = 4;
-    const uint32_t group = (blockIdx.x * kGradThreads + threadIdx.x) / a.lanes, lane = threadIdx.x % a.lanes;
-    const uint32_t c = group % a.chunks, k = 512 * (group / a.chunks) + 8 * lane;
-    if (k >= a.cols) return;
-    const uint64_t first = (uint64_t)c * a.chunk, last = std::min<uint64_t>(a.count, first + a.chunk);
-    if (first >= last) return;
-    uint32_t key = a.keys[first];
-    bool inside = first == 0 || a.keys[first - 1] != key;  // the run began here
-    float sum[8] = {};
-    for (uint64_t p = first; p < last; p += kAhead) {
-        Piece<In> rows[kAhead];
-        uint32_t next[kAhead];
+    const uint32_t tid = threadIdx.x, c = blockIdx.x % a.chunks, part = blockIdx.x / a.chunks;
+    const uint64_t first = (uint64_t)c * a.chunk;
+    const uint32_t size = (uint32_t)std::min<uint64_t>(a.chunk, a.count - first), reach = size + a.chunk / 4;
+    for (uint32_t i = tid; i <= reach; i += kGradThreads) pairs[i] = first + i < a.count ? a.sorted[first + i] : uint2{0xFFFFFFFFu, 0};
+    const uint32_t before = first ? a.sorted[first - 1].x : 0xFFFFFFFFu, far = first > a.chunk ? a.sorted[first - a.chunk - 1].x : 0xFFFFFFFFu;
+    if (tid == 0) found_longs = 0;
+    __syncthreads();
+    // where runs begin, and the first place
+    uint32_t mine = 0, number = 0;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (p + u >= last) continue;
-            rows[u].load((const In *)a.grad + a.order[p + u] * a.grad_stride, k, a.cols);
-            next[u] = p + u + 1 < a.count ? a.keys[p + u + 1] : 0xFFFFFFFFu;
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t at = tid * kEach + i;
+        if (at < size && (at == 0 || pairs[at].x != pairs[at - 1].x)) mine |= 1u << i, ++number;
+    }
+    uint32_t upto = number;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t other = __shfl_up(upto, d);
+        if (tid % 64 >= (uint32_t)d) upto += other;
+    }
+    if (tid % 64 == 63) counts[tid / 64] = upto;
+    __syncthreads();
+    uint32_t to = upto - number, all = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kGradThreads / 64; ++w) {
+        if (w < tid / 64) to += counts[w];
+        all += counts[w];
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i)
+        if (mine >> i & 1) begins[to++] = (uint16_t)(tid * kEach + i);
+    __syncthreads();
+    const bool headless = pairs[0].x == before;  // the first run began before, and ended soon behind its first border:
+    const bool left_out = headless && far != before && pairs[a.chunk / 4].x != before;
+    const uint32_t lanes = a.lanes, lane = tid % lanes, groups = kGradThreads / lanes;
+    const bool used = 512 * part + 8 * lane < a.cols;
+    const uint32_t k = first_of<kWide>(512 * part + 8 * lane, a.cols);
+    // run j from place p on, behind `end`; whether it is finished here
+    const auto run_of = [&](uint32_t j, uint32_t &p, uint32_t &end, bool &goes_on) {
+        p = begins[j];
+        goes_on = false;
+        if (j + 1 < all) {
+            end = begins[j + 1];
+            return;
         }
+        end = size;
+        const uint32_t key = pairs[p].x;
+        if (pairs[end].x != key) return;
+        goes_on = (j == 0 && headless) || pairs[reach].x == key;
+        while (!goes_on && pairs[end].x == key) ++end;
+    };
+    const auto add_up = [&](uint32_t p, uint32_t end, uint32_t step, float (&sum)[8]) {
+        for (; p < end; p += 4 * step) {
+            Piece<In> rows[4];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (p + u >= last) continue;
-            float v[8];
-            rows[u].values(v);
+            for (uint32_t u = 0; u < 4; ++u)
+                if (p + u * step < end) rows[u].load((const In *)a.grad + pairs[p + u * step].y * a.grad_stride, k, cols_of<kWide>(k, a.cols));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += v[i];
-            if (next[u] != key || p + u + 1 == last) {
-                if (key < a.rows) {
-                    if (inside && next[u] != key) put_sum<Out>(a, key, k, sum);
-                    else store_piece(a.partial + (2ull * c + (inside ? 1 : 0)) * a.cols, k, a.cols, sum);
-                }
+            for (uint32_t u = 0; u < 4; ++u) {
+                if (p + u * step >= end) continue;
+                float v[8];
+                rows[u].values(v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-                key = next[u];
-                inside = true;
+                for (int i = 0; i < 8; ++i) sum[i] += v[i];
             }
         }
+    };
+    const auto finish = [&](uint32_t j, uint32_t key, bool goes_on, float (&sum)[8]) {
+        const bool head = j == 0 && headless;
+        if (!head && !goes_on) put_sum<Out, kWide>(a, key, k, sum);
+        else store_piece(a.partial + (2ull * c + (head ? 0 : 1)) * a.cols, k, cols_of<kWide>(k, a.cols), sum);
+    };
+    for (uint32_t j = tid / lanes; j < all; j += groups) {
+        uint32_t p, end;
+        bool goes_on;
+        run_of(j, p, end, goes_on);
+        const uint32_t key = pairs[p].x;
+        if (key >= a.rows || (j == 0 && left_out)) continue;
+        if (end - p > kLong) {
+            if (lane == 0) longs[atomicAdd(&found_longs, 1u)] = (uint16_t)j;
+            continue;
+        }
+        if (!used) continue;
+        float sum[8] = {};
+        add_up(p, end, 1, sum);
+        finish(j, key, goes_on, sum);
+    }
+    __syncthreads();
+    for (uint32_t l = 0; l < found_longs; ++l) {
+        uint32_t p, end;
+        bool goes_on;
+        run_of(longs[l], p, end, goes_on);
+        float sum[8] = {};
+        if (used) add_up(p + tid / lanes, end, groups, sum);
+        join_groups(sum, scratch, lanes);
+        if (tid < lanes && used) finish(longs[l], pairs[p].x, goes_on, sum);
+        __syncthreads();
     }
 }
 
-// Joins the partial sums of a run that begins among the places of c and goes on behind them.
-template <class Out>
+// Joins the partial sums of the long runs that begin among the places of kJoinChunks chunks: a thread looks at each chunk, and the workgroup
+// goes through what was found.
+constexpr uint32_t kJoinChunks = 64;
+
+template <class Out, bool kWide>
 __global__ __launch_bounds__(kGradThreads) void k_join_runs(LookupGradArgs a) {
     __shared__ float scratch[kGradThreads][8];
-    const uint32_t c = blockIdx.x % a.chunks;
-    const uint64_t first = (uint64_t)c * a.chunk, last = first + a.chunk;
-    if (last >= a.count) return;
-    const uint32_t key = a.keys[last - 1];
-    if (key >= a.rows || a.keys[last] != key) return;
-    if (a.keys[first] == key && first > 0 && a.keys[first - 1] == key) return;
-    uint32_t more = 0;  // chunks behind c that begin inside the run
-    for (;;) {
-        const uint64_t at = last + (uint64_t)(more + threadIdx.x) * a.chunk;
-        const uint32_t some = __syncthreads_count(at < a.count && a.keys[at] == key);
-        more += some;
-        if (some < kGradThreads) break;
-    }
-    const uint32_t lanes = a.lanes, lane = threadIdx.x % lanes, groups = kGradThreads / lanes, k = 512 * (blockIdx.x / a.chunks) + 8 * lane;
-    float sum[8] = {};
-    if (k < a.cols) {
-        for (uint32_t j = threadIdx.x / lanes; j <= more; j += 4 * groups) {  // 0: its own
-            float v[4][8];
-#pragma unroll
-            for (uint32_t u = 0; u < 4; ++u) {
-                const uint32_t at = j + u * groups;
-                if (at <= more) load_piece(a.partial + (2ull * (c + at) + (at == 0 ? 1 : 0)) * a.cols, k, a.cols, v[u]);
-            }
-#pragma unroll
-            for (uint32_t u = 0; u < 4; ++u)
-                if (j + u * groups <= more)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) sum[i] += v[u][i];
+    __shared__ uint64_t found;
+    const uint32_t blocks = (a.chunks + kJoinChunks - 1) / kJoinChunks, base = blockIdx.x % blocks * kJoinChunks;
+    const uint32_t lanes = a.lanes, lane = threadIdx.x % lanes, groups = kGradThreads / lanes;
+    const bool used = 512 * (blockIdx.x / blocks) + 8 * lane < a.cols;
+    const uint32_t k = first_of<kWide>(512 * (blockIdx.x / blocks) + 8 * lane, a.cols);
+    if (threadIdx.x < 64) {
+        const uint64_t first = (uint64_t)(base + threadIdx.x) * a.chunk, last = first + a.chunk;
+        bool mine = false;
+        if (base + threadIdx.x < a.chunks && last < a.count) {
+            const uint32_t key = key_at(a, last - 1);
+            const bool began = key_at(a, first) != key || first == 0 || key_at(a, first - 1) != key;
+            mine = key < a.rows && key_at(a, last) == key && began && !ends_soon(a, last, key);
         }
+        const uint64_t all = __ballot(mine);
+        if (threadIdx.x == 0) found = all;
     }
-    join_groups(sum, scratch, lanes);
-    if (threadIdx.x < lanes && k < a.cols) put_sum<Out>(a, key, k, sum);
+    __syncthreads();
+    for (uint64_t left = found; left; left &= left - 1) {
+        const uint32_t c = base + __builtin_ctzll(left);
+        const uint64_t last = (uint64_t)(c + 1) * a.chunk;
+        const uint32_t key = key_at(a, last);
+        uint32_t more = 0;  // chunks behind c that begin inside the run
+        for (;;) {
+            const uint32_t some = __syncthreads_count(key_at(a, last + (uint64_t)(more + threadIdx.x) * a.chunk) == key);
+            more += some;
+            if (some < kGradThreads) break;
+        }
+        float sum[8] = {};
+        if (used) {
+            for (uint32_t j = threadIdx.x / lanes; j <= more; j += 4 * groups) {  // 0: its own
+                float v[4][8];
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u) {
+                    const uint32_t at = j + u * groups;
+                    if (at <= more) load_piece(a.partial + (2ull * (c + at) + (at == 0 ? 1 : 0)) * a.cols, k, cols_of<kWide>(k, a.cols), v[u]);
+                }
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u)
+                    if (j + u * groups <= more)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sum[i] += v[u][i];
+            }
+        }
+        join_groups(sum, scratch, lanes);
+        if (threadIdx.x < lanes && used) put_sum<Out, kWide>(a, key, k, sum);
+        __syncthreads();
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -470,16 +572,17 @@ uint32_t lanes_of(uint32_t cols) {
 // How a batch is cut, and where its parts of the workspace lie (in words of four bytes).
 struct Plan {
     uint32_t lanes, parts, chunk, chunks, bits, passes, tiles;
-    uint64_t keys[2], order[2], counts, totals, flags, partial, words;
+    uint64_t sorted[2], counts, totals, flags, partial, words;
 };
-constexpr uint64_t kSumLanes = 1 << 18;
 
 Plan plan_of(uint64_t count, uint64_t rows, uint32_t cols, bool add) {
     Plan p{};
     p.lanes = lanes_of(cols);
     p.parts = (cols + 511) / 512;
-    const uint64_t most = std::max<uint64_t>(1, kSumLanes / ((uint64_t)p.lanes * p.parts));
-    p.chunk = (uint32_t)std::max<uint64_t>(8, (count + most - 1) / most);
+    // a thousand workgroups, of at least 32 places and of at most 256, unless the partial sums of long rows took over 32 MB
+    p.chunk = 32;
+    while (p.chunk < 256 && p.chunk * 1024ull < count) p.chunk *= 2;
+    while (p.chunk < kMostChunk && count / p.chunk * cols > (1 << 22)) p.chunk *= 2;
     p.chunks = (uint32_t)((count + p.chunk - 1) / p.chunk);
     while (rows >> p.bits) ++p.bits;  // `rows` itself is a key
     p.passes = (p.bits + 10) / 11;
@@ -491,7 +594,7 @@ Plan plan_of(uint64_t count, uint64_t rows, uint32_t cols, bool add) {
         return here;
     };
     const int pairs = count <= kRanked ? 1 : 2;
-    for (int i = 0; i < pairs; ++i) p.keys[i] = take(count), p.order[i] = take(count);
+    for (int i = 0; i < pairs; ++i) p.sorted[i] = take(2 * count);
     if (count > kRanked) {
         p.counts = take((uint64_t)kMostDigits * p.tiles);
         p.totals = take(kMostDigits);
@@ -536,8 +639,10 @@ hipError_t launch_lookup_grad(const LookupGradArgs &args, void *workspace, hipSt
         const uint32_t fill = a.add ? 0 : (uint32_t)std::min<uint64_t>((a.rows + fill_rows - 1) / fill_rows, 1 << 16);
         if (a.count == 0 && fill == 0) return hipSuccess;
         return by_types(a.type, a.out_type, [&](auto *i, auto *o) {
-            return launch(k_grad_few<std::remove_pointer_t<decltype(i)>, std::remove_pointer_t<decltype(o)>>, (uint32_t)a.count * parts + fill,
-                          kGradThreads, 0, stream, a, parts, fill, fill_rows);
+            using In = std::remove_pointer_t<decltype(i)>;
+            using Out = std::remove_pointer_t<decltype(o)>;
+            return launch(a.cols >= 8 ? k_grad_few<In, Out, true> : k_grad_few<In, Out, false>, (uint32_t)a.count * parts + fill, kGradThreads, 0,
+                          stream, a, parts, fill, fill_rows);
         });
     }
     const Plan p = plan_of(a.count, a.rows, a.cols, a.add);
@@ -551,7 +656,7 @@ hipError_t launch_lookup_grad(const LookupGradArgs &args, void *workspace, hipSt
         if (e == hipSuccess) e = next;
         return e == hipSuccess;
     };
-    a.keys = words + p.keys[0], a.order = words + p.order[0];
+    a.sorted = (uint2 *)(words + p.sorted[0]);
     if (a.count <= kRanked) {
         if (a.flags) {
             const uint32_t blocks = (uint32_t)std::min<uint64_t>((a.rows / 4 + 256) / 256, 4096);
@@ -566,22 +671,23 @@ hipError_t launch_lookup_grad(const LookupGradArgs &args, void *workspace, hipSt
             d.shift = done;
             d.bits = (p.bits - done + p.passes - pass - 1) / (p.passes - pass);
             done += d.bits;
-            d.to_keys = words + p.keys[pass % 2], d.to_order = words + p.order[pass % 2];
+            d.to = (uint2 *)(words + p.sorted[pass % 2]);
             d.set_flags = pass + 1 == p.passes ? a.flags : nullptr;
             if (!then(launch(k_count_digits, p.tiles, kSortThreads, 0, stream, a, d))) return e;
             if (!then(launch(k_sum_digits, ((1u << d.bits) + 3) / 4, 256, 0, stream, a, d))) return e;
             if (!then(launch(k_place_digits, p.tiles, kSortThreads, 0, stream, a, d))) return e;
-            d.keys = d.to_keys, d.order = d.to_order;
+            d.from = d.to;
         }
-        a.keys = d.to_keys, a.order = d.to_order;
+        a.sorted = d.to;
     }
-    const uint32_t sum_blocks = (uint32_t)(((uint64_t)p.chunks * p.parts * p.lanes + kGradThreads - 1) / kGradThreads);
-    const uint32_t fill = a.add ? 0 : (uint32_t)std::min<uint64_t>((a.rows * pieces + kGradThreads - 1) / kGradThreads, 4096);
+    const uint32_t sum_blocks = p.chunks * p.parts;
+    const uint32_t fill = a.add ? 0 : (uint32_t)std::min<uint64_t>(((uint64_t)a.rows * pieces + kGradThreads - 1) / kGradThreads, 1 << 16);
+    const Walk walk = fill ? walk_of(a.rows, pieces, (uint64_t)fill * kGradThreads) : Walk{};
     return by_types(a.type, a.out_type, [&](auto *i, auto *o) {
         using In = std::remove_pointer_t<decltype(i)>;
         using Out = std::remove_pointer_t<decltype(o)>;
-        if (!then(launch(k_sum_runs<In, Out>, sum_blocks + fill, kGradThreads, 0, stream, a, sum_blocks))) return e;
-        if (p.chunks > 1) then(launch(k_join_runs<Out>, p.chunks * p.parts, kGradThreads, 0, stream, a));
+        if (!then(launch(a.cols >= 8 ? k_sum_runs<In, Out, true> : k_sum_runs<In, Out, false>, sum_blocks + fill, kGradThreads, 0, stream, a, walk, sum_blocks))) return e;
+        if (p.chunks > 1) then(launch(a.cols >= 8 ? k_join_runs<Out, true> : k_join_runs<Out, false>, (p.chunks + kJoinChunks - 1) / kJoinChunks * p.parts, kGradThreads, 0, stream, a));
         return e;
     });
 }

@@ -37,10 +37,10 @@ __device__ __forceinline__ uint32_t largest_of_lanes(uint32_t x) {
     return join_lanes<kLanes>(x, larger);
 }
 
-// Calls take(row, item) for the items of this thread (see Walk).
+// Calls take(row, item) for the items of this thread (see Walk), of a workgroup that is `block` in the walk.
 template <class Walk, class Take>
-__device__ __forceinline__ void walk_items(const Walk &w, Take &&take) {
-    uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x, row;
+__device__ __forceinline__ void walk_items(const Walk &w, Take &&take, uint32_t block = blockIdx.x) {
+    uint64_t i = (uint64_t)block * blockDim.x + threadIdx.x, row;
     uint32_t item;
     if (w.all >> 32 == 0) {
         row = (uint32_t)i / w.each;

@@ -105,7 +105,8 @@ struct LookupGradArgs {
     float scale;
     bool add;
     // of the workspace, and how the batch is cut
-    uint32_t *keys, *order, *digit_counts, *digit_totals;
+    uint2 *sorted;  // rows and the places that name them
+    uint32_t *digit_counts, *digit_totals;
     uint8_t *flags;
     float *partial;
     uint32_t lanes, chunk, chunks;
