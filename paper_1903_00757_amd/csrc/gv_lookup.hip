@@ -237,7 +237,7 @@ __global__ __launch_bounds__(256) void k_clear_flags(uint8_t *flags, uint64_t ro
 
 // More: digits of up to 11 bits, the lowest first; places with equal digits keep their order.  Three launches a digit: how often
 // each workgroup's places have each digit, where those begin, and the places moved there.
-constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64, kSortSteps = 8;
+constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64, kSortSteps = 4;
 constexpr uint32_t kSortTile = kSortThreads * kSortSteps, kMostDigits = 1u << 11;
 
 struct Digit {
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(kSortThreads) void k_place_digits(LookupGradArgs a,
         if (digit < digits) base[digit] = upto + a.digit_counts[(uint64_t)digit * d.tiles + blockIdx.x];
         upto += total[i];
     }
-    // a wave takes 512 places in a row, and counts those with the same digit before each
+    // a wave takes 256 places in a row, and counts those with the same digit before each
     uint2 pair[kSortSteps];
     uint32_t rank[kSortSteps];
     const uint64_t first = (uint64_t)blockIdx.x * kSortTile + wave * (64 * kSortSteps) + lane;
@@ -494,7 +494,7 @@ __global__ __launch_bounds__(kGradThreads) void k_sum_runs(LookupGradArgs a, Wal
 
 // Joins the partial sums of the long runs that begin among the places of kJoinChunks chunks: a thread looks at each chunk, and the workgroup
 // goes through what was found.
-constexpr uint32_t kJoinChunks = 64;
+constexpr uint32_t kJoinChunks = 16;
 
 template <class Out, bool kWide>
 __global__ __launch_bounds__(kGradThreads) void k_join_runs(LookupGradArgs a) {
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(kGradThreads) void k_join_runs(LookupGradArgs a) {
     if (threadIdx.x < 64) {
         const uint64_t first = (uint64_t)(base + threadIdx.x) * a.chunk, last = first + a.chunk;
         bool mine = false;
-        if (base + threadIdx.x < a.chunks && last < a.count) {
+        if (threadIdx.x < kJoinChunks && base + threadIdx.x < a.chunks && last < a.count) {
             const uint32_t key = key_at(a, last - 1);
             const bool began = key_at(a, first) != key || first == 0 || key_at(a, first - 1) != key;
             mine = key < a.rows && key_at(a, last) == key && began && !ends_soon(a, last, key);
