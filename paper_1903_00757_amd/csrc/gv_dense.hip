@@ -23,14 +23,14 @@ typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 
 // The normal distribution's Phi(z) and, on the way, exp(-z^2 / 2).  Phi(-|z|) = (a1 t + ... + a5 t^5) exp(-z^2 / 2) / 2 with
-// t = 1 / (1 + 0.3275911 |z| / sqrt 2): formula 7.1.26 of Abramowitz and Stegun's Handbook, within 1.5e-7 / 2 of the true value, which is a
+// t = 1 / (1 + 0.3275911 |z| / sqrt 2) (the halves are in the numbers below): formula 7.1.26 of Abramowitz and Stegun's Handbook, within 1.5e-7 / 2 of the true value, which is a
 // unit of fp32 near 1; where Phi is small the factor exp(-z^2 / 2) keeps it so.  erff takes three times the instructions: 65536 x 512 x
 // 2048 with gelu took 520 us by it.
 __device__ __forceinline__ float normal(float z, float &bell) {
     const float x = fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(x, 0.23164190f, 1.0f));
-    bell = __expf(-0.5f * z * z);
-    const float poly = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
-    const float tail = 0.5f * t * poly * bell;
+    bell = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
+    const float poly = fmaf(fmaf(fmaf(fmaf(0.5307027145f, t, -0.7265760135f), t, 0.7107068705f), t, -0.142248368f), t, 0.127414796f);
+    const float tail = t * poly * bell;
     return z < 0.0f ? tail : 1.0f - tail;
 }
 // act(z), and its slope
@@ -375,9 +375,9 @@ typedef __attribute__((address_space(3))) void LdsAny;
 constexpr uint32_t kWide = 64;                 // k's of a step
 constexpr uint64_t kWideStride = 1ull << 21;   // a tile's rows lie within 2^31 bytes
 
-// kSpread: row 4 g + r of tile j of the matrix instruction is row 16 g + 4 j + r of 64 rows, and tiles 4 to 7 are of the next 64.  For B that
-// leaves the lanes of group g with 16 columns of the result in a row, which four of them write as a whole line; operands that
-// are turned are read at fewer different addresses.
+// kSpread: row 4 g + r of tile j of the matrix instruction is row 32 (j / 2) + 8 g + 4 (j % 2) + r of 64 rows, and tiles 4 to 7 are of the next
+// 64.  For B that leaves the lanes of group g with 8 columns of the result in a row, twice, and four of them write 64 bytes in a row
+// with each store; operands that are turned are read at fewer different addresses.
 template <int kTile, bool kAlong, bool kSpread>
 struct Operand {
     static constexpr uint32_t kThreads = 2 * kTile, kLoads = kTile * 128 / 16 / kThreads;
@@ -385,12 +385,12 @@ struct Operand {
     static constexpr uint32_t kRows = kThreads / kLine;        // that the workgroup loads at once
     const char *at, *end;  // the tile's first value of the next step, and of the matrix behind its last
     uint64_t step, rows;   // bytes to the next step, and to the next rows
-    uint32_t from;         // of this lane in the first rows (and in the others likewise), in bytes
+    uint32_t stride;       // values
     // A piece's place: along k rows of 128 bytes, piece p of row r at p ^ turn(r); otherwise rows of kTile values of one k, piece p of
     // row k at p ^ turn(k): what lanes read together lies in different banks.
     static __device__ __forceinline__ uint32_t turn(uint32_t row) {
-        if constexpr (kAlong) return kSpread ? (row & 3) | (row >> 4 & 1) << 2 : row & 7;
-        else return (row & 1) | (row >> 1 & 1) << 3;
+        if constexpr (kAlong) return kSpread ? (row & 3) | (row >> 3 & 1) << 2 : row & 7;
+        else return (row & 3) << 2;
     }
     // value k (and first row) of a matrix of `lines` lines of `length` values
     __device__ __forceinline__ void begin(const void *p, uint64_t stride, uint64_t lines, uint64_t length, uint32_t first, uint32_t k) {
@@ -398,17 +398,25 @@ struct Operand {
         end = (const char *)p + 2 * ((lines - 1) * stride + length);
         step = kAlong ? 2 * kWide : 2 * kWide * stride;
         rows = 2 * kRows * stride;
-        from = 2 * (threadIdx.x / kLine * (uint32_t)stride + (threadIdx.x % kLine ^ turn(threadIdx.x / kLine)) * 8);
+        this->stride = (uint32_t)stride;
+    }
+    // What a thread loads of the first rows (and of the others likewise), in bytes from there.
+    __device__ __forceinline__ uint32_t from(uint32_t thread) const {
+        return 2 * (thread / kLine * stride + (thread % kLine ^ turn(thread / kLine)) * 8);
     }
     // Asks for the next step.  Nothing is read behind the matrix's end; what lies behind its rows and columns is not used.
-    __device__ __forceinline__ void fetch(char *tile) {
-        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63u);
+    __device__ __forceinline__ void fetch(char *tile, uint32_t wave) {
+        uint32_t thread = threadIdx.x;
+        asm volatile("" : "+v"(thread));  // a few instructions a step, and no register that the sums need
+        const uint32_t offset = from(thread);
         const char *p = at;
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; ++j, p += rows) {
-            const uint32_t bytes = p < end ? (uint32_t)std::min<uint64_t>(end - p, 0xFFFFFFFFu) : 0;
+            const int64_t left = end - p;  // scalar instructions compare words
+            const int high = (int)(left >> 32);
+            const uint32_t bytes = high < 0 ? 0u : high > 0 ? 0xFFFFFFFFu : (uint32_t)left;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, bytes, 0x00020000),
-                                                     (LdsAny *)(tile + (j * kThreads + wave) * 16), 16, from, 0, 0, 0);
+                                                     (LdsAny *)(tile + j * kThreads * 16 + wave), 16, offset, 0, 0, 0);
         }
         at += step;
     }
@@ -420,7 +428,7 @@ struct Operand {
             const uint32_t id = j * kThreads + threadIdx.x;
             const uint32_t k = kAlong ? (id % kLine ^ turn(id / kLine)) * 8 : id / kLine;
             uint4 v = {};
-            if (k < left && p + from < end) __builtin_memcpy(&v, p + from, 16);  // whole pieces: 8 k's of a row, or 8 rows of a k
+            if (k < left && p + from(threadIdx.x) < end) __builtin_memcpy(&v, p + from(threadIdx.x), 16);  // whole pieces: 8 k's of a row, or 8 rows of a k
             *(uint4 *)(tile + id * 16) = v;
         }
     }
@@ -434,21 +442,21 @@ struct Reader {
         using Of = Operand<kTile, kAlong, kSpread>;
         const uint32_t lane = threadIdx.x % 64, group = lane / 16, at = lane % 16;
         if constexpr (kAlong) {
-            row += kSpread ? at / 4 * 16 + at % 4 : at;  // tiles are 4 or 16 rows apart
+            row += kSpread ? at / 4 * 8 + at % 4 : at;
             base = row * 128 + (group ^ Of::turn(row)) * 16;
         } else {
             // lanes point to four rows of one k each, and get four k's of one row
             const uint32_t k = 8 * group + at / 4;
-            base = k * (2 * kTile) + ((row / 8 + at % 4 * 2) ^ Of::turn(k)) * 16;
+            base = k * (2 * kTile) + ((row / 8 + at % 4) ^ Of::turn(k)) * 16;
         }
     }
     __device__ __forceinline__ uint4 read(const char *tile, int half, int i) const {
         if constexpr (kAlong) {
-            // turn() of rows that are 16 apart is the same; of rows 4 i apart as well
-            return *(const uint4 *)(tile + (base ^ 64 * half) + (kSpread ? 512 : 2048) * i);
+            // turn() is the same for all tiles' rows
+            return *(const uint4 *)(tile + (base ^ 64 * half) + (kSpread ? 512 * (i % 2) + 4096 * (i / 2) : 2048 * i));
         } else {
             static_assert(kSpread, "what is turned is spread");
-            const char *at = tile + (base ^ (16 * (i % 4 / 2) + 128 * (i / 4))) + 8 * (i % 2) + half * (32 * 2 * kTile);
+            const char *at = tile + (base ^ (64 * (i % 4 / 2) + 128 * (i / 4))) + 8 * (i % 2) + half * (32 * 2 * kTile);
             const s4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsFour *)at);
             const s4v high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsFour *)(at + 8 * kTile));
             const uint2 x = __builtin_bit_cast(uint2, low), y = __builtin_bit_cast(uint2, high);
@@ -470,7 +478,7 @@ __global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint
     const uint32_t band = id / (8 * tiles_n), high = std::min(8u, tiles_m - 8 * band), in_band = id - 8 * band * tiles_n;
     const uint32_t m0 = (8 * band + in_band % high) * kTile, n0 = in_band / high * kTile;
     const uint32_t k_first = split * a.split_k, k_last = std::min<uint64_t>(a.cols, (uint64_t)k_first + a.split_k);
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, wm = wave % 2 * (kTile / 2), wn = wave / 2 * 64;
+    const uint32_t wave = threadIdx.x / 64, wm = wave % 2 * (kTile / 2), wn = wave / 2 * 64;
     f4 sums[kMs][kNs];
 #pragma unroll
     for (int i = 0; i < kMs; ++i)
@@ -483,10 +491,11 @@ __global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint
     // Steps go in pairs.  What is left of k behind the whole steps goes first, and a step of zeros makes the number even.
     uint32_t whole = (k_last - k_first) / kWide;
     const uint32_t left = (k_last - k_first) % kWide, odd = (whole + (left ? 1 : 0)) % 2;
+    const uint32_t wave_at = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 1024;  // in LDS, of what a wave loads
     const auto fetch = [&](char *ta, char *tb) {
         if (whole == 0) return;
-        of_a.fetch(ta);
-        of_b.fetch(tb);
+        of_a.fetch(ta, wave_at);
+        of_b.fetch(tb, wave_at);
         --whole;
     };
     const auto arrived = [] {
@@ -543,7 +552,72 @@ __global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint
         fetch(a1, b1);
         products(kSecond, a0, b0);
     }
-    // a lane has 16 columns in a row of each of its rows
+    // What the results' places are made of is taken again here: kept through the steps, it took registers that they need.
+    uint32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const uint32_t end_lane = thread % 64, end_wave = __builtin_amdgcn_readfirstlane(thread / 64);
+    const uint32_t end_m = m0 + end_wave % 2 * (kTile / 2), end_n = n0 + end_wave / 2 * 64;
+    // a lane has twice 8 columns in a row of each of its rows
+    const auto row_of = [&](int i) {
+        return end_m + (kAAlong ? 16 * i + end_lane % 16 : 64 * (i / 4) + 32 * (i % 4 / 2) + end_lane % 16 / 4 * 8 + 4 * (i % 2) + end_lane % 4);
+    };
+    const auto column_of = [&](int h) { return end_n + 32 * h + 8 * (end_lane / 16); };
+    // A whole tile without a check: bias is read once, and the residual's values are asked for a row ahead (what is written may be they, so the
+    // compiler leaves each load behind the stores before it).  A value that is read under a condition of its own is waited for on the
+    // way past it, and with it all stores before: 65536 x 512 x 2048 took 290 us instead of 200.
+    const auto whole_tile = [&](auto with) {
+        constexpr bool kResidual = decltype(with)::value;
+        float bias[2][8];
+        Values<T, 8> residual[2][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            Values<T, 8> b = {};
+            if (a.bias) b.load((const T *)a.bias + column_of(h), 8);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) bias[h][c] = (float)b.at[c];
+        }
+        const auto ask = [&](int i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) residual[i % 2][h].load((const T *)a.residual + row_of(i) * a.residual_stride + column_of(h), 8);
+        };
+        if constexpr (kResidual) ask(0);
+#pragma unroll
+        for (int i = 0; i < kMs; ++i) {
+            if (kResidual && i + 1 < kMs) ask(i + 1);
+            float z[2][8];
+            Values<T, 8> to[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) z[h][c] = sums[i][2 * h + c / 4][c % 4] + bias[h][c];
+            if (a.pre) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    to[h].round(z[h]);
+                    to[h].store((T *)a.pre + row_of(i) * a.pre_stride + column_of(h), 8);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (a.act != GV_ACT_NONE) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) z[h][c] = act_of(a.act, z[h][c]);
+                }
+                if constexpr (kResidual) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) z[h][c] += (float)residual[i % 2][h].at[c];
+                }
+                to[h].round(z[h]);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) to[h].store((T *)a.out + row_of(i) * a.out_stride + column_of(h), 8);
+        }
+    };
+    if (!a.partial && m0 + kTile <= a.rows && n0 + kTile <= a.outs) {
+        if (a.residual) whole_tile(std::true_type());
+        else whole_tile(std::false_type());
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < kMs; ++i)
 #pragma unroll
@@ -551,8 +625,7 @@ __global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint
             float z[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) z[c] = sums[i][2 * h + c / 4][c % 4];
-            const uint32_t m = kAAlong ? 16 * i + lane % 16 : 64 * (i / 4) + 4 * (i % 4) + lane % 16 / 4 * 16 + lane % 4;
-            finish<T>(a, m0 + wm + m, n0 + wn + 16 * (lane / 16) + 8 * h, split, z);
+            finish<T>(a, row_of(i), column_of(h), split, z);
         }
 }
 
@@ -622,36 +695,55 @@ __global__ __launch_bounds__(kFewThreads) void k_product_few(DenseArgs a) {
 // gz = grad * slope(pre), and the sums over its rows: a lane has eight columns, a wave 512, the waves of a workgroup take rows in turn.
 constexpr int kSlopeThreads = 256, kSlopeWaves = kSlopeThreads / 64;
 
-template <class T>
+// Rows of eight columns and more (kWide) have no broken piece: the last one lies back so far that it is whole, and two lanes have the
+// columns that it shares with the one before, and the same of them.  A part has 512 columns, or 504 where the last would have fewer than eight.
+__host__ __device__ __forceinline__ uint32_t part_of(uint32_t cols) { return cols > 512 && cols % 512 > 0 && cols % 512 < 8 ? 504 : 512; }
+
+template <class T, bool kWide>
 __global__ __launch_bounds__(kSlopeThreads) void k_slope(DenseGradArgs a) {
     __shared__ float joined[kSlopeWaves][512];
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, parts = (a.outs + 511) / 512;
-    const uint32_t part = blockIdx.x % parts, chunk = blockIdx.x / parts, k = 512 * part + 8 * lane;
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, width = part_of(a.outs), parts = (a.outs + width - 1) / width;
+    const uint32_t part = blockIdx.x % parts, chunk = blockIdx.x / parts;
+    const bool used = 8 * lane < width && width * part + 8 * lane < a.outs;
+    const uint32_t k = kWide ? std::min(width * part + 8 * lane, a.outs - 8) : width * part + 8 * lane, cols = kWide ? k + 8 : a.outs;
     const uint64_t first = (uint64_t)chunk * a.chunk, last = std::min<uint64_t>(a.rows, first + a.chunk);
     float sums[8] = {};
-    if (k < a.outs) {
-        for (uint64_t row = first + wave; row < last; row += kSlopeWaves) {
-            float g[8];
-            load_piece((const T *)a.grad + row * a.grad_stride, k, a.outs, g);
-            if (a.act != GV_ACT_NONE) {
-                float z[8];
-                load_piece((const T *)a.pre + row * a.pre_stride, k, a.outs, z);
+    if (used) {
+        for (uint64_t row = first + wave; row < last; row += 2 * kSlopeWaves) {
+            Piece<T> g[2], z[2];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] *= slope_of(a.act, z[i]);
-                if (a.gz) store_piece((T *)a.gz + row * a.outs, k, a.outs, g);
+            for (int h = 0; h < 2; ++h) {
+                const uint64_t at = row + h * kSlopeWaves;
+                if (at >= last) continue;
+                g[h].load((const T *)a.grad + at * a.grad_stride, k, cols);
+                if (a.act != GV_ACT_NONE) z[h].load((const T *)a.pre + at * a.pre_stride, k, cols);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sums[i] += g[i];
+            for (int h = 0; h < 2; ++h) {
+                const uint64_t at = row + h * kSlopeWaves;
+                if (at >= last) continue;
+                float v[8];
+                g[h].values(v);
+                if (a.act != GV_ACT_NONE) {
+                    float of[8];
+                    z[h].values(of);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] *= slope_of(a.act, of[i]);
+                    if (a.gz) store_piece((T *)a.gz + at * a.outs, k, cols, v);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sums[i] += v[i];
+            }
         }
     }
     if (!a.bias_partial) return;
-    __builtin_memcpy(&joined[wave][8 * lane], sums, sizeof sums);
+    if (used) __builtin_memcpy(&joined[wave][k - width * part], sums, sizeof sums);
     __syncthreads();
-    for (uint32_t c = threadIdx.x; c < 512 && 512 * part + c < a.outs; c += kSlopeThreads) {
+    for (uint32_t c = threadIdx.x; c < width && width * part + c < a.outs; c += kSlopeThreads) {
         float all = 0.0f;
 #pragma unroll
         for (int w = 0; w < kSlopeWaves; ++w) all += joined[w][c];
-        a.bias_partial[(uint64_t)chunk * a.outs + 512 * part + c] = all;
+        a.bias_partial[(uint64_t)chunk * a.outs + width * part + c] = all;
     }
 }
 
@@ -680,13 +772,15 @@ hipError_t by_type(int type, Run &&run) {
 // How a product of rows x outs over `cols` k's is cut: the way that is the shortest by what steps were measured to take.  Larger tiles ask
 // for fewer values (8192 x 4096 x 4096 in bfloat16: 214 us by tiles of 256, 256 by 128; 65536 x 512 x 2048 202, 227 and 413 by the small
 // ones), smaller ones are more workgroups (1000 x 1000 x 1000: 32, 22 and 10 us), and a long k is cut where there are few (a weight's
-// gradient of 65536 x 128 x 512: 50 us in 64 parts of 128 tiles, 203 in 8).
+// gradient of 65536 x 128 x 512: 50 us in 64 parts of 128 tiles, 203 in 8).  `more`: an epilogue with an activation or other matrices is as long as
+// several steps, and only where workgroups share a compute unit does another's product go on beside it (65536 x 512 x 2048 with gelu and
+// pre: 357 us by tiles of 256, 319 by 128).
 struct Cut {
     uint32_t tile, tiles_m, tiles_n, splits, split_k;
 };
 constexpr uint32_t kFewRows = 64;
 
-Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide) {
+Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide, bool more) {
     const uint64_t step = kStep / (type == GV_F32 ? 4 : 2), steps = std::max<uint64_t>(1, (cols + step - 1) / step);
     // tiles, workgroups that run at once, and what a step of theirs takes then, in microseconds
     struct Way {
@@ -702,7 +796,7 @@ Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide) {
         for (uint64_t splits = 1; splits <= 64 && (splits == 1 || steps >= 4 * splits); splits *= 2) {
             const uint64_t each = (steps + splits - 1) / splits, cut = (steps + each - 1) / each;
             const double rounds = (double)(m * n * cut) / w.at_once, alone = 0.3 + 0.7 * std::min(1.0, rounds);
-            const double time = std::ceil(rounds) * ((double)each * w.each * alone + 3.0) + (cut > 1 ? 4.0 + (double)(cut * rows * outs) * 2e-6 : 0.0);
+            const double time = std::ceil(rounds) * ((double)each * w.each * alone + (more && w.m == 256 ? 12.0 : 3.0)) + (cut > 1 ? 4.0 + (double)(cut * rows * outs) * 2e-6 : 0.0);
             if (time < least) {
                 least = time;
                 best = {w.m, (uint32_t)m, (uint32_t)n, (uint32_t)cut, (uint32_t)(each * step)};
@@ -713,10 +807,11 @@ Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide) {
 }
 uint64_t partial_of(const Cut &c, uint64_t rows, uint64_t outs) { return c.splits > 1 ? 4ull * c.splits * rows * outs : 0; }
 
-// with what an alignment may ask for
+// of any alignment and epilogue
 uint64_t most_partial_of(uint64_t rows, uint64_t cols, uint64_t outs, int type) {
-    const uint64_t some = partial_of(cut_of(rows, cols, outs, type, false), rows, outs);
-    return type == GV_F32 ? some : std::max(some, partial_of(cut_of(rows, cols, outs, type, true), rows, outs));
+    uint64_t most = 0;
+    for (int i = 0; i < 4; ++i) most = std::max(most, partial_of(cut_of(rows, cols, outs, type, i % 2, i / 2), rows, outs));
+    return most;
 }
 
 template <class T, bool kAAlong, bool kBAlong>
@@ -726,7 +821,7 @@ hipError_t product(DenseArgs a, void *workspace, hipStream_t stream) {
         return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && together % 8 == 0 && together > 0 && stride < kWideStride;
     };
     const bool wide = sizeof(T) == 2 && whole(a.x, a.x_stride, kAAlong ? a.cols : a.rows) && whole(a.weight, a.weight_stride, kBAlong ? a.cols : a.outs);
-    const Cut c = cut_of(a.rows, a.cols, a.outs, a.type, wide);
+    const Cut c = cut_of(a.rows, a.cols, a.outs, a.type, wide, a.act != GV_ACT_NONE || a.pre || a.residual);
     a.split_k = c.split_k;
     a.partial = c.splits > 1 ? (float *)workspace : nullptr;
     const uint32_t blocks = c.tiles_m * c.tiles_n * c.splits;
@@ -800,7 +895,7 @@ hipError_t launch_dense_grad(const DenseGradArgs &args, void *workspace, hipStre
         a.bias_partial = a.grad_bias ? (float *)((char *)workspace + p.bias) : nullptr;
         void *space = (char *)workspace + p.product;
         hipError_t e = hipSuccess;
-        if ((a.gz || a.grad_bias) && a.rows > 0) e = launch(k_slope<T>, p.chunks * ((a.outs + 511) / 512), kSlopeThreads, 0, stream, a);
+        if ((a.gz || a.grad_bias) && a.rows > 0) e = launch(a.outs >= 8 ? k_slope<T, true> : k_slope<T, false>, p.chunks * ((a.outs + part_of(a.outs) - 1) / part_of(a.outs)), kSlopeThreads, 0, stream, a);
         if (e == hipSuccess && a.grad_bias) e = launch(k_join_bias<T>, (a.outs + 31) / 32, 1024, 0, stream, a, p.chunks);
         const void *gz = a.gz ? a.gz : a.grad;
         const uint64_t gz_stride = a.gz ? a.outs : a.grad_stride;

@@ -64,9 +64,11 @@ __global__ __launch_bounds__(kLookupThreads) void k_copy_rows(LookupArgs a, Walk
 // after the other where it is longer.
 
 // Rows of eight columns and more (kWide) have no broken piece: the last one lies back so far that it is whole, and two lanes of a group
-// have the columns that it shares with the one before, and the same sums of them.  (A piece that may be broken is loaded in so many parts
+// have the columns that it shares with the one before, and the same sums of them.  A part of
+// a row has 512 columns, or 504 where the last would have fewer than eight: pieces of two parts share none.  (A piece that may be broken is loaded in so many parts
 // that a step of the sums waits for each of them: 2^20 rows of 128 took 240 us instead of 120.)  They are the same wave's, so that
 // with add both have read what was there before either writes.
+__host__ __device__ __forceinline__ uint32_t part_of(uint32_t cols) { return cols > 512 && cols % 512 > 0 && cols % 512 < 8 ? 504 : 512; }
 template <bool kWide>
 __device__ __forceinline__ uint32_t first_of(uint32_t k, uint32_t cols) {
     return kWide ? std::min(k, cols - 8) : k;
@@ -168,8 +170,9 @@ __global__ __launch_bounds__(kGradThreads) void k_grad_few(LookupGradArgs a, uin
         if (found >> i & 1) same[to++] = (uint16_t)(kEach * tid + i);
     __syncthreads();
     const uint32_t lanes = a.lanes, lane = tid % lanes, groups = kGradThreads / lanes;
-    const bool used = 512 * part + 8 * lane < a.cols;
-    const uint32_t k = first_of<kWide>(512 * part + 8 * lane, a.cols);
+    const uint32_t width = part_of(a.cols), column = width * part + 8 * lane;
+    const bool used = 8 * lane < width && column < a.cols;
+    const uint32_t k = first_of<kWide>(column, a.cols);
     float sum[8] = {};
     if (used) {
         for (uint32_t j = tid / lanes; j < all; j += 4 * groups) {
@@ -427,8 +430,9 @@ __global__ __launch_bounds__(kGradThreads) void k_sum_runs(LookupGradArgs a, Wal
     const bool headless = pairs[0].x == before;  // the first run began before, and ended soon behind its first border:
     const bool left_out = headless && far != before && pairs[a.chunk / 4].x != before;
     const uint32_t lanes = a.lanes, lane = tid % lanes, groups = kGradThreads / lanes;
-    const bool used = 512 * part + 8 * lane < a.cols;
-    const uint32_t k = first_of<kWide>(512 * part + 8 * lane, a.cols);
+    const uint32_t width = part_of(a.cols), column = width * part + 8 * lane;
+    const bool used = 8 * lane < width && column < a.cols;
+    const uint32_t k = first_of<kWide>(column, a.cols);
     // run j from place p on, behind `end`; whether it is finished here
     const auto run_of = [&](uint32_t j, uint32_t &p, uint32_t &end, bool &goes_on) {
         p = begins[j];
@@ -502,8 +506,9 @@ __global__ __launch_bounds__(kGradThreads) void k_join_runs(LookupGradArgs a) {
     __shared__ uint64_t found;
     const uint32_t blocks = (a.chunks + kJoinChunks - 1) / kJoinChunks, base = blockIdx.x % blocks * kJoinChunks;
     const uint32_t lanes = a.lanes, lane = threadIdx.x % lanes, groups = kGradThreads / lanes;
-    const bool used = 512 * (blockIdx.x / blocks) + 8 * lane < a.cols;
-    const uint32_t k = first_of<kWide>(512 * (blockIdx.x / blocks) + 8 * lane, a.cols);
+    const uint32_t width = part_of(a.cols), column = width * (blockIdx.x / blocks) + 8 * lane;
+    const bool used = 8 * lane < width && column < a.cols;
+    const uint32_t k = first_of<kWide>(column, a.cols);
     if (threadIdx.x < 64) {
         const uint64_t first = (uint64_t)(base + threadIdx.x) * a.chunk, last = first + a.chunk;
         bool mine = false;
@@ -578,7 +583,7 @@ struct Plan {
 Plan plan_of(uint64_t count, uint64_t rows, uint32_t cols, bool add) {
     Plan p{};
     p.lanes = lanes_of(cols);
-    p.parts = (cols + 511) / 512;
+    p.parts = (cols + part_of(cols) - 1) / part_of(cols);
     // a thousand workgroups, of at least 32 places and of at most 256, unless the partial sums of long rows took over 32 MB
     p.chunk = 32;
     while (p.chunk < 256 && p.chunk * 1024ull < count) p.chunk *= 2;
@@ -632,7 +637,7 @@ hipError_t launch_lookup_grad(const LookupGradArgs &args, void *workspace, hipSt
     const uint32_t pieces = (a.cols + 7) / 8;
     if (a.count <= kFew) {
         a.lanes = lanes_of(a.cols);
-        const uint32_t parts = (a.cols + 511) / 512;
+        const uint32_t parts = (a.cols + part_of(a.cols) - 1) / part_of(a.cols);
         // rows that a workgroup writes zeros to: 16 KB of them at least, and a thousand workgroups where that is enough
         const uint64_t each = std::max<uint64_t>(std::max<uint64_t>(1, 512 / pieces), (a.rows + 1023) / 1024);
         const uint32_t fill_rows = (uint32_t)std::min<uint64_t>(each, kFillRows);

@@ -190,7 +190,7 @@ def test_layer(gv, kind, rows, cols, outs, pad, shift):
 
 @gpu
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("rows,cols,outs,pad,shift", SHAPES + [(5000, 17, 9, 0, 0), (40_000, 64, 96, 0, 0)])
+@pytest.mark.parametrize("rows,cols,outs,pad,shift", SHAPES + [(5000, 17, 9, 0, 0), (40_000, 64, 96, 0, 0), (300, 33, 515, 1, 1), (90, 20, 1031, 0, 0)])
 def test_gradients(gv, kind, rows, cols, outs, pad, shift):
     import torch
 

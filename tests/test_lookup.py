@@ -189,7 +189,8 @@ def test_lookup_copies_bits(gv, name):
 GRADS = [(1, 1, 1, "i64", 0, 0), (7, 3, 5, "i32", 1, 1), (0, 100, 16, "i64", 0, 0), (50, 0, 16, "i32", 0, 0), (997, 5003, 353, "i64", 0, 0),
          (1024, 40000, 32, "pair", 0, 0), (1025, 17, 128, "i32", 0, 0), (3000, 100000, 64, "i64", 3, 1), (16384, 900, 600, "i32", 0, 0),
          (16385, 2047, 128, "pair", 0, 0), (20001, 2048, 40, "i64", 0, 0), (60000, 70000, 9, "i32", 0, 0), (40000, 1, 24, "i64", 0, 0),
-         (30000, 5_000_000, 3, "i64", 0, 0), (1500, 40, 8200, "i32", 0, 0), (1024, 5, 1100, "i64", 7, 0)]
+         (30000, 5_000_000, 3, "i64", 0, 0), (1500, 40, 8200, "i32", 0, 0), (1024, 5, 1100, "i64", 7, 0),
+         (700, 50, 515, "i64", 0, 0), (6000, 300, 1031, "i32", 1, 1), (17_000, 900, 519, "i64", 0, 0)]  # a last part of few columns
 
 
 @gpu
