@@ -771,16 +771,14 @@ hipError_t by_type(int type, Run &&run) {
 
 // How a product of rows x outs over `cols` k's is cut: the way that is the shortest by what steps were measured to take.  Larger tiles ask
 // for fewer values (8192 x 4096 x 4096 in bfloat16: 214 us by tiles of 256, 256 by 128; 65536 x 512 x 2048 202, 227 and 413 by the small
-// ones), smaller ones are more workgroups (1000 x 1000 x 1000: 32, 22 and 10 us), and a long k is cut where there are few (a weight's
-// gradient of 65536 x 128 x 512: 50 us in 64 parts of 128 tiles, 203 in 8).  `more`: an epilogue with an activation or other matrices is as long as
-// several steps, and only where workgroups share a compute unit does another's product go on beside it (65536 x 512 x 2048 with gelu and
-// pre: 357 us by tiles of 256, 319 by 128).
+// ones; with bias, gelu and pre 242 and 275), smaller ones are more workgroups (1000 x 1000 x 1000: 32, 22 and 10 us), and a long k is cut where there are few (a weight's
+// gradient of 65536 x 128 x 512: 50 us in 64 parts of 128 tiles, 203 in 8).
 struct Cut {
     uint32_t tile, tiles_m, tiles_n, splits, split_k;
 };
 constexpr uint32_t kFewRows = 64;
 
-Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide, bool more) {
+Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide) {
     const uint64_t step = kStep / (type == GV_F32 ? 4 : 2), steps = std::max<uint64_t>(1, (cols + step - 1) / step);
     // tiles, workgroups that run at once, and what a step of theirs takes then, in microseconds
     struct Way {
@@ -796,7 +794,7 @@ Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide, boo
         for (uint64_t splits = 1; splits <= 64 && (splits == 1 || steps >= 4 * splits); splits *= 2) {
             const uint64_t each = (steps + splits - 1) / splits, cut = (steps + each - 1) / each;
             const double rounds = (double)(m * n * cut) / w.at_once, alone = 0.3 + 0.7 * std::min(1.0, rounds);
-            const double time = std::ceil(rounds) * ((double)each * w.each * alone + (more && w.m == 256 ? 12.0 : 3.0)) + (cut > 1 ? 4.0 + (double)(cut * rows * outs) * 2e-6 : 0.0);
+            const double time = std::ceil(rounds) * ((double)each * w.each * alone + 3.0) + (cut > 1 ? 4.0 + (double)(cut * rows * outs) * 2e-6 : 0.0);
             if (time < least) {
                 least = time;
                 best = {w.m, (uint32_t)m, (uint32_t)n, (uint32_t)cut, (uint32_t)(each * step)};
@@ -807,10 +805,10 @@ Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide, boo
 }
 uint64_t partial_of(const Cut &c, uint64_t rows, uint64_t outs) { return c.splits > 1 ? 4ull * c.splits * rows * outs : 0; }
 
-// of any alignment and epilogue
+// of any alignment
 uint64_t most_partial_of(uint64_t rows, uint64_t cols, uint64_t outs, int type) {
     uint64_t most = 0;
-    for (int i = 0; i < 4; ++i) most = std::max(most, partial_of(cut_of(rows, cols, outs, type, i % 2, i / 2), rows, outs));
+    for (int i = 0; i < 2; ++i) most = std::max(most, partial_of(cut_of(rows, cols, outs, type, i), rows, outs));
     return most;
 }
 
@@ -821,7 +819,7 @@ hipError_t product(DenseArgs a, void *workspace, hipStream_t stream) {
         return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && together % 8 == 0 && together > 0 && stride < kWideStride;
     };
     const bool wide = sizeof(T) == 2 && whole(a.x, a.x_stride, kAAlong ? a.cols : a.rows) && whole(a.weight, a.weight_stride, kBAlong ? a.cols : a.outs);
-    const Cut c = cut_of(a.rows, a.cols, a.outs, a.type, wide, a.act != GV_ACT_NONE || a.pre || a.residual);
+    const Cut c = cut_of(a.rows, a.cols, a.outs, a.type, wide);
     a.split_k = c.split_k;
     a.partial = c.splits > 1 ? (float *)workspace : nullptr;
     const uint32_t blocks = c.tiles_m * c.tiles_n * c.splits;
