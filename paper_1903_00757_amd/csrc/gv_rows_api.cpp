@@ -297,6 +297,7 @@ int gv_dense_rows(uint64_t rows, uint32_t cols, uint32_t outs, int type, const v
     if (dev_residual) GV_TRY(check_matrices(call, outs, {{"residual", dev_residual, residual_stride, type}}));
     if (dev_pre) GV_TRY(check_matrices(call, outs, {pre.matrix}));
     GV_TRY(check_apart(call, {out, pre}, {x, weight}));
+    GV_TRY(check_apart(call, {pre}, {out, {{"residual", dev_residual, residual_stride, type}, rows, outs}}));
     GV_TRY(check_workspace(call, dev_workspace, workspace_bytes, gv::dense_workspace(rows, cols, outs, type)));
     gv::DenseArgs a{};
     a.x = dev_x, a.weight = dev_weight, a.bias = dev_bias, a.residual = dev_residual, a.pre = dev_pre, a.out = dev_out;

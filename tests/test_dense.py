@@ -114,7 +114,9 @@ def test_refusals_need_no_device(gv):
                       (dict(weight=None), "null weight"), (dict(out=None), "null out"), (dict(x_stride=7), "stride"), (dict(weight_stride=7), "stride"),
                       (dict(out_stride=15), "stride"), (dict(bias=P(2)), "aligned"), (dict(residual=to, residual_stride=15), "stride"),
                       (dict(pre=P(1 << 35), pre_stride=15), "stride"), (dict(out=at), "overlaps x"), (dict(out=P((1 << 30) + 480)), "overlaps weight"),
-                      (dict(pre=at, pre_stride=16), "overlaps x"), (dict(cols=16384, outs=8, x_stride=16384, weight_stride=16384), "workspace")]:
+                      (dict(pre=at, pre_stride=16), "overlaps x"),
+                      (dict(pre=to, pre_stride=16), "pre overlaps out"), (dict(pre=P(1 << 35), pre_stride=16, residual=P(1 << 35), residual_stride=16), "overlaps residual"),
+                      (dict(cols=16384, outs=8, x_stride=16384, weight_stride=16384), "workspace")]:
         assert L.gv_dense_rows(*{**ok, **bad}.values()) == gv.GV_EINVAL, bad
         assert word in L.gv_last_error(None).decode(), (bad, L.gv_last_error(None))
     assert L.gv_dense_rows(*{**ok, "rows": 0, "x": None}.values()) == gv.GV_OK
@@ -132,6 +134,19 @@ def test_refusals_need_no_device(gv):
     with pytest.raises(gv.GvError):
         gv.gv_dense_rows_backward_workspace(1, 10, 10, gv.GV_F32, 9)
     assert gv.gv_dense_rows_workspace(16, 4096, 4096, gv.GV_BF16) == 0
+
+
+def test_products_keep_their_sums_in_registers(gv):
+    """The tiles on matrix instructions have all registers of a lane, and a spilled one would be read back in every step."""
+    from test_kernel_registers import code_objects, kernels_of
+
+    with open(gv.LIB_PATH, "rb") as f:
+        data = f.read()
+    found = {k[".name"]: k for elf in code_objects(data) for k in kernels_of(elf) if "k_product" in k[".name"] or "k_sum_runs" in k[".name"]}
+    assert len([n for n in found if "k_product_wide" in n]) == 2 * 2 * 3
+    for name, k in found.items():
+        if "k_product_wide" in name or "small" in name or "few" in name or "k_sum_runs" in name:
+            assert k[".vgpr_spill_count"] == 0 and k[".private_segment_fixed_size"] == 0, name
 
 
 @gpu

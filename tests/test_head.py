@@ -1,0 +1,111 @@
+"""The operators on rows together, as a head's training and a search use them: rows by index, a layer, their gradients and a step on the
+table; scores, their selection, and the paths that are reordered with it."""
+import importlib.util
+import os
+
+import numpy as np
+import pytest
+
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def gv():
+    import paper_1903_00757_amd as gv
+
+    if not os.path.exists(gv.LIB_PATH):
+        from paper_1903_00757_amd import build
+
+        build.build()
+    gv.load()
+    return gv
+
+
+@pytest.fixture(scope="module")
+def example():
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "answer_queries.py")
+    spec = importlib.util.spec_from_file_location("answer_queries", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+@gpu
+@pytest.mark.parametrize("places,nodes,cols,hidden", [(5, 40, 24, 16), (700, 300, 64, 96), (5000, 900, 33, 50)])
+def test_steps_of_training(gv, places, nodes, cols, hidden):
+    """Three steps of descent on a table, two layers and a norm's gain, against torch's autograd in 64 bits on the host.  Every sum here has at
+    most n = `places` terms and is off by 2 n 2^-24 of their sizes at worst; a step passes through eight such sums and moves a
+    parameter by a hundredth of its size, so three leave 3 * 8 * 2 n 2^-24 / 100 of it: the gate is ten times as wide for
+    gradients whose terms cancel, and never below fp32's own rounding of the parameters, 2^-22."""
+    import torch
+
+    rng = np.random.default_rng(places)
+    table = rng.standard_normal((nodes, cols))
+    w1, w2 = rng.standard_normal((hidden, cols)) / np.sqrt(cols), rng.standard_normal((cols, hidden)) / np.sqrt(hidden)
+    start = [table, w1, 0.1 * rng.standard_normal(hidden), w2, np.ones(cols)]
+    host = [torch.tensor(np.float32(a)).double().requires_grad_() for a in start]
+    dev = [torch.tensor(np.float32(a)).cuda() for a in start]
+    scale, rate = 1.5, 0.01
+    for step in range(3):
+        at = rng.integers(-1, nodes, places)
+        grad = rng.standard_normal((places, cols)) / np.sqrt(places)
+        t, a, b, c, g = host
+        named = torch.tensor(at >= 0).unsqueeze(1)
+        x = torch.where(named, t[torch.tensor(np.maximum(at, 0))] * scale, 0.0)
+        h = torch.nn.functional.gelu(x @ a.t() + b)
+        y = x + h @ c.t()
+        n = y / torch.sqrt((y * y).mean(1, keepdim=True) + 1e-6) * g
+        wrt = torch.autograd.grad((n * torch.tensor(np.float32(grad)).double()).sum(), host)
+        with torch.no_grad():
+            for p, q in zip(host, wrt):
+                p -= rate * q
+        T, A, B, C, G = dev
+        index, go = torch.tensor(at).cuda(), torch.tensor(np.float32(grad)).cuda()
+        x = gv.gv_lookup_rows(T, index, scale=scale)
+        first = gv.gv_dense_rows(x, A, B, act=gv.GV_ACT_GELU, keep_pre=True)
+        second = gv.gv_dense_rows(first.out, C, residual=x)
+        normed = gv.gv_norm_rows(second.out, G, keep_rstd=True)
+        gn = gv.gv_norm_rows_backward(go, second.out, G, normed.rstd)
+        g2 = gv.gv_dense_rows_backward(gn.x, first.out, C)
+        g1 = gv.gv_dense_rows_backward(g2.x, x, A, first.pre, act=gv.GV_ACT_GELU, keep_bias=True)
+        A -= rate * g1.weight
+        B -= rate * g1.bias
+        C -= rate * g2.weight
+        G -= rate * gn.gain
+        gv.gv_lookup_rows_backward(g1.x + gn.x, index, nodes, scale=-rate * scale, out=T, add=True)
+    gate = max(10 * 3 * 8 * 2 * places * 2.0 ** -24 / 100, 2.0 ** -22)
+    for got, want in zip(dev, host):
+        want = want.detach()
+        assert (got.double().cpu() - want).norm() <= gate * want.norm()
+
+
+@gpu
+@pytest.mark.parametrize("nodes,beams,steps", [(300, 4, 3), (3000, 3, 4), (2, 4, 2)])
+def test_paths(gv, example, nodes, beams, steps):
+    """The example's search against the same search in 64 bits over the same scores.  A step passes on fp32's rounding of the totals, 2^-24 of a
+    total below 40, and the sums' (|d| + 4) 2^-23.  Paths whose totals are no further apart than twice that may come in either order: of two
+    nodes that stay where they are nearly for certain, 0 0 1 and 0 1 1 differ by what p(0, 0) and p(1, 1) do, here 2e-11 of 25, where
+    fp32's totals have steps of 2e-6.  So each place has a path of its own, whose total in 64 bits is that of its place."""
+    import torch
+
+    rng = np.random.default_rng(nodes)
+    vertex, context = (torch.tensor(rng.standard_normal((nodes, 32)).astype(np.float32)).cuda() for _ in range(2))
+    gain = torch.ones(32, device="cuda")
+    table = gv.gv_quantize_rows(vertex, group=32)
+    some = torch.tensor(rng.integers(0, nodes, 3)).cuda()
+    paths, totals = example.follow(vertex, context, gain, table, some, steps, beams)
+    scores = example.scores_of(vertex, context, gain, table, torch.arange(nodes, device="cuda")).double().cpu().numpy()
+    logs = scores - scores.max(1, keepdims=True)
+    logs -= np.log(np.exp(logs).sum(1, keepdims=True))
+    for k, node in enumerate(some.tolist()):
+        known = [(0.0, (node,))]
+        for _ in range(steps):
+            every = [(t + logs[p[-1], i], p + (i,)) for t, p in known for i in range(nodes)]
+            known = sorted(every, key=lambda e: -e[0])[:beams]
+        off = steps * (40 * 2.0 ** -24 + 44 * 2.0 ** -23)
+        found = [tuple(p) for p in paths[k, :len(known)].tolist()]
+        assert len(set(found)) == len(found)
+        for path, (total, _) in zip(found, known):
+            assert path[0] == node and abs(sum(logs[a, b] for a, b in zip(path, path[1:])) - total) <= 2 * off
+        assert np.abs(totals[k, :len(known)].cpu().numpy() - np.array([t for t, _ in known])).max() <= off
+        assert (totals[k, len(known):] == -float("inf")).all()
