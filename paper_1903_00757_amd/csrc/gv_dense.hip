@@ -651,35 +651,43 @@ __global__ __launch_bounds__(256) void k_join_product(DenseArgs a, uint32_t spli
 
 // ---------------------------------------------------------------------------
 // Few rows of x: every value of the weight is read once, from memory straight into the matrix instruction's registers.  A workgroup takes
-// 16 columns of the result, its waves take steps of k in turn and are joined through LDS.
+// 16 columns of the result, its waves take lines of k (256 bytes of each row) in turn and are joined through LDS.  What is bound by memory
+// is so by what is asked for at once: whole lines are loaded without a check, eight pieces a lane ahead.
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
 
 template <class T, int kMs>
 __global__ __launch_bounds__(kFewThreads) void k_product_few(DenseArgs a) {
-    constexpr int N = kEach<T>, kAhead = 4;
+    constexpr int N = kEach<T>, kLine = 4, kAhead = kMs == 1 ? 8 : 4;
+    constexpr uint32_t kStride = kFewWaves * kLine * 4 * N;  // k's from a wave's line to its next
     __shared__ f4 joined[kFewWaves][kMs][64];
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = blockIdx.x * 16 + lane % 16;
-    const T *weight = (const T *)a.weight + std::min(n, a.outs - 1) * a.weight_stride;  // rows past the end are not used
-    f4 sums[kMs];
+    // rows past the ends are not used
+    const T *weight = (const T *)a.weight + std::min(n, a.outs - 1) * a.weight_stride + lane / 16 * N;
+    const T *x[kMs];
 #pragma unroll
-    for (int i = 0; i < kMs; ++i) sums[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t k = wave * 4 * N; k < a.cols; k += kAhead * kFewWaves * 4 * N) {
-        Values<T, N> w[kAhead], x[kAhead][kMs];
+    for (int i = 0; i < kMs; ++i) x[i] = (const T *)a.x + std::min(16 * i + lane % 16, a.rows - 1) * a.x_stride + lane / 16 * N;
+    f4 sums[kMs] = {};
+    const auto take = [&](auto whole, uint32_t first, auto number) {
+        constexpr int kNumber = decltype(number)::value;
+        Values<T, N> w[kNumber], v[kNumber][kMs];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const uint32_t at = k + u * kFewWaves * 4 * N + lane / 16 * N, left = left_of(at, a.cols);
-            w[u].load(weight + at, left);
+        for (int u = 0; u < kNumber; ++u) {
+            const uint32_t k = first + u / kLine * kStride + u % kLine * 4 * N;
+            const uint32_t left = decltype(whole)::value ? N : left_of(k + lane / 16 * N, a.cols);
+            w[u].load(weight + k, left);
 #pragma unroll
-            for (int i = 0; i < kMs; ++i) {
-                const uint32_t m = 16 * i + lane % 16;
-                x[u][i].load((const T *)a.x + m * a.x_stride + at, m < a.rows ? left : 0);
-            }
+            for (int i = 0; i < kMs; ++i) v[u][i].load(x[i] + k, left);
         }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
+        for (int u = 0; u < kNumber; ++u)
 #pragma unroll
-            for (int i = 0; i < kMs; ++i) multiply(__builtin_bit_cast(uint4, w[u]), __builtin_bit_cast(uint4, x[u][i]), sums[i], (T *)nullptr);
-    }
+            for (int i = 0; i < kMs; ++i) multiply(__builtin_bit_cast(uint4, w[u]), __builtin_bit_cast(uint4, v[u][i]), sums[i], (T *)nullptr);
+    };
+    uint32_t k = wave * (kLine * 4 * N);
+    for (; k + (kAhead / kLine - 1) * kStride + kLine * 4 * N <= a.cols; k += kAhead / kLine * kStride)
+        take(std::true_type(), k, std::integral_constant<int, kAhead>());
+    for (; k + kLine * 4 * N <= a.cols; k += kStride) take(std::true_type(), k, std::integral_constant<int, kLine>());
+    if (k < a.cols) take(std::false_type(), k, std::integral_constant<int, kLine>());
 #pragma unroll
     for (int i = 0; i < kMs; ++i) joined[wave][i][lane] = sums[i];
     __syncthreads();
@@ -707,19 +715,20 @@ __global__ __launch_bounds__(kSlopeThreads) void k_slope(DenseGradArgs a) {
     const bool used = 8 * lane < width && width * part + 8 * lane < a.outs;
     const uint32_t k = kWide ? std::min(width * part + 8 * lane, a.outs - 8) : width * part + 8 * lane, cols = kWide ? k + 8 : a.outs;
     const uint64_t first = (uint64_t)chunk * a.chunk, last = std::min<uint64_t>(a.rows, first + a.chunk);
+    constexpr int kAhead = 2;  // rows of a wave asked for at once (four: 112 us for 65536 x 2048 with the bias' gradient alone, 98 with two)
     float sums[8] = {};
     if (used) {
-        for (uint64_t row = first + wave; row < last; row += 2 * kSlopeWaves) {
-            Piece<T> g[2], z[2];
+        for (uint64_t row = first + wave; row < last; row += kAhead * kSlopeWaves) {
+            Piece<T> g[kAhead], z[kAhead];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < kAhead; ++h) {
                 const uint64_t at = row + h * kSlopeWaves;
                 if (at >= last) continue;
                 g[h].load((const T *)a.grad + at * a.grad_stride, k, cols);
                 if (a.act != GV_ACT_NONE) z[h].load((const T *)a.pre + at * a.pre_stride, k, cols);
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < kAhead; ++h) {
                 const uint64_t at = row + h * kSlopeWaves;
                 if (at >= last) continue;
                 float v[8];
