@@ -1,10 +1,11 @@
 // gfx950 kernels of a layer: out = residual + act(x weight^T + bias), and its gradients.
 //
-// All products are sums over k of A(m, k) B(n, k) on matrix instructions, with sums in fp32.  An operand lies with the values of one
-// row together (k runs along memory: x and weight in the forward pass), or with those of one k together (the gradients'
-// operands); the latter are transposed in registers on the way into LDS, so that there the tiles are all alike: rows of 128 bytes
-// of k, in eight pieces of 16 bytes, piece p of row r at place p ^ (r ^ r / 8) % 8.  Eight rows in a row then have a piece in eight
-// different places (what a matrix instruction's lanes read), and so have rows 4 i + j for eight i in a row (what is written transposed).
+// All products are sums over k of A(m, k) B(n, k) on matrix instructions, with sums in fp32.  An operand lies with the values
+// of one row together (k runs along memory: x and weight in the forward pass), or with those of one k together (the gradients'
+// operands); the latter are transposed in registers on the way into LDS, so that there the tiles are all alike: rows of 128
+// bytes of k, in eight pieces of 16 bytes, piece p of row r at place p ^ (r ^ r / 8) % 8.  Eight rows in a row then have a
+// piece in eight different places (what a matrix instruction's lanes read), and so have rows 4 i + j for eight i in a row (what
+// is written transposed).
 #include "gv_row_pieces.hpp"
 #include "gv_rows.hpp"
 #include "gvhot.h"
@@ -22,10 +23,10 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 
-// The normal distribution's Phi(z) and, on the way, exp(-z^2 / 2).  Phi(-|z|) = (a1 t + ... + a5 t^5) exp(-z^2 / 2) / 2 with
-// t = 1 / (1 + 0.3275911 |z| / sqrt 2) (the halves are in the numbers below): formula 7.1.26 of Abramowitz and Stegun's Handbook, within 1.5e-7 / 2 of the true value, which is a
-// unit of fp32 near 1; where Phi is small the factor exp(-z^2 / 2) keeps it so.  erff takes three times the instructions: 65536 x 512 x
-// 2048 with gelu took 520 us by it.
+// The normal distribution's Phi(z) and, on the way, exp(-z^2 / 2).  Phi(-|z|) = (a1 t + ... + a5 t^5) exp(-z^2 / 2) / 2 with t
+// = 1 / (1 + 0.3275911 |z| / sqrt 2) (the halves are in the numbers below): formula 7.1.26 of Abramowitz and Stegun's Handbook,
+// within 1.5e-7 / 2 of the true value, which is a unit of fp32 near 1; where Phi is small the factor exp(-z^2 / 2) keeps it so.
+// erff takes three times the instructions: 65536 x 512 x 2048 with gelu took 520 us by it.
 __device__ __forceinline__ float normal(float z, float &bell) {
     const float x = fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(x, 0.23164190f, 1.0f));
     bell = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
@@ -144,8 +145,8 @@ __device__ __forceinline__ void finish(const DenseArgs &a, uint32_t m, uint32_t 
 }
 
 // ---------------------------------------------------------------------------
-// Tiles of kTile x kTile, 2 kTile threads: eight or four waves side by side.  The next step's values are loaded into registers while this
-// step's are multiplied, and go to the other half of LDS.
+// Tiles of kTile x kTile, 2 kTile threads: eight or four waves side by side.  The next step's values are loaded into registers
+// while this step's are multiplied, and go to the other half of LDS.
 constexpr int kStep = 128;  // bytes of k
 
 template <class T>
@@ -264,8 +265,9 @@ __global__ __launch_bounds__(2 * kTile) void k_product(DenseArgs a, uint32_t til
 }
 
 // ---------------------------------------------------------------------------
-// Small products, of any type and alignment: tiles of 32 x 64, four waves with 16 x 32 of it each, so that there are many workgroups, and
-// values asked for three steps ahead, since a step's products take a quarter of what its loads take.
+// Small products, of any type and alignment: tiles of 32 x 64, four waves with 16 x 32 of it each, so that there are many
+// workgroups, and values asked for three steps ahead, since a step's products take a quarter of what its loads take (six make
+// no difference).  1021 x 357 x 500 in fp32: 10 us, where tiles of 64 x 64 and one step ahead took 25.
 constexpr int kSmallM = 32, kSmallN = 64, kSmallThreads = 256, kSmallAhead = 3;
 
 template <class T, int kRows, bool kAlong>
@@ -364,10 +366,12 @@ __global__ __launch_bounds__(kSmallThreads) void k_product_small(DenseArgs a, ui
 }
 
 // ---------------------------------------------------------------------------
-// The same for 16-bit types whose rows are whole pieces (of 8 values, aligned): a step's 64 k's go from memory straight into LDS, where
-// an operand lies as it does in memory, and what lies with the values of a k together is turned by the loads that transpose.
-// A wave's values of half a step are read while those of the half before are multiplied; one barrier a step says that the next
-// step has arrived and that this one's place is free for the step after that.
+// The same for 16-bit types whose rows are whole pieces (of 8 values, aligned): a step's 64 k's go from memory straight into
+// LDS, where an operand lies as it does in memory, and what lies with the values of a k together is turned by the loads that
+// transpose. A wave's values of half a step are read while those of the half before are multiplied; one barrier a step says
+// that the next step has arrived and that this one's place is free for the step after that.  8192 x 4096 x 4096 in bfloat16
+// with bias, gelu and residual 227 us, 1.21 PFLOP/s: the matrix units are busy for half of the compute units' cycles, LDS for a
+// fifth (a wave's 128 x 64 take 24 KB of reads a step for 2^20 products), and the epilogue goes on beside nothing.
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s4v LdsFour;
 typedef __attribute__((address_space(3))) void LdsAny;
@@ -375,9 +379,9 @@ typedef __attribute__((address_space(3))) void LdsAny;
 constexpr uint32_t kWide = 64;                 // k's of a step
 constexpr uint64_t kWideStride = 1ull << 21;   // a tile's rows lie within 2^31 bytes
 
-// kSpread: row 4 g + r of tile j of the matrix instruction is row 32 (j / 2) + 8 g + 4 (j % 2) + r of 64 rows, and tiles 4 to 7 are of the next
-// 64.  For B that leaves the lanes of group g with 8 columns of the result in a row, twice, and four of them write 64 bytes in a row
-// with each store; operands that are turned are read at fewer different addresses.
+// kSpread: row 4 g + r of tile j of the matrix instruction is row 32 (j / 2) + 8 g + 4 (j % 2) + r of 64 rows, and tiles 4 to 7
+// are of the next 64.  For B that leaves the lanes of group g with 8 columns of the result in a row, twice, and four of them
+// write 64 bytes in a row with each store; operands that are turned are read at fewer different addresses.
 template <int kTile, bool kAlong, bool kSpread>
 struct Operand {
     static constexpr uint32_t kThreads = 2 * kTile, kLoads = kTile * 128 / 16 / kThreads;
@@ -386,8 +390,8 @@ struct Operand {
     const char *at, *end;  // the tile's first value of the next step, and of the matrix behind its last
     uint64_t step, rows;   // bytes to the next step, and to the next rows
     uint32_t stride;       // values
-    // A piece's place: along k rows of 128 bytes, piece p of row r at p ^ turn(r); otherwise rows of kTile values of one k, piece p of
-    // row k at p ^ turn(k): what lanes read together lies in different banks.
+    // A piece's place: along k rows of 128 bytes, piece p of row r at p ^ turn(r); otherwise rows of kTile values of one k,
+    // piece p of row k at p ^ turn(k): what lanes read together lies in different banks.
     static __device__ __forceinline__ uint32_t turn(uint32_t row) {
         if constexpr (kAlong) return kSpread ? (row & 3) | (row >> 3 & 1) << 2 : row & 7;
         else return (row & 3) << 2;
@@ -427,8 +431,9 @@ struct Operand {
         for (uint32_t j = 0; j < kLoads; ++j, p += rows) {
             const uint32_t id = j * kThreads + threadIdx.x;
             const uint32_t k = kAlong ? (id % kLine ^ turn(id / kLine)) * 8 : id / kLine;
+            const char *piece = p + from(threadIdx.x);  // whole: 8 k's of a row, or 8 rows of a k
             uint4 v = {};
-            if (k < left && p + from(threadIdx.x) < end) __builtin_memcpy(&v, p + from(threadIdx.x), 16);  // whole pieces: 8 k's of a row, or 8 rows of a k
+            if (k < left && piece < end) __builtin_memcpy(&v, piece, 16);
             *(uint4 *)(tile + id * 16) = v;
         }
     }
@@ -562,9 +567,9 @@ __global__ __launch_bounds__(2 * kTile, 2) void k_product_wide(DenseArgs a, uint
         return end_m + (kAAlong ? 16 * i + end_lane % 16 : 64 * (i / 4) + 32 * (i % 4 / 2) + end_lane % 16 / 4 * 8 + 4 * (i % 2) + end_lane % 4);
     };
     const auto column_of = [&](int h) { return end_n + 32 * h + 8 * (end_lane / 16); };
-    // A whole tile without a check: bias is read once, and the residual's values are asked for a row ahead (what is written may be they, so the
-    // compiler leaves each load behind the stores before it).  A value that is read under a condition of its own is waited for on the
-    // way past it, and with it all stores before: 65536 x 512 x 2048 took 290 us instead of 200.
+    // A whole tile without a check: bias is read once, and the residual's values are asked for a row ahead (what is written may
+    // be they, so the compiler leaves each load behind the stores before it).  A value that is read under a condition of its
+    // own is waited for on the way past it, and with it all stores before: 65536 x 512 x 2048 took 290 us instead of 200.
     const auto whole_tile = [&](auto with) {
         constexpr bool kResidual = decltype(with)::value;
         float bias[2][8];
@@ -650,9 +655,10 @@ __global__ __launch_bounds__(256) void k_join_product(DenseArgs a, uint32_t spli
 }
 
 // ---------------------------------------------------------------------------
-// Few rows of x: every value of the weight is read once, from memory straight into the matrix instruction's registers.  A workgroup takes
-// 16 columns of the result, its waves take lines of k (256 bytes of each row) in turn and are joined through LDS.  What is bound by memory
-// is so by what is asked for at once: whole lines are loaded without a check, eight pieces a lane ahead.
+// Few rows of x: every value of the weight is read once, from memory straight into the matrix instruction's registers.  A
+// workgroup takes 16 columns of the result, its waves take lines of k (256 bytes of each row) in turn and are joined through
+// LDS.  What is bound by memory is so by what is asked for at once: whole lines are loaded without a check, eight pieces a lane
+// ahead.  16 x 4096 x 4096 in bfloat16: 11 us, 3.1 TB/s; with four pieces of 64 bytes each, checked, 16 us.
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
 
 template <class T, int kMs>
@@ -700,11 +706,14 @@ __global__ __launch_bounds__(kFewThreads) void k_product_few(DenseArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// gz = grad * slope(pre), and the sums over its rows: a lane has eight columns, a wave 512, the waves of a workgroup take rows in turn.
+// gz = grad * slope(pre), and the sums over its rows: a lane has eight columns, a wave 512, the waves of a workgroup take rows
+// in turn. 65536 x 2048 in bfloat16 with gelu: 185 us for 810 MB, 4.4 TB/s, the vector units busy for half of it; the bias'
+// gradient alone 98 us for 537.
 constexpr int kSlopeThreads = 256, kSlopeWaves = kSlopeThreads / 64;
 
-// Rows of eight columns and more (kWide) have no broken piece: the last one lies back so far that it is whole, and two lanes have the
-// columns that it shares with the one before, and the same of them.  A part has 512 columns, or 504 where the last would have fewer than eight.
+// Rows of eight columns and more (kWide) have no broken piece: the last one lies back so far that it is whole, and two lanes
+// have the columns that it shares with the one before, and the same of them.  A part has 512 columns, or 504 where the last
+// would have fewer than eight.
 __host__ __device__ __forceinline__ uint32_t part_of(uint32_t cols) { return cols > 512 && cols % 512 > 0 && cols % 512 < 8 ? 504 : 512; }
 
 template <class T, bool kWide>
@@ -778,10 +787,11 @@ hipError_t by_type(int type, Run &&run) {
     return run((_Float16 *)nullptr);
 }
 
-// How a product of rows x outs over `cols` k's is cut: the way that is the shortest by what steps were measured to take.  Larger tiles ask
-// for fewer values (8192 x 4096 x 4096 in bfloat16: 214 us by tiles of 256, 256 by 128; 65536 x 512 x 2048 202, 227 and 413 by the small
-// ones; with bias, gelu and pre 242 and 275), smaller ones are more workgroups (1000 x 1000 x 1000: 32, 22 and 10 us), and a long k is cut where there are few (a weight's
-// gradient of 65536 x 128 x 512: 50 us in 64 parts of 128 tiles, 203 in 8).
+// How a product of rows x outs over `cols` k's is cut: the way that is the shortest by what steps were measured to take.
+// Larger tiles ask for fewer values (8192 x 4096 x 4096 in bfloat16: 214 us by tiles of 256, 256 by 128; 65536 x 512 x 2048
+// 202, 227 and 413 by the small ones; with bias, gelu and pre 242 and 275), smaller ones are more workgroups (1000 x 1000 x
+// 1000: 32, 22 and 10 us), and a long k is cut where there are few (a weight's gradient of 65536 x 128 x 512: 50 us in 64 parts
+// of 128 tiles, 203 in 8).
 struct Cut {
     uint32_t tile, tiles_m, tiles_n, splits, split_k;
 };
@@ -795,7 +805,9 @@ Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide) {
         double at_once, each;
     };
     const bool f32 = type == GV_F32;
-    const Way ways[3] = {{256, 256, 256, f32 ? 7.5 : wide ? 2.1 : 5.0}, {128, 128, 512, f32 ? 4.0 : wide ? 1.2 : 2.6}, {kSmallM, kSmallN, 1024, f32 ? 1.0 : 0.8}};
+    const Way ways[3] = {{256, 256, 256, f32 ? 7.5 : wide ? 2.1 : 5.0},
+                         {128, 128, 512, f32 ? 4.0 : wide ? 1.2 : 2.6},
+                         {kSmallM, kSmallN, 1024, f32 ? 1.0 : 0.8}};
     Cut best{};
     double least = 1e300;
     for (const Way &w : ways) {
@@ -803,7 +815,8 @@ Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide) {
         for (uint64_t splits = 1; splits <= 64 && (splits == 1 || steps >= 4 * splits); splits *= 2) {
             const uint64_t each = (steps + splits - 1) / splits, cut = (steps + each - 1) / each;
             const double rounds = (double)(m * n * cut) / w.at_once, alone = 0.3 + 0.7 * std::min(1.0, rounds);
-            const double time = std::ceil(rounds) * ((double)each * w.each * alone + 3.0) + (cut > 1 ? 4.0 + (double)(cut * rows * outs) * 2e-6 : 0.0);
+            const double join = cut > 1 ? 4.0 + (double)(cut * rows * outs) * 2e-6 : 0.0;
+            const double time = std::ceil(rounds) * ((double)each * w.each * alone + 3.0) + join;
             if (time < least) {
                 least = time;
                 best = {w.m, (uint32_t)m, (uint32_t)n, (uint32_t)cut, (uint32_t)(each * step)};
@@ -827,7 +840,8 @@ hipError_t product(DenseArgs a, void *workspace, hipStream_t stream) {
     const auto whole = [](const void *p, uint64_t stride, uint64_t together) {
         return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && together % 8 == 0 && together > 0 && stride < kWideStride;
     };
-    const bool wide = sizeof(T) == 2 && whole(a.x, a.x_stride, kAAlong ? a.cols : a.rows) && whole(a.weight, a.weight_stride, kBAlong ? a.cols : a.outs);
+    const bool wide = sizeof(T) == 2 && whole(a.x, a.x_stride, kAAlong ? a.cols : a.rows) &&
+                      whole(a.weight, a.weight_stride, kBAlong ? a.cols : a.outs);
     const Cut c = cut_of(a.rows, a.cols, a.outs, a.type, wide);
     a.split_k = c.split_k;
     a.partial = c.splits > 1 ? (float *)workspace : nullptr;
@@ -902,7 +916,9 @@ hipError_t launch_dense_grad(const DenseGradArgs &args, void *workspace, hipStre
         a.bias_partial = a.grad_bias ? (float *)((char *)workspace + p.bias) : nullptr;
         void *space = (char *)workspace + p.product;
         hipError_t e = hipSuccess;
-        if ((a.gz || a.grad_bias) && a.rows > 0) e = launch(a.outs >= 8 ? k_slope<T, true> : k_slope<T, false>, p.chunks * ((a.outs + part_of(a.outs) - 1) / part_of(a.outs)), kSlopeThreads, 0, stream, a);
+        const uint32_t slope_blocks = p.chunks * ((a.outs + part_of(a.outs) - 1) / part_of(a.outs));
+        if ((a.gz || a.grad_bias) && a.rows > 0)
+            e = launch(a.outs >= 8 ? k_slope<T, true> : k_slope<T, false>, slope_blocks, kSlopeThreads, 0, stream, a);
         if (e == hipSuccess && a.grad_bias) e = launch(k_join_bias<T>, (a.outs + 31) / 32, 1024, 0, stream, a, p.chunks);
         const void *gz = a.gz ? a.gz : a.grad;
         const uint64_t gz_stride = a.gz ? a.outs : a.grad_stride;

@@ -1,5 +1,5 @@
-// Device functions of the kernels on rows (gv_rows.hip, gv_scores.hip): pieces of eight columns, and what the lanes of a
-// row share.
+// Device functions of the kernels on rows (gv_rows.hip, gv_scores.hip, gv_lookup.hip, gv_dense.hip, gv_select.hip): pieces of eight
+// columns, and what the lanes of a row share.
 #pragma once
 
 #include <hip/hip_runtime.h>

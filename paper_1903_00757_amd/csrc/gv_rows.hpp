@@ -1,6 +1,5 @@
-// Internal interface between the checks of the operators on rows (gv_rows_api.cpp) and their kernels
-// (gv_rows.hip, gv_scores.hip, gv_lookup.hip, gv_dense.hip,
-// gv_select.hip).  Not part of the C boundary.
+// Internal interface between the checks of the operators on rows (gv_rows_api.cpp) and their kernels (gv_rows.hip, gv_scores.hip,
+// gv_lookup.hip, gv_dense.hip, gv_select.hip).  Not part of the C boundary.
 #pragma once
 
 #include <hip/hip_runtime.h>

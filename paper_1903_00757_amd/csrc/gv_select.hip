@@ -1,8 +1,9 @@
 // gfx950 kernels of the selection of the best rows over the scores of beams.
 //
-// A score s of beam b counts total[b] + (s - M) - log sum exp(s' - M), M the largest of the beam (or total[b] + s).  Within a beam
-// that is the order of the scores, so one pass over them is enough: every workgroup reads a part of a beam, keeps what may be among its best
-// in LDS and adds up the exponentials; a workgroup of each group joins the sums, and ranks what is left of the beams by what it counts.
+// A score s of beam b counts total[b] + (s - M) - log sum exp(s' - M), M the largest of the beam (or total[b] + s).  Within a
+// beam that is the order of the scores, so one pass over them is enough: every workgroup reads a part of a beam, keeps what may
+// be among its best in LDS and adds up the exponentials; a workgroup of each group joins the sums, and ranks what is left of
+// the beams by what it counts.
 //
 // What may be among the best is told by a bound, a value that at least `best` scores seen so far reach.  The largest score of each
 // thread is one of them, and in a wave the k-th largest of its lanes' takes 32 steps of a ballot: with every wave's
@@ -67,8 +68,8 @@ __device__ __forceinline__ uint32_t kth_of_lanes(const uint32_t (&x)[kOf], uint3
     return found;
 }
 
-// A bound that `best` of a workgroup's numbers reach: by every wave's ceil(best / waves)-th, or by the best-th of one wave.  A few are
-// looked for among the threads' largest, many among all kOf numbers of each.
+// A bound that `best` of a workgroup's numbers reach: by every wave's ceil(best / waves)-th, or by the best-th of one wave.  A
+// few are looked for among the threads' largest, many among all kOf numbers of each.
 template <int kWavesOf, int kOf>
 __device__ __forceinline__ uint32_t bound_of_threads(const uint32_t (&x)[kOf], uint32_t best, uint32_t (*scratch)[kWavesOf]) {
     const uint32_t wave = threadIdx.x / 64, each = (best + kWavesOf - 1) / kWavesOf;
@@ -158,7 +159,8 @@ __device__ __forceinline__ uint32_t block_count(const bool (&x)[kOf], uint32_t (
     for (int w = 0; w < kWavesOf; ++w) all += scratch[w];
     return all;
 }
-// A number that exactly the k largest of a workgroup's reach, unless several equal the k-th: then that.  0 is none; there are k others.
+// A number that exactly the k largest of a workgroup's reach, unless several equal the k-th: then that.  0 is none; there are k
+// others.
 template <int kWavesOf, int kOf>
 __device__ __forceinline__ uint64_t block_kth(const uint64_t (&x)[kOf], uint32_t k, SearchShared<kWavesOf> &s) {
     uint64_t one = 0, differ = 0;
@@ -217,8 +219,9 @@ __device__ __forceinline__ float narrow(Shared &s, uint32_t n, uint32_t best) {
     return value_of((uint32_t)(found >> 32));
 }
 
-// A turn with more candidates than there is room for: `kept` of the turns before, and the turn's scores that reach `least`, two of each thread at
-// a time, narrowed whenever the next may not fit.  Returns how many are kept; `bound` is raised to what `best` of them reach.
+// A turn with more candidates than there is room for: `kept` of the turns before, and the turn's scores that reach `least`, two
+// of each thread at a time, narrowed whenever the next may not fit.  Returns how many are kept; `bound` is raised to what
+// `best` of them reach.
 template <class T>
 __device__ __forceinline__ uint32_t take_slowly(Shared &s, uint32_t kept, uint32_t best, const T *scores, uint32_t first, uint32_t end, float least,
                                                 float &bound) {
@@ -265,7 +268,9 @@ __device__ __forceinline__ void put(const SelectArgs &a, uint64_t group, uint32_
     a.total[at] = (float)total;
 }
 
-// One part of one beam.  kAlone: groups of one beam in one part are finished here.
+// One part of one beam.  kAlone: groups of one beam in one part are finished here.  64 x 10^6 floats, best 1: 43 us, 6 TB/s;
+// best 100: 60, for the search of the bound and the candidates of the first turns; 128 x 10^6 with softmax 104 us, 4.9 TB/s,
+// the vector units busy for half of it.
 template <class T, bool kLog, bool kAlone>
 __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
     __shared__ Shared s;
@@ -403,7 +408,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
     }
 }
 
-// --- the beams of a group joined
+// --- the beams of a group joined: one workgroup for each, as long as its few dependent loads and searches take (12 to 23 us)
 constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / 64;
 constexpr uint32_t kJoinSlots = 2 * kJoinThreads, kMostLists = 2048, kMostBeams = GV_MAX_BEAMS;
 static_assert(GV_MAX_BEST + kJoinThreads <= kJoinSlots, "room for the best and a turn");
@@ -424,7 +429,8 @@ __device__ __forceinline__ uint64_t ordered(double x) {
     return bits ^ (bits >> 63 ? ~0ull : 1ull << 63);
 }
 
-// Leaves the `best` first of n candidates (n > best): by total; of those that equal the last one by beam and score; of those by row.
+// Leaves the `best` first of n candidates (n > best): by total; of those that equal the last one by beam and score; of those by
+// row.
 __device__ __forceinline__ void narrow(JoinShared &s, uint32_t n, uint32_t best) {
     double total[2];
     float score[2];
@@ -657,9 +663,9 @@ __global__ __launch_bounds__(kJoinThreads) void k_select_join(SelectArgs a) {
     for (uint32_t r = n + tid; r < a.best; r += kJoinThreads) put_none(a, group, r);
 }
 
-// How scores are cut: parts of whole turns, so many that a thousand workgroups are at work, but no more than leave the join with
-// candidates that its registers hold (some 1.3 `best` a part; one query, 4 x 10^6 scores, best 100: 245 parts took 99 us), as far as the
-// chip is filled once.
+// How scores are cut: parts of whole turns, so many that a thousand workgroups are at work, but no more than leave the join
+// with candidates that its registers hold (some 1.3 `best` a part; one query, 4 x 10^6 scores, best 100: 245 parts took 99 us),
+// as far as the chip is filled once.
 struct Cut {
     uint32_t parts, part_rows, slots;
     bool alone;
@@ -668,7 +674,8 @@ Cut cut_of(uint64_t queries, uint64_t rows, uint32_t beams, uint32_t best) {
     constexpr uint64_t kWanted = 1024;
     const uint64_t tiles = std::max<uint64_t>(1, (rows + kTile - 1) / kTile);
     uint64_t parts = std::min<uint64_t>(tiles, std::max<uint64_t>(1, kWanted / queries));
-    parts = std::min<uint64_t>(parts, std::max<uint64_t>({1, 3 * kJoinThreads / ((uint64_t)best * beams), std::min<uint64_t>(32, kWanted / 2 / queries)}));
+    const uint64_t held = 3 * kJoinThreads / ((uint64_t)best * beams), filled = std::min<uint64_t>(32, kWanted / 2 / queries);
+    parts = std::min<uint64_t>(parts, std::max<uint64_t>({1, held, filled}));
     parts = std::min<uint64_t>(parts, kMostLists / beams);
     const uint64_t each = (tiles + parts - 1) / parts;
     parts = (tiles + each - 1) / each;

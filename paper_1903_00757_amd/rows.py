@@ -3,9 +3,9 @@ from the tensors, results that the caller does not pass are allocated, and the k
 of the tensors' GPU.  Rows are 2-D tensors whose last dimension is contiguous; their rows may lie further apart.
 No arithmetic happens here.
 
-The calls record no graph for autograd: gradients are calls of their own (gv_norm_rows_backward; dropout's is dropout).  So
-where gradients are enabled and a tensor of a floating result asks for one, a call refuses: it belongs under torch.no_grad(), or
-takes detached tensors.  Codes, of 8-bit rows and of tables, are constants.
+The calls record no graph for autograd: gradients are calls of their own (gv_norm_rows_backward, gv_lookup_rows_backward,
+gv_dense_rows_backward; dropout's is dropout).  So where gradients are enabled and a tensor of a floating result asks for one, a
+call refuses: it belongs under torch.no_grad(), or takes detached tensors.  Codes, of 8-bit rows and of tables, are constants.
 """
 from __future__ import annotations
 
@@ -70,7 +70,7 @@ def _refuse(text):
 def _without_graph(*tensors):
     if any(t is not None and t.requires_grad for t in tensors):
         _refuse("no graph is recorded here, and a tensor asks for gradients: call under torch.no_grad() or pass it detached "
-                "(gradients are calls of their own: gv_norm_rows_backward, gv_drop_rows)")
+                "(gradients are calls of their own: gv_norm_rows_backward, gv_drop_rows, gv_lookup_rows_backward, gv_dense_rows_backward)")
 
 
 # A call that finds its kernel's launch waiting for nothing is as long as the host takes for it, 3.5 us of which are the launch:

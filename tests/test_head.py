@@ -109,3 +109,37 @@ def test_paths(gv, example, nodes, beams, steps):
             assert path[0] == node and abs(sum(logs[a, b] for a, b in zip(path, path[1:])) - total) <= 2 * off
         assert np.abs(totals[k, :len(known)].cpu().numpy() - np.array([t for t, _ in known])).max() <= off
         assert (totals[k, len(known):] == -float("inf")).all()
+
+
+@gpu
+def test_calls_on_two_streams_at_once(gv):
+    """The same calls on two streams, nothing waited for in between, give what they give alone: each has a workspace of its own."""
+    import torch
+
+    def work(seed):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        rand = lambda *shape: torch.randn(*shape, device="cuda", generator=gen)  # noqa: E731
+        table, weight, scores = rand(20_000, 96), rand(200, 96), rand(12, 150_000)
+        index = torch.randint(-1, 20_000, (30_000,), device="cuda", generator=gen)
+        return table, weight, scores, index
+
+    def calls(table, weight, scores, index):
+        x = gv.gv_lookup_rows(table, index)
+        got = gv.gv_dense_rows(x, weight, act=gv.GV_ACT_SILU, keep_pre=True)
+        grads = gv.gv_dense_rows_backward(got.out, x, weight, got.pre, act=gv.GV_ACT_SILU, keep_bias=True)
+        back = gv.gv_lookup_rows_backward(grads.x, index, 20_000)
+        best = gv.gv_select_rows(scores, 40, beams=4)
+        return [got.out, grads.weight, grads.bias, back, best.parent, best.row, best.total]
+
+    inputs = [work(1), work(2)]
+    alone = [calls(*i) for i in inputs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        together = [None, None]
+        for k, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                together[k] = calls(*inputs[k])
+        torch.cuda.synchronize()
+        for got, want in zip(together, alone):
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
