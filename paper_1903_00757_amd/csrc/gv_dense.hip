@@ -795,7 +795,7 @@ hipError_t by_type(int type, Run &&run) {
 struct Cut {
     uint32_t tile, tiles_m, tiles_n, splits, split_k;
 };
-constexpr uint32_t kFewRows = 64;
+constexpr uint32_t kFewRows = 64, kMostTogether = 1u << 30;
 
 Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide) {
     const uint64_t step = kStep / (type == GV_F32 ? 4 : 2), steps = std::max<uint64_t>(1, (cols + step - 1) / step);
@@ -837,6 +837,17 @@ uint64_t most_partial_of(uint64_t rows, uint64_t cols, uint64_t outs, int type) 
 template <class T, bool kAAlong, bool kBAlong>
 hipError_t product(DenseArgs a, void *workspace, hipStream_t stream) {
     if (a.rows == 0 || a.outs == 0) return hipSuccess;
+    if (kAAlong && a.rows > kMostTogether) {  // so many tiles that a launch would have 2^32 threads; k is never cut there
+        const uint32_t first = a.rows / 2;
+        DenseArgs rest = a;
+        const auto behind = [&](auto *&p, uint64_t stride) {
+            if (p) p = (T *)p + first * stride;
+        };
+        behind(rest.x, a.x_stride), behind(rest.residual, a.residual_stride), behind(rest.pre, a.pre_stride), behind(rest.out, a.out_stride);
+        rest.rows -= first, a.rows = first;
+        const hipError_t e = product<T, kAAlong, kBAlong>(a, workspace, stream);
+        return e != hipSuccess ? e : product<T, kAAlong, kBAlong>(rest, workspace, stream);
+    }
     const auto whole = [](const void *p, uint64_t stride, uint64_t together) {
         return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && together % 8 == 0 && together > 0 && stride < kWideStride;
     };

@@ -323,6 +323,23 @@ def test_far_offsets(gv):
 
 
 @gpu
+def test_as_many_rows_as_there_may_be(gv):
+    """2^31 rows of one column, of whole numbers: what is rounded is exact in fp32, here and there."""
+    import torch
+
+    rows, piece = 1 << 31, 1 << 20
+    x = torch.arange(piece, device="cuda").remainder(251).to(torch.bfloat16).repeat(rows // piece).view(rows, 1)
+    w = torch.full((1, 1), 2.0, dtype=torch.bfloat16, device="cuda")
+    out = gv.gv_dense_rows(x, w, residual=x, act=gv.GV_ACT_RELU).out
+    assert all(torch.equal(o, 3 * i) for o, i in zip(out.chunk(64), x.chunk(64)))
+    out.zero_()
+    out[rows - 1], out[rows // 2], out[5] = 1.0, 2.0, 4.0
+    grads = gv.gv_dense_rows_backward(out, x, w, keep_weight=False, keep_bias=True)
+    assert grads.bias.item() == 7.0 and sum(int(g.count_nonzero()) for g in grads.x.chunk(64)) == 3
+    assert [grads.x[i, 0].item() for i in (5, rows // 2, rows - 1)] == [8.0, 4.0, 2.0]
+
+
+@gpu
 @pytest.mark.parametrize("rows", [7, 300, 3000])
 def test_captured_and_replayed(gv, rows):
     import torch
