@@ -282,6 +282,21 @@ def test_far_offsets(gv):
 
 
 @gpu
+def test_as_many_places_as_there_may_be(gv):
+    """2^31 places: ones, whose sums stay below 2^24, so fp32 holds them."""
+    import torch
+
+    count, rows = 1 << 31, 1000
+    index = torch.arange(count, dtype=torch.int32, device="cuda").remainder_(rows)
+    table = torch.arange(rows, device="cuda").remainder(251).to(torch.bfloat16).view(rows, 1)
+    out = gv.gv_lookup_rows(table, index)
+    assert all(torch.equal(o, table[i]) for o, i in zip(out.chunk(64), index.chunk(64)))
+    out.fill_(1)
+    grad = gv.gv_lookup_rows_backward(out, index, rows, out_type=torch.float32)
+    assert torch.equal(grad, torch.full((rows, 1), float(count // rows), device="cuda") + (torch.arange(rows, device="cuda").view(-1, 1) < count % rows))
+
+
+@gpu
 @pytest.mark.parametrize("count", [500, 5000, 50_000])
 def test_captured_and_replayed(gv, count):
     """Replays with other inputs, eager work in between, two graphs at once and another stream than the default."""

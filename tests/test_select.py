@@ -255,6 +255,23 @@ def test_far_offsets(gv):
 
 
 @gpu
+@pytest.mark.parametrize("log", [False, True])
+def test_as_many_rows_as_there_may_be(gv, log):
+    """2^31 rows, the last of which is the best; of the equal ones the lowest."""
+    import torch
+
+    rows = 1 << 31
+    s = torch.zeros(1, rows, dtype=torch.bfloat16, device="cuda")
+    s[0, rows - 1], s[0, rows // 2] = 4.0, 3.0
+    done = torch.zeros(1, dtype=torch.bool, device="cuda")
+    got = gv.gv_select_rows(s, 4, done=done, end=rows - 1, log_softmax=log)
+    assert got.row.tolist() == [[rows - 1, rows // 2, 0, 1]] and got.parent.tolist() == [[0, 0, 0, 0]]
+    assert log or got.total.tolist() == [[4.0, 3.0, 0.0, 0.0]]
+    got = gv.gv_select_rows(s, 2, done=~done, end=rows - 1, totals=torch.tensor([-2.5], device="cuda"), log_softmax=log)
+    assert got.row.tolist() == [[rows - 1, -1]] and got.total.tolist() == [[-2.5, -np.inf]]
+
+
+@gpu
 @pytest.mark.parametrize("rows", [3000, 200_000])
 def test_captured_and_replayed(gv, rows):
     """A step of a search, with the states reordered, replayed on other scores; eager work and another stream in between."""
