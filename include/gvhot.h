@@ -457,10 +457,11 @@ int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t inde
 
 /* A layer: z = x weight^T + bias, out = residual + act(z); x has cols columns, weight outs rows of cols, bias outs values, and residual,
  * pre and out have outs columns, all of `type` (GV_F32, GV_BF16, GV_F16).  bias, residual and pre may be NULL; pre receives z, which
- * the backward pass takes.  GV_ACT_GELU is z (1 + erf(z / sqrt 2)) / 2, GV_ACT_SILU z / (1 + exp(-z)).  Sums are fp32 in an order that
- * sizes, type, strides and alignment decide, act is taken of the sum, and a result is rounded once.  out may be residual itself; else neither
- * out nor pre may overlap x, weight or each other, nor pre the residual.  1 <= outs <= GV_MAX_ROW_COLS.  dev_workspace points to workspace_bytes bytes (at least those of
- * gv_dense_rows_workspace, which may be none; aligned to 16) that the call may overwrite.                               */
+ * the backward pass takes.  GV_ACT_GELU is z (1 + erf(z / sqrt 2)) / 2, its second factor to within 4e-7, GV_ACT_SILU z / (1 + exp(-z)).
+ * Sums are fp32 in an order that sizes, type, strides and alignment decide, act is taken of the sum, and a result is rounded once.
+ * out may be residual itself; else neither out nor pre may overlap x, weight or each other, nor pre the residual.  1 <= outs <=
+ * GV_MAX_ROW_COLS.  dev_workspace points to workspace_bytes bytes (at least those of gv_dense_rows_workspace, which may be none;
+ * aligned to 16) that the call may overwrite.                                                                          */
 enum { GV_ACT_NONE = 0, GV_ACT_RELU = 1, GV_ACT_GELU = 2, GV_ACT_SILU = 3 };
 int gv_dense_rows_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, uint64_t *bytes);
 int gv_dense_rows(uint64_t rows, uint32_t cols, uint32_t outs, int type, const void *dev_x, uint64_t x_stride, const void *dev_weight,

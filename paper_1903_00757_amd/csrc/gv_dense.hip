@@ -25,7 +25,8 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 
 // The normal distribution's Phi(z) and, on the way, exp(-z^2 / 2).  Phi(-|z|) = (a1 t + ... + a5 t^5) exp(-z^2 / 2) / 2 with t
 // = 1 / (1 + 0.3275911 |z| / sqrt 2) (the halves are in the numbers below): formula 7.1.26 of Abramowitz and Stegun's Handbook,
-// within 1.5e-7 / 2 of the true value, which is a unit of fp32 near 1; where Phi is small the factor exp(-z^2 / 2) keeps it so.
+// within 1.5e-7 / 2 of the true value, and 2.9e-7 with the roundings of these steps (4 x 10^6 values from -12 to 12); z Phi(z) is
+// off by 3.1e-7 at most, since the factor exp(-z^2 / 2) makes the error small where z is large.
 // erff takes three times the instructions: 65536 x 512 x 2048 with gelu took 520 us by it.
 __device__ __forceinline__ float normal(float z, float &bell) {
     const float x = fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(x, 0.23164190f, 1.0f));
