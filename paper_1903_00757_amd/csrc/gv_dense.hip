@@ -796,7 +796,7 @@ hipError_t by_type(int type, Run &&run) {
 struct Cut {
     uint32_t tile, tiles_m, tiles_n, splits, split_k;
 };
-constexpr uint32_t kFewRows = 64, kMostTogether = 1u << 30;
+constexpr uint32_t kFewRows = 64;
 
 Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide) {
     const uint64_t step = kStep / (type == GV_F32 ? 4 : 2), steps = std::max<uint64_t>(1, (cols + step - 1) / step);
@@ -838,7 +838,16 @@ uint64_t most_partial_of(uint64_t rows, uint64_t cols, uint64_t outs, int type) 
 template <class T, bool kAAlong, bool kBAlong>
 hipError_t product(DenseArgs a, void *workspace, hipStream_t stream) {
     if (a.rows == 0 || a.outs == 0) return hipSuccess;
-    if (kAAlong && a.rows > kMostTogether) {  // so many tiles that a launch would have 2^32 threads; k is never cut there
+    const auto whole = [](const void *p, uint64_t stride, uint64_t together) {
+        return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && together % 8 == 0 && together > 0 && stride < kWideStride;
+    };
+    const bool wide = sizeof(T) == 2 && whole(a.x, a.x_stride, kAAlong ? a.cols : a.rows) &&
+                      whole(a.weight, a.weight_stride, kBAlong ? a.cols : a.outs);
+    const Cut c = cut_of(a.rows, a.cols, a.outs, a.type, wide);
+    const uint32_t threads = c.tile == 256 ? 512 : 256;  // of all three ways
+    static_assert(kSmallThreads == 256, "as many as of a tile of 128");
+    const uint64_t blocks = (uint64_t)c.tiles_m * c.tiles_n * c.splits;
+    if (kAAlong && blocks * threads > 0xFFFFFFFFull) {  // more than a launch takes: two halves; k is never cut where tiles are so many
         const uint32_t first = a.rows / 2;
         DenseArgs rest = a;
         const auto behind = [&](auto *&p, uint64_t stride) {
@@ -849,23 +858,16 @@ hipError_t product(DenseArgs a, void *workspace, hipStream_t stream) {
         const hipError_t e = product<T, kAAlong, kBAlong>(a, workspace, stream);
         return e != hipSuccess ? e : product<T, kAAlong, kBAlong>(rest, workspace, stream);
     }
-    const auto whole = [](const void *p, uint64_t stride, uint64_t together) {
-        return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && together % 8 == 0 && together > 0 && stride < kWideStride;
-    };
-    const bool wide = sizeof(T) == 2 && whole(a.x, a.x_stride, kAAlong ? a.cols : a.rows) &&
-                      whole(a.weight, a.weight_stride, kBAlong ? a.cols : a.outs);
-    const Cut c = cut_of(a.rows, a.cols, a.outs, a.type, wide);
     a.split_k = c.split_k;
     a.partial = c.splits > 1 ? (float *)workspace : nullptr;
-    const uint32_t blocks = c.tiles_m * c.tiles_n * c.splits;
-    const auto run = [&](auto kernel, uint32_t threads) { return launch(kernel, blocks, threads, 0, stream, a, c.tiles_m, c.tiles_n); };
+    const auto run = [&](auto kernel) { return launch(kernel, (uint32_t)blocks, threads, 0, stream, a, c.tiles_m, c.tiles_n); };
     hipError_t e = hipSuccess;
     if (c.tile == kSmallM) {
-        e = run(k_product_small<T, kAAlong, kBAlong>, kSmallThreads);
+        e = run(k_product_small<T, kAAlong, kBAlong>);
     } else if (!wide) {
-        e = c.tile == 256 ? run(k_product<T, 256, kAAlong, kBAlong>, 512) : run(k_product<T, 128, kAAlong, kBAlong>, 256);
+        e = c.tile == 256 ? run(k_product<T, 256, kAAlong, kBAlong>) : run(k_product<T, 128, kAAlong, kBAlong>);
     } else if constexpr (sizeof(T) == 2) {
-        e = c.tile == 256 ? run(k_product_wide<T, 256, kAAlong, kBAlong>, 512) : run(k_product_wide<T, 128, kAAlong, kBAlong>, 256);
+        e = c.tile == 256 ? run(k_product_wide<T, 256, kAAlong, kBAlong>) : run(k_product_wide<T, 128, kAAlong, kBAlong>);
     }
     if (e != hipSuccess || c.splits == 1) return e;
     const uint64_t pieces = (uint64_t)a.rows * ((a.outs + 3) / 4);

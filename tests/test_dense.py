@@ -340,6 +340,22 @@ def test_as_many_rows_as_there_may_be(gv):
 
 
 @gpu
+def test_many_rows_of_few_results(gv):
+    """More tiles of 32 x 64 than one launch takes, of whole numbers: every sum is exact."""
+    import torch
+
+    rows, cols, piece = (1 << 29) + 3, 33, 1 << 16
+    some = torch.randint(-3, 4, (piece, cols), device="cuda").float()
+    x, w = some.repeat(rows // piece + 1, 1)[:rows], torch.arange(1.0, cols + 1, device="cuda").view(1, cols)
+    want = product(torch, some.double(), w.double()).float()
+    out = gv.gv_dense_rows(x, w, residual=x[:, 5:6]).out
+    want += some[:, 5:6]
+    assert all(torch.equal(o, want[:o.shape[0]]) for o in out.split(piece))
+    grads = gv.gv_dense_rows_backward(out, x, w, keep_weight=False)
+    assert all(torch.equal(g, want[:g.shape[0]] * w) for g in grads.x.split(piece))
+
+
+@gpu
 @pytest.mark.parametrize("rows", [7, 300, 3000])
 def test_captured_and_replayed(gv, rows):
     import torch
