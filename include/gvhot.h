@@ -486,7 +486,7 @@ int gv_dense_rows_backward(uint64_t rows, uint32_t cols, uint32_t outs, int type
  *   totals[b] + scores[b][i] - log sum over i' of exp(scores[b][i'])    (log_softmax)
  *   totals[b] + scores[b][i]                                            (otherwise)
  * (dev_totals NULL: 0), the largest first; of equal ones the lower beam's, then the higher score, then the lower row.  What counts is
- * taken in fp64.  dev_parent, dev_row and dev_total [groups][best] receive b (counted over all queries: what gv_lookup_rows takes to
+ * taken in fp64, each exponential to within 2^-34 of it; a logarithm of a probability is at most 0.  dev_parent, dev_row and dev_total [groups][best] receive b (counted over all queries: what gv_lookup_rows takes to
  * reorder what belongs to the beams), i, and what they count, rounded to float.  Scores of -inf and NaN are never selected and have
  * no share in the sum; of scores of +inf each counts as an equal share.  A beam whose total is not finite offers nothing; one with
  * dev_done[b] != 0 (may be NULL) offers row `end` (< rows) alone, with its total as it is, whatever its scores are.  Where

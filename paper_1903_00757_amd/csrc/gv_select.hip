@@ -53,6 +53,26 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 }
 __device__ __forceinline__ float next_above(float x) { return value_of(ordered(x) + 1); }  // NaN, which nothing reaches, above infinity
 
+// exp(d), d <= 21, within 2^-34 of it, and 1 of 0: 2^n times 2^f, |f| <= 1/2, by a polynomial whose first number is 1 and whose
+// others make the largest error the least.  What is below exp(-700) counts as that, which no sum that has a term of 1 notices.
+// Fifteen instructions, each as long as one in fp32.  __expf takes four, but is off by up to (|d| + 1) 2^-23 of a term, and the sum of equal
+// scores by as much of it: beams whose totals lie closer came in the wrong order (the call for 16 x 8 beams of 10^6 took 116 us by it, 151
+// by this).
+__device__ __forceinline__ double exp_of(double d) {
+    constexpr double kLog2E = 1.4426950408889634, kWhole = 0x1.8p52;  // added, it leaves a whole number in the low word
+    d = fmax(d, -700.0);
+    const double t = fma(d, kLog2E, kWhole), f = fma(d, kLog2E, kWhole - t);
+    double p = 1.519615612132076e-05;
+    p = fma(p, f, 0.00015466756367126918);
+    p = fma(p, f, 0.0013333935057608427);
+    p = fma(p, f, 0.009618038131876797);
+    p = fma(p, f, 0.05550410365988536);
+    p = fma(p, f, 0.2402265106656269);
+    p = fma(p, f, 0.693147180704533);
+    p = fma(p, f, 1.0);
+    return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
+}
+
 // The k-th largest of the kOf numbers of each of the 64 lanes (1 <= k <= 64 kOf).
 template <int kOf>
 __device__ __forceinline__ uint32_t kth_of_lanes(const uint32_t (&x)[kOf], uint32_t k) {
@@ -253,6 +273,11 @@ __device__ __forceinline__ bool offers(const SelectArgs &a, uint64_t beam, float
     return fabsf(total) < infinity();
 }
 
+// What a score counts beyond its beam's total: at most 0, as what is counted from may lie below the largest score and the sum is rounded.
+__device__ __forceinline__ double log_of(float score, float top, double log_sum) {
+    return fmin((score == top ? 0.0 : (double)score - (double)top) - log_sum, 0.0);
+}
+
 __device__ __forceinline__ void put_none(const SelectArgs &a, uint64_t group, uint32_t rank) {
     const uint64_t at = group * a.best + rank;
     a.parent[at] = -1;
@@ -269,8 +294,8 @@ __device__ __forceinline__ void put(const SelectArgs &a, uint64_t group, uint32_
 }
 
 // One part of one beam.  kAlone: groups of one beam in one part are finished here.  64 x 10^6 floats, best 1: 43 us, 6 TB/s;
-// best 100: 60, for the search of the bound and the candidates of the first turns; 128 x 10^6 with softmax 104 us, 4.9 TB/s,
-// the vector units busy for half of it.
+// best 100: 60, for the search of the bound and the candidates of the first turns; 128 x 10^6 with softmax 139 us, for the
+// exponentials in fp64.
 template <class T, bool kLog, bool kAlone>
 __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
     __shared__ Shared s;
@@ -318,20 +343,20 @@ __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
             // exponentials of differences from a score of this thread that is not far below its largest
             if (most > top + 20.0f || top == -infinity()) {
                 if (most > top) {
-                    sum = top == -infinity() || most == infinity() ? 0.0 : sum * (double)__expf(top - most);
+                    sum = top == -infinity() || most == infinity() ? 0.0 : sum * exp_of((double)top - (double)most);
                     top = most;
                 }
             }
-            float terms[4] = {};
+            double terms[2] = {};
             if (top < infinity()) {
-                const float from = top == -infinity() ? 0.0f : top;
+                const double from = top == -infinity() ? 0.0 : (double)top;
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) terms[i % 4] += __expf(v[i] - from);
+                for (int i = 0; i < kEach; ++i) terms[i % 2] += exp_of((double)v[i] - from);
             } else {  // scores of infinity share everything
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) terms[i % 4] += v[i] == infinity() ? 1.0f : 0.0f;
+                for (int i = 0; i < kEach; ++i) terms[i % 2] += v[i] == infinity() ? 1.0 : 0.0;
             }
-            sum += (double)((terms[0] + terms[1]) + (terms[2] + terms[3]));
+            sum += terms[0] + terms[1];
         }
         if ((turn & (turn + 1)) == 0 || first + kTile >= end) {  // turns 0, 1, 3, 7, ..., and the last
             uint32_t order[kPieces];
@@ -389,8 +414,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
             for (uint32_t j = 0; j < kept; ++j) rank += key_of(s.kept[j].score, s.kept[j].row) > key;
             if (rank >= a.best) continue;
             const float score = s.kept[i].score;
-            const double total = !kLog ? (double)base + (double)score
-                                       : (double)base + (score == all_top ? 0.0 : (double)score - (double)all_top) - log_sum;
+            const double total = (double)base + (kLog ? log_of(score, all_top, log_sum) : (double)score);
             put(a, beam, rank, beam, s.kept[i].row, total);
         }
         for (uint32_t r = kept + tid; r < a.best; r += kThreads) put_none(a, beam, r);
@@ -559,7 +583,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_select_join(SelectArgs a) {
     __syncthreads();
     const auto total_of = [&](uint32_t beam, float score) {
         const double base = (double)s.base[beam];
-        return !kLog ? base + (double)score : base + (score == s.top[beam] ? 0.0 : (double)score - (double)s.top[beam]) - s.log_sum[beam];
+        return base + (kLog ? log_of(score, s.top[beam], s.log_sum[beam]) : (double)score);
     };
     const auto take = [&](uint32_t i, uint32_t &beam, Candidate &c) {
         uint32_t lo = 0, hi = lists - 1;  // the first list that ends behind i
