@@ -51,7 +51,12 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 __device__ __forceinline__ float value_of(uint32_t order) {
     return __uint_as_float(order ^ (order >> 31 ? 0x80000000u : 0xFFFFFFFFu));
 }
-__device__ __forceinline__ float next_above(float x) { return value_of(ordered(x) + 1); }  // NaN, which nothing reaches, above infinity
+// What a score has to reach to be of interest still, when those that equal x are not: above infinity NaN, which nothing reaches and
+// which then stays.  (std::max would leave it out.)
+__device__ __forceinline__ float raised_above(float least, float x) {
+    const float next = value_of(ordered(x) + 1);
+    return next <= least ? least : next;
+}
 
 // exp(d), d <= 21, within 2^-34 of it, and 1 of 0: 2^n times 2^f, |f| <= 1/2, by a polynomial whose first number is 1 and whose
 // others make the largest error the least.  What is below exp(-700) counts as that, which no sum that has a term of 1 notices.
@@ -373,7 +378,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
         if (most >= least) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                if (v[i] < least) continue;
+                if (!(v[i] >= least)) continue;
                 const uint32_t at = atomicAdd(&s.count, 1u);
                 if (at < kSlots) s.kept[at] = {v[i], row + (i / 8) * (kTile / kPieces) + i % 8};
                 else full = true;
@@ -382,14 +387,14 @@ __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
         if (__syncthreads_or(full)) {
             if (kept >= a.best) {  // scores that equal the last of those come behind
                 bound = std::max(bound, narrow(s, kept, a.best));
-                least = std::max(least, next_above(bound));
+                least = raised_above(least, bound);
                 kept = a.best;
             }
             kept = take_slowly(s, kept, a.best, scores, (uint32_t)first, end, least, bound);
         } else {
             kept = s.count;
         }
-        if (kept >= a.best && bound > -infinity()) least = std::max(least, next_above(bound));
+        if (kept >= a.best && bound > -infinity()) least = raised_above(least, bound);
         __syncthreads();
     }
     double log_sum = 0.0;

@@ -307,3 +307,37 @@ def test_captured_and_replayed(gv, rows):
         for got, moved in [eager] + [rest for _, *rest in graphs]:
             assert torch.equal(got.parent, want.parent) and torch.equal(got.row, want.row) and torch.equal(got.total, want.total)
             assert torch.equal(moved, states[want.parent.view(-1)])
+
+
+@gpu
+@pytest.mark.parametrize("log", [False, True])
+@pytest.mark.parametrize("rows,share", [(70_000, 1.0), (70_000, 0.2), (200_000, 0.05)])
+def test_many_scores_of_infinity(gv, log, rows, share):
+    """More of them than a workgroup keeps, over several of its turns: the lowest rows, each with an equal share."""
+    import torch
+
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    s = torch.randn(3, rows, device="cuda", generator=gen)
+    s[torch.rand(3, rows, device="cuda", generator=gen) < share] = float("inf")
+    check(gv, s, 100, log=log)
+    check(gv, s.half(), 700, beams=3, log=log)
+
+
+@gpu
+def test_scores_of_infinity_take_no_longer_than_other_equal_ones(gv):
+    """Once `best` of them are kept none of the others is of interest.  (Taken up in every turn they took nine times as long.)"""
+    import torch
+
+    def least_time(s):
+        times = []
+        for _ in range(6):
+            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            begin.record()
+            gv.gv_select_rows(s, 10, log_softmax=False)
+            end.record()
+            end.synchronize()
+            times.append(begin.elapsed_time(end))
+        return min(times)
+
+    zeros = torch.zeros(1024, 40 * 16384, dtype=torch.float16, device="cuda")
+    assert least_time(torch.full_like(zeros, float("inf"))) < 2 * least_time(zeros)
