@@ -373,7 +373,8 @@ int gv_link_prediction_auc(gv_ctx *ctx, const uint32_t *host_edge_first, const u
  * cols (the values of a row lie together).  GV_F32 = float, GV_BF16 = bfloat16, GV_F16 = IEEE half, GV_I8 = int8; GV_I32 = int32
  * and GV_I64 = int64 are types of indices and of what gv_lookup_rows copies.
  * rows <= 2^31, 1 <= cols <= GV_MAX_ROW_COLS; rows = 0 is an empty call.  An output may be the very matrix (pointer, stride and
- * type) of an input of the same call; matrices that overlap otherwise leave undefined values.
+ * type) of an input of the same call; matrices that overlap otherwise leave undefined values.  Matrices whose rows lie between each
+ * other's (column slices of one buffer, or every other row of it) do not overlap.
  * Arithmetic is fp32 whatever the types; a result is rounded once, to nearest even, when it is written.          */
 enum { GV_F32 = 0, GV_BF16 = 1, GV_F16 = 2, GV_I8 = 3, GV_I32 = 4, GV_I64 = 5 };
 #define GV_MAX_ROW_COLS 16384u
@@ -408,7 +409,7 @@ int gv_norm_rows(uint64_t rows, uint32_t cols, int type, const void *dev_x, uint
  *   alone, so a call gives the same bits each time).
  * dev_sum is h as gv_norm_rows kept it (x itself, where nothing was added or dropped), dev_rstd what it gave.
  * With grad_gain, dev_workspace points to workspace_bytes bytes (at least those of gv_norm_rows_workspace, which may be
- * none; aligned to 16) that the call may overwrite.                                                            */
+ * none; aligned to 16) that the call may overwrite.                              */
 int gv_norm_rows_workspace(uint64_t rows, uint32_t cols, uint64_t *bytes);
 int gv_norm_rows_backward(uint64_t rows, uint32_t cols, int type, const void *dev_grad_out, uint64_t grad_out_stride,
                           const void *dev_sum, uint64_t sum_stride, const float *dev_gain, const float *dev_rstd,
@@ -438,8 +439,8 @@ int gv_score_rows(uint64_t rows, uint32_t cols, uint32_t group, const uint8_t *d
 /* Rows by index: out[t] = scale * table[index[t]], t < count.  An index is GV_I32 or GV_I64, index[t] lies t * index_stride values
  * behind the first (a column of a pool has stride 2); one that names no row (negative, or >= rows) gives a row of zeros.
  * table has `rows` rows of `type`, out `count` rows of out_type: GV_F32, GV_BF16 and GV_F16 in any pair, or the same type of whole
- * numbers with scale 1.  With scale 1 and one type, values are copied bit by bit.  out may not overlap the table.  count <= 2^31;
- * count = 0 is an empty call, and a table of no rows gives zeros.                                                    */
+ * numbers with scale 1.  With scale 1 and one type, values are copied bit by bit.  out may not overlap the table.
+ * count <= 2^31; count = 0 is an empty call, and a table of no rows gives zeros.             */
 int gv_lookup_rows(uint64_t count, const void *dev_index, uint64_t index_stride, int index_type, uint64_t rows, uint32_t cols, int type,
                    const void *dev_table, uint64_t table_stride, float scale, int out_type, void *dev_out, uint64_t out_stride,
                    void *stream);
@@ -448,8 +449,8 @@ int gv_lookup_rows(uint64_t count, const void *dev_index, uint64_t index_stride,
  * of out_type, `rows` rows; type and out_type are GV_F32, GV_BF16 or GV_F16 in any pair.  Rows that no index names become 0,
  * or with add stay as they are, untouched: with the table itself as out and a negative scale, add makes a step of descent on the
  * rows that the batch names.  Sums are fp32, in an order that the indices decide: a call gives the same bits each time.  grad and out
- * may not overlap.  dev_workspace points to workspace_bytes bytes (at least those of gv_lookup_rows_workspace, which may be none;
- * aligned to 16) that the call may overwrite.                                                                          */
+ * may not overlap.  dev_workspace points to workspace_bytes bytes (at least those of
+ * gv_lookup_rows_workspace, which may be none; aligned to 16) that the call may overwrite.                              */
 int gv_lookup_rows_workspace(uint64_t count, uint64_t rows, uint32_t cols, int add, uint64_t *bytes);
 int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t index_stride, int index_type, uint64_t rows, uint32_t cols,
                             int type, const void *dev_grad, uint64_t grad_stride, float scale, int add, int out_type, void *dev_out,
@@ -459,9 +460,8 @@ int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t inde
  * pre and out have outs columns, all of `type` (GV_F32, GV_BF16, GV_F16).  bias, residual and pre may be NULL; pre receives z, which
  * the backward pass takes.  GV_ACT_GELU is z (1 + erf(z / sqrt 2)) / 2, its second factor to within 4e-7, GV_ACT_SILU z / (1 + exp(-z)).
  * Sums are fp32 in an order that sizes, type, strides and alignment decide, act is taken of the sum, and a result is rounded once.
- * out may be residual itself; else neither out nor pre may overlap x, weight or each other, nor pre the residual.  1 <= outs <=
- * GV_MAX_ROW_COLS.  dev_workspace points to workspace_bytes bytes (at least those of gv_dense_rows_workspace, which may be none;
- * aligned to 16) that the call may overwrite.                                                                          */
+ * out may be residual itself; else neither out nor pre may overlap x, weight or each other, nor pre the residual.  1 <= outs <= GV_MAX_ROW_COLS.  dev_workspace points to workspace_bytes bytes (at least those of
+ * gv_dense_rows_workspace, which may be none; aligned to 16) that the call may overwrite.                              */
 enum { GV_ACT_NONE = 0, GV_ACT_RELU = 1, GV_ACT_GELU = 2, GV_ACT_SILU = 3 };
 int gv_dense_rows_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, uint64_t *bytes);
 int gv_dense_rows(uint64_t rows, uint32_t cols, uint32_t outs, int type, const void *dev_x, uint64_t x_stride, const void *dev_weight,
@@ -472,7 +472,8 @@ int gv_dense_rows(uint64_t rows, uint32_t cols, uint32_t outs, int type, const v
  *   grad_x = gz weight,  grad_weight = gz^T x,  grad_bias = sum over the rows of gz,
  * each of `type` and each may be NULL (the residual's gradient is grad_out).  pre is what the forward pass left; without an activation
  * it is not read.  The products take gz rounded to `type`, as they take their other operand; grad_bias adds up what is not rounded.
- * grad_x and grad_weight may not overlap each other or what the call reads.  rows = 0 leaves grad_weight and grad_bias 0.  The workspace is that
+ * grad_x and grad_weight may not overlap each other or what the call reads: x where grad_weight is asked for, weight where grad_x is, pre
+ * with an activation.  rows = 0 leaves grad_weight and grad_bias 0.  The workspace is that
  * of gv_dense_rows_backward_workspace, which is told which gradients are asked for.                                  */
 int gv_dense_rows_backward_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, int act, int grad_x, int grad_weight,
                                      int grad_bias, uint64_t *bytes);
@@ -486,8 +487,9 @@ int gv_dense_rows_backward(uint64_t rows, uint32_t cols, uint32_t outs, int type
  *   totals[b] + scores[b][i] - log sum over i' of exp(scores[b][i'])    (log_softmax)
  *   totals[b] + scores[b][i]                                            (otherwise)
  * (dev_totals NULL: 0), the largest first; of equal ones the lower beam's, then the higher score, then the lower row.  What counts is
- * taken in fp64, each exponential to within 2^-34 of it; a logarithm of a probability is at most 0.  dev_parent, dev_row and dev_total [groups][best] receive b (counted over all queries: what gv_lookup_rows takes to
- * reorder what belongs to the beams), i, and what they count, rounded to float.  Scores of -inf and NaN are never selected and have
+ * taken in fp64, each exponential to within 2^-34 of it; a logarithm of a probability is at most 0.  dev_parent, dev_row and
+ * dev_total [groups][best] receive b (counted over all queries: what gv_lookup_rows takes to reorder what belongs to the beams),
+ * i, and what they count, rounded to float.  Scores of -inf and NaN are never selected and have
  * no share in the sum; of scores of +inf each counts as an equal share.  A beam whose total is not finite offers nothing; one with
  * dev_done[b] != 0 (may be NULL) offers row `end` (< rows) alone, with its total as it is, whatever its scores are.  Where
  * there is less to select than `best`, parent and row are -1 and total -inf.

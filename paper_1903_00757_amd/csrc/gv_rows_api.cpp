@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <initializer_list>
+#include <numeric>
 
 #include "gv_host.hpp"
 #include "gv_rows.hpp"
@@ -68,12 +69,32 @@ int check_index(const char *call, const gv::Index &index, uint64_t count, uint64
     return check_array(call, "index", index.at, size_of(index.type));
 }
 
-// Whether two matrices share memory.
-bool overlap(const Matrix &a, uint64_t a_rows, uint32_t a_cols, const Matrix &b, uint64_t b_rows, uint32_t b_cols) {
-    if (a_rows == 0 || b_rows == 0) return false;
-    const uintptr_t a_end = (uintptr_t)a.at + ((a_rows - 1) * a.stride + a_cols) * size_of(a.type);
-    const uintptr_t b_end = (uintptr_t)b.at + ((b_rows - 1) * b.stride + b_cols) * size_of(b.type);
-    return (uintptr_t)a.at < b_end && (uintptr_t)b.at < a_end;
+// A matrix, as far as it goes.
+struct Sized {
+    Matrix matrix;
+    uint64_t rows;
+    uint32_t cols;
+    uint64_t step() const { return rows > 1 ? matrix.stride * size_of(matrix.type) : 0; }  // bytes from row to row
+    uint64_t width() const { return (uint64_t)cols * size_of(matrix.type); }
+    unsigned __int128 end() const { return (unsigned __int128)(uintptr_t)matrix.at + (unsigned __int128)(rows - 1) * step() + width(); }
+};
+
+// Whether two matrices share values.  Those whose rows lie between each other's, as column slices of one buffer do, share none: what
+// the steps from row to row have in common is a pattern that both repeat, and each has its own part of it.
+bool overlap(const Sized &a, const Sized &b) {
+    if (!a.matrix.at || !b.matrix.at || a.rows == 0 || b.rows == 0) return false;
+    const uintptr_t a_at = (uintptr_t)a.matrix.at, b_at = (uintptr_t)b.matrix.at;
+    if (a_at >= b.end() || b_at >= a.end()) return false;
+    const uint64_t pattern = std::gcd(a.step(), b.step());
+    if (pattern == 0) return true;  // one row each
+    const uint64_t behind = b_at >= a_at ? (b_at - a_at) % pattern : (pattern - (a_at - b_at) % pattern) % pattern;
+    return behind < a.width() || behind + b.width() > pattern;
+}
+int check_apart(const char *call, std::initializer_list<Sized> written, std::initializer_list<Sized> read) {
+    for (const Sized &w : written)
+        for (const Sized &r : read)
+            if (overlap(w, r)) return fail_call(GV_EINVAL, "%s: %s overlaps %s", call, w.matrix.name, r.matrix.name);
+    return GV_OK;
 }
 
 int check_workspace(const char *call, const void *workspace, uint64_t bytes, uint64_t need) {
@@ -219,7 +240,7 @@ int gv_lookup_rows(uint64_t count, const void *dev_index, uint64_t index_stride,
     const Matrix table{"table", dev_table, table_stride, type}, out{"out", dev_out, out_stride, out_type};
     if (rows > 0) GV_TRY(check_matrices(call, cols, {table}));
     GV_TRY(check_matrices(call, cols, {out}));
-    if (overlap(table, rows, cols, out, count, cols)) return fail_call(GV_EINVAL, "%s: out overlaps the table", call);
+    if (overlap({table, rows, cols}, {out, count, cols})) return fail_call(GV_EINVAL, "%s: out overlaps the table", call);
     return launched(call, gv::launch_lookup({index, dev_table, dev_out, count, table_stride, out_stride, (uint32_t)rows, cols, type, out_type,
                                              scale}, (hipStream_t)stream));
 }
@@ -245,7 +266,7 @@ int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t inde
     const Matrix grad{"grad", dev_grad, grad_stride, type}, out{"out", dev_out, out_stride, out_type};
     if (count > 0) GV_TRY(check_matrices(call, cols, {grad}));
     GV_TRY(check_matrices(call, cols, {out}));
-    if (overlap(grad, count, cols, out, rows, cols)) return fail_call(GV_EINVAL, "%s: out overlaps grad", call);
+    GV_TRY(check_apart(call, {{out, rows, cols}}, {{grad, count, cols}}));
     GV_TRY(check_workspace(call, dev_workspace, workspace_bytes, gv::lookup_grad_workspace(count, rows, cols, add != 0)));
     gv::LookupGradArgs a{};
     a.index = index, a.grad = dev_grad, a.out = dev_out, a.count = count, a.grad_stride = grad_stride, a.out_stride = out_stride;
@@ -257,20 +278,6 @@ static int check_dense(const char *call, uint64_t rows, uint32_t cols, uint32_t 
     GV_TRY(check_shape(call, rows, cols, type, false));
     if (outs == 0 || outs > GV_MAX_ROW_COLS) return fail_call(GV_EINVAL, "%s: %u columns of out: 1..%u", call, outs, GV_MAX_ROW_COLS);
     if (act < GV_ACT_NONE || act > GV_ACT_SILU) return fail_call(GV_EINVAL, "%s: bad activation %d", call, act);
-    return GV_OK;
-}
-
-// A matrix of a layer, as far as it goes.
-struct Sized {
-    Matrix matrix;
-    uint64_t rows;
-    uint32_t cols;
-};
-static int check_apart(const char *call, std::initializer_list<Sized> written, std::initializer_list<Sized> read) {
-    for (const Sized &w : written)
-        for (const Sized &r : read)
-            if (w.matrix.at && r.matrix.at && overlap(w.matrix, w.rows, w.cols, r.matrix, r.rows, r.cols))
-                return fail_call(GV_EINVAL, "%s: %s overlaps %s", call, w.matrix.name, r.matrix.name);
     return GV_OK;
 }
 
@@ -296,8 +303,9 @@ int gv_dense_rows(uint64_t rows, uint32_t cols, uint32_t outs, int type, const v
     if (dev_bias) GV_TRY(check_array(call, "bias", dev_bias, size_of(type)));
     if (dev_residual) GV_TRY(check_matrices(call, outs, {{"residual", dev_residual, residual_stride, type}}));
     if (dev_pre) GV_TRY(check_matrices(call, outs, {pre.matrix}));
+    const Sized residual{{"residual", dev_residual, residual_stride, type}, rows, outs};
     GV_TRY(check_apart(call, {out, pre}, {x, weight}));
-    GV_TRY(check_apart(call, {pre}, {out, {{"residual", dev_residual, residual_stride, type}, rows, outs}}));
+    GV_TRY(check_apart(call, {pre}, {out, residual}));
     GV_TRY(check_workspace(call, dev_workspace, workspace_bytes, gv::dense_workspace(rows, cols, outs, type)));
     gv::DenseArgs a{};
     a.x = dev_x, a.weight = dev_weight, a.bias = dev_bias, a.residual = dev_residual, a.pre = dev_pre, a.out = dev_out;
@@ -333,7 +341,10 @@ int gv_dense_rows_backward(uint64_t rows, uint32_t cols, uint32_t outs, int type
     }
     if (dev_grad_weight) GV_TRY(check_matrices(call, cols, {grad_weight.matrix}));
     if (dev_grad_bias) GV_TRY(check_array(call, "grad_bias", dev_grad_bias, size_of(type)));
-    GV_TRY(check_apart(call, {grad_x, grad_weight}, {grad, x, weight, pre}));
+    // of what the call reads
+    const Sized none{};
+    const std::initializer_list<Sized> read = {grad, dev_grad_weight ? x : none, dev_grad_x && rows > 0 ? weight : none, act != GV_ACT_NONE ? pre : none};
+    GV_TRY(check_apart(call, {grad_x, grad_weight}, read));
     GV_TRY(check_apart(call, {grad_x}, {grad_weight}));
     GV_TRY(check_workspace(call, dev_workspace, workspace_bytes,
                            gv::dense_grad_workspace(rows, cols, outs, type, act, dev_grad_x, dev_grad_weight, dev_grad_bias)));

@@ -387,3 +387,24 @@ def test_captured_and_replayed(gv, rows):
         torch.cuda.current_stream().wait_stream(side)
         for _, got in graphs:
             assert all(torch.equal(a, b) for a, b in zip(got, eager))
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,outs", [(1, 40, 24), (33, 40, 24), (700, 96, 160), (5000, 64, 264)])
+def test_slices_of_one_buffer(gv, kind, rows, cols, outs):
+    """A layer's result and what it is taken of side by side in one buffer: the same bits as apart, and nothing else is written."""
+    import torch
+
+    rng = np.random.default_rng(rows)
+    buf, _ = make_rows(torch, rng, rows, 2 * cols + 2 * outs, kind)
+    before = buf.clone()
+    w, _ = make_rows(torch, rng, outs, cols, kind, 0, 0, cols ** -0.5)
+    x, grad_x, out, g = buf.split([cols, cols, outs, outs], 1)
+    want = gv.gv_dense_rows(x.clone(), w, residual=g.clone(), act=gv.GV_ACT_SILU).out
+    assert torch.equal(gv.gv_dense_rows(x, w, residual=g, act=gv.GV_ACT_SILU, out=out).out, want)
+    assert torch.equal(buf[:, :2 * cols], before[:, :2 * cols]) and torch.equal(g, before[:, 2 * cols + outs:])
+    index = torch.arange(rows, device="cuda").flip(0)
+    assert torch.equal(gv.gv_lookup_rows(x, index, out=grad_x), before[:, :cols].flip(0))
+    back = gv.gv_lookup_rows_backward(g, index, rows, out=out)
+    assert torch.equal(back, before[:, 2 * cols + outs:].flip(0)) and torch.equal(x, before[:, :cols])

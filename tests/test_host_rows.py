@@ -13,6 +13,7 @@ HIPCC = "/opt/rocm/bin/hipcc"
 pytestmark = pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not installed")
 
 F32, BF16, F16 = 0, 1, 2
+EINVAL = -1
 SIZE = {F32: 4, BF16: 2, F16: 2}
 X, W, OUT, PRE, SPACE = (ctypes.c_void_p(i << 42) for i in range(1, 6))  # far apart
 
@@ -126,3 +127,74 @@ def test_rows_by_index_and_selections_can_be_launched(calls):
                 rc, text, launches = calls.call("gv_select_rows", queries, rows, BF16, X, max(1, rows), beams, None, None, 0, 1, best, OUT, PRE, W,
                                                 SPACE if space else None, space, None)
                 assert rc == 0 and all(0 < l["blocks"] * l["threads"] < 2**32 for l in launches), (text, launches)
+
+
+def at(base, values, type=F32):
+    """The address that lies so many values behind another."""
+    return ctypes.c_void_p(base.value + values * SIZE[type])
+
+
+def layer(x=X, x_stride=8, w=W, w_stride=8, bias=None, residual=None, residual_stride=16, pre=None, pre_stride=16, out=OUT, out_stride=16, rows=100):
+    return "gv_dense_rows", rows, 8, 16, F32, x, x_stride, w, w_stride, bias, 0, residual, residual_stride, pre, pre_stride, out, out_stride, None, 0, None
+
+
+def test_layers_beside_what_they_read(calls):
+    """Column slices of one buffer, and rows between other rows, share no value; what shares one is refused."""
+    for fine in [dict(x_stride=24, out=at(X, 8), out_stride=24), dict(x=at(X, 16), x_stride=24, out=X, out_stride=24),  # x and out side by side
+                 dict(x_stride=48, out=at(X, 24), out_stride=96),          # beside every other row
+                 dict(x_stride=64, out=at(X, 32), out_stride=64),          # every other row
+                 dict(out_stride=32, pre=at(OUT, 16), pre_stride=32), dict(out_stride=32, residual=at(OUT, 16), residual_stride=32),
+                 dict(out_stride=32, residual=at(OUT, -16), residual_stride=32), dict(residual=OUT), dict(residual=OUT, residual_stride=16, out_stride=16),
+                 dict(rows=1, bias=OUT), dict(rows=1, bias=OUT, residual=OUT, residual_stride=99), dict(rows=1, pre=PRE, bias=PRE),
+                 dict(rows=1, x_stride=999, out=at(X, 8)), dict(out=at(X, 100 * 8)), dict(out=at(X, 99 * 24 + 8), x_stride=24), dict(bias=at(OUT, -16))]:
+        name, *args = layer(**fine)
+        rc, text, launches = calls.call(name, *args)
+        assert rc == 0 and launches, (fine, text)
+    for bad, word in [(dict(x_stride=23, out=at(X, 8), out_stride=23), "out overlaps x"), (dict(x_stride=24, out=at(X, 7), out_stride=24), "out overlaps x"),
+                      (dict(x_stride=24, out=at(X, 9), out_stride=24), "out overlaps x"), (dict(x_stride=24, out=at(X, 8), out_stride=25), "out overlaps x"),
+                      (dict(out_stride=32, pre=at(OUT, 15), pre_stride=32), "pre overlaps out"), (dict(rows=1, x_stride=999, out=at(X, 7)), "out overlaps x"),
+                      (dict(out=at(X, 99 * 24 + 7), x_stride=24), "out overlaps x"),
+                      (dict(x_stride=48, out=at(X, 24), out_stride=24), "out overlaps x")]:  # out's second row lies on x's
+        name, *args = layer(**bad)
+        rc, text, launches = calls.call(name, *args)
+        assert rc == EINVAL and word in text and not launches, (bad, text)
+
+
+def gradients(g=OUT, g_stride=16, x=X, x_stride=8, w=W, w_stride=8, act=0, pre=None, grad_x=None, grad_x_stride=8, grad_w=None, grad_w_stride=8, grad_b=None):
+    return ("gv_dense_rows_backward", 100, 8, 16, F32, g, g_stride, x, x_stride, w, w_stride, act, pre, 16, grad_x, grad_x_stride, grad_w, grad_w_stride,
+            grad_b, SPACE, 1 << 30, None)
+
+
+def test_gradients_beside_what_they_read(calls):
+    """What a call does not read may be overwritten by it."""
+    for fine in [dict(g_stride=24, grad_x=at(OUT, 16), grad_x_stride=24), dict(x_stride=16, grad_x=at(X, 8), grad_x_stride=16),
+                 dict(w_stride=16, grad_w=at(W, 8), grad_w_stride=16), dict(grad_x=X), dict(grad_w=W), dict(pre=PRE, grad_x=PRE), dict(grad_b=X), dict(grad_b=W),
+                 dict(grad_x=PRE, grad_x_stride=24, grad_b=at(PRE, 8))]:  # between two rows
+        name, *args = gradients(**fine)
+        rc, text, launches = calls.call(name, *args)
+        assert rc == 0 and launches, (fine, text)
+    for bad, word in [(dict(grad_x=OUT), "grad_x overlaps grad_out"), (dict(grad_x=X, grad_w=PRE), "grad_x overlaps x"), (dict(grad_w=W, grad_x=PRE), "grad_weight overlaps weight"),
+                      (dict(act=1, pre=PRE, grad_x=PRE), "grad_x overlaps pre"),
+                      (dict(grad_w=PRE, grad_x=at(PRE, 8), grad_x_stride=15), "grad_x overlaps grad_weight")]:
+        name, *args = gradients(**bad)
+        rc, text, launches = calls.call(name, *args)
+        assert rc == EINVAL and word in text and not launches, (bad, text)
+
+
+def test_rows_by_index_beside_what_they_read(calls):
+    I32, I64 = 4, 5
+
+    def lookup(index=W, index_stride=1, index_type=I32, cols=8, type=F32, table=X, table_stride=8, out=OUT, out_stride=8):
+        return calls.call("gv_lookup_rows", 50, index, index_stride, index_type, 100, cols, type, table, table_stride, 1.0, type, out, out_stride, None)
+
+    def backward(index=W, index_stride=1, grad=X, grad_stride=8, out=OUT, out_stride=8):
+        return calls.call("gv_lookup_rows_backward", 50, index, index_stride, I32, 100, 8, F32, grad, grad_stride, 1.0, 0, F32, out, out_stride, None, 0, None)
+
+    eight = ctypes.c_void_p(OUT.value + 8 * 8)
+    for rc, text, launches in (lookup(table_stride=16, out=at(X, 8), out_stride=16), lookup(out_stride=9, index=at(OUT, 8), index_stride=9),
+                               lookup(index=OUT, index_type=I64, cols=1, type=I64, out_stride=1), lookup(index=OUT, index_type=I64, index_stride=9, cols=1, type=I64, out_stride=9),
+                               lookup(index=eight, index_type=I64, index_stride=9, type=I64, out_stride=9),
+                               backward(grad_stride=16, out=at(X, 8), out_stride=16), backward(out_stride=9, index=at(OUT, 8), index_stride=9)):
+        assert rc == 0 and launches, text
+    for (rc, text, launches), word in ((lookup(table_stride=16, out=at(X, 7), out_stride=16), "overlaps the table"), (backward(grad_stride=16, out=at(X, 9), out_stride=16), "overlaps grad")):
+        assert rc == EINVAL and word in text and not launches, text
