@@ -439,8 +439,8 @@ int gv_score_rows(uint64_t rows, uint32_t cols, uint32_t group, const uint8_t *d
 /* Rows by index: out[t] = scale * table[index[t]], t < count.  An index is GV_I32 or GV_I64, index[t] lies t * index_stride values
  * behind the first (a column of a pool has stride 2); one that names no row (negative, or >= rows) gives a row of zeros.
  * table has `rows` rows of `type`, out `count` rows of out_type: GV_F32, GV_BF16 and GV_F16 in any pair, or the same type of whole
- * numbers with scale 1.  With scale 1 and one type, values are copied bit by bit.  out may not overlap the table.
- * count <= 2^31; count = 0 is an empty call, and a table of no rows gives zeros.             */
+ * numbers with scale 1.  With scale 1 and one type, values are copied bit by bit.  out may not overlap the table, nor the
+ * index without being it.  count <= 2^31; count = 0 is an empty call, and a table of no rows gives zeros.             */
 int gv_lookup_rows(uint64_t count, const void *dev_index, uint64_t index_stride, int index_type, uint64_t rows, uint32_t cols, int type,
                    const void *dev_table, uint64_t table_stride, float scale, int out_type, void *dev_out, uint64_t out_stride,
                    void *stream);
@@ -448,8 +448,8 @@ int gv_lookup_rows(uint64_t count, const void *dev_index, uint64_t index_stride,
  *   out[i] = (add ? out[i] : 0) + scale * sum over the t with index[t] = i of grad[t]
  * of out_type, `rows` rows; type and out_type are GV_F32, GV_BF16 or GV_F16 in any pair.  Rows that no index names become 0,
  * or with add stay as they are, untouched: with the table itself as out and a negative scale, add makes a step of descent on the
- * rows that the batch names.  Sums are fp32, in an order that the indices decide: a call gives the same bits each time.  grad and out
- * may not overlap.  dev_workspace points to workspace_bytes bytes (at least those of
+ * rows that the batch names.  Sums are fp32, in an order that the indices decide: a call gives the same bits each time.  out may
+ * overlap neither grad nor the index.  dev_workspace points to workspace_bytes bytes (at least those of
  * gv_lookup_rows_workspace, which may be none; aligned to 16) that the call may overwrite.                              */
 int gv_lookup_rows_workspace(uint64_t count, uint64_t rows, uint32_t cols, int add, uint64_t *bytes);
 int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t index_stride, int index_type, uint64_t rows, uint32_t cols,
@@ -460,7 +460,8 @@ int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t inde
  * pre and out have outs columns, all of `type` (GV_F32, GV_BF16, GV_F16).  bias, residual and pre may be NULL; pre receives z, which
  * the backward pass takes.  GV_ACT_GELU is z (1 + erf(z / sqrt 2)) / 2, its second factor to within 4e-7, GV_ACT_SILU z / (1 + exp(-z)).
  * Sums are fp32 in an order that sizes, type, strides and alignment decide, act is taken of the sum, and a result is rounded once.
- * out may be residual itself; else neither out nor pre may overlap x, weight or each other, nor pre the residual.  1 <= outs <= GV_MAX_ROW_COLS.  dev_workspace points to workspace_bytes bytes (at least those of
+ * out may be residual itself, and of one row out or pre may be bias; else neither out nor pre may overlap what the call reads, or
+ * each other.  1 <= outs <= GV_MAX_ROW_COLS.  dev_workspace points to workspace_bytes bytes (at least those of
  * gv_dense_rows_workspace, which may be none; aligned to 16) that the call may overwrite.                              */
 enum { GV_ACT_NONE = 0, GV_ACT_RELU = 1, GV_ACT_GELU = 2, GV_ACT_SILU = 3 };
 int gv_dense_rows_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, uint64_t *bytes);
@@ -472,7 +473,7 @@ int gv_dense_rows(uint64_t rows, uint32_t cols, uint32_t outs, int type, const v
  *   grad_x = gz weight,  grad_weight = gz^T x,  grad_bias = sum over the rows of gz,
  * each of `type` and each may be NULL (the residual's gradient is grad_out).  pre is what the forward pass left; without an activation
  * it is not read.  The products take gz rounded to `type`, as they take their other operand; grad_bias adds up what is not rounded.
- * grad_x and grad_weight may not overlap each other or what the call reads: x where grad_weight is asked for, weight where grad_x is, pre
+ * None of the three may overlap another of them or what the call reads: x where grad_weight is asked for, weight where grad_x is, pre
  * with an activation.  rows = 0 leaves grad_weight and grad_bias 0.  The workspace is that
  * of gv_dense_rows_backward_workspace, which is told which gradients are asked for.                                  */
 int gv_dense_rows_backward_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, int act, int grad_x, int grad_weight,

@@ -90,6 +90,10 @@ bool overlap(const Sized &a, const Sized &b) {
     const uint64_t behind = b_at >= a_at ? (b_at - a_at) % pattern : (pattern - (a_at - b_at) % pattern) % pattern;
     return behind < a.width() || behind + b.width() > pattern;
 }
+// Whether an output is the very matrix of an input.
+bool itself(const Sized &a, const Sized &b) {
+    return a.matrix.at == b.matrix.at && a.rows == b.rows && a.cols == b.cols && a.matrix.type == b.matrix.type && a.step() == b.step();
+}
 int check_apart(const char *call, std::initializer_list<Sized> written, std::initializer_list<Sized> read) {
     for (const Sized &w : written)
         for (const Sized &r : read)
@@ -241,6 +245,8 @@ int gv_lookup_rows(uint64_t count, const void *dev_index, uint64_t index_stride,
     if (rows > 0) GV_TRY(check_matrices(call, cols, {table}));
     GV_TRY(check_matrices(call, cols, {out}));
     if (overlap({table, rows, cols}, {out, count, cols})) return fail_call(GV_EINVAL, "%s: out overlaps the table", call);
+    const Sized result{out, count, cols}, indices{{"index", dev_index, index_stride, index_type}, count, 1};
+    if (!itself(result, indices)) GV_TRY(check_apart(call, {result}, {indices}));
     return launched(call, gv::launch_lookup({index, dev_table, dev_out, count, table_stride, out_stride, (uint32_t)rows, cols, type, out_type,
                                              scale}, (hipStream_t)stream));
 }
@@ -266,7 +272,7 @@ int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t inde
     const Matrix grad{"grad", dev_grad, grad_stride, type}, out{"out", dev_out, out_stride, out_type};
     if (count > 0) GV_TRY(check_matrices(call, cols, {grad}));
     GV_TRY(check_matrices(call, cols, {out}));
-    GV_TRY(check_apart(call, {{out, rows, cols}}, {{grad, count, cols}}));
+    GV_TRY(check_apart(call, {{out, rows, cols}}, {{grad, count, cols}, {{"index", dev_index, index_stride, index_type}, count, 1}}));
     GV_TRY(check_workspace(call, dev_workspace, workspace_bytes, gv::lookup_grad_workspace(count, rows, cols, add != 0)));
     gv::LookupGradArgs a{};
     a.index = index, a.grad = dev_grad, a.out = dev_out, a.count = count, a.grad_stride = grad_stride, a.out_stride = out_stride;
@@ -303,9 +309,12 @@ int gv_dense_rows(uint64_t rows, uint32_t cols, uint32_t outs, int type, const v
     if (dev_bias) GV_TRY(check_array(call, "bias", dev_bias, size_of(type)));
     if (dev_residual) GV_TRY(check_matrices(call, outs, {{"residual", dev_residual, residual_stride, type}}));
     if (dev_pre) GV_TRY(check_matrices(call, outs, {pre.matrix}));
-    const Sized residual{{"residual", dev_residual, residual_stride, type}, rows, outs};
+    const Sized residual{{"residual", dev_residual, residual_stride, type}, rows, outs}, bias{{"bias", dev_bias, outs, type}, 1, outs};
     GV_TRY(check_apart(call, {out, pre}, {x, weight}));
     GV_TRY(check_apart(call, {pre}, {out, residual}));
+    if (!itself(out, residual)) GV_TRY(check_apart(call, {out}, {residual}));
+    for (const Sized &written : {out, pre})
+        if (!itself(written, bias)) GV_TRY(check_apart(call, {written}, {bias}));
     GV_TRY(check_workspace(call, dev_workspace, workspace_bytes, gv::dense_workspace(rows, cols, outs, type)));
     gv::DenseArgs a{};
     a.x = dev_x, a.weight = dev_weight, a.bias = dev_bias, a.residual = dev_residual, a.pre = dev_pre, a.out = dev_out;
@@ -342,12 +351,14 @@ int gv_dense_rows_backward(uint64_t rows, uint32_t cols, uint32_t outs, int type
     if (dev_grad_weight) GV_TRY(check_matrices(call, cols, {grad_weight.matrix}));
     if (dev_grad_bias) GV_TRY(check_array(call, "grad_bias", dev_grad_bias, size_of(type)));
     // of what the call reads
-    const Sized none{};
+    const Sized none{}, bias{{"grad_bias", dev_grad_bias, outs, type}, 1, outs};
     const std::initializer_list<Sized> read = {grad, dev_grad_weight ? x : none, dev_grad_x && rows > 0 ? weight : none, act != GV_ACT_NONE ? pre : none};
     GV_TRY(check_apart(call, {grad_x, grad_weight}, read));
     GV_TRY(check_apart(call, {grad_x}, {grad_weight}));
     GV_TRY(check_workspace(call, dev_workspace, workspace_bytes,
                            gv::dense_grad_workspace(rows, cols, outs, type, act, dev_grad_x, dev_grad_weight, dev_grad_bias)));
+    GV_TRY(check_apart(call, {bias}, read));
+    GV_TRY(check_apart(call, {bias}, {grad_x, grad_weight}));
     gv::DenseGradArgs a{};
     a.grad = dev_grad_out, a.x = dev_x, a.weight = dev_weight, a.pre = dev_pre, a.grad_x = rows > 0 ? dev_grad_x : nullptr;
     a.grad_weight = dev_grad_weight, a.grad_bias = dev_grad_bias, a.rows = rows, a.grad_stride = grad_out_stride, a.x_stride = x_stride;

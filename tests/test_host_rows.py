@@ -152,7 +152,9 @@ def test_layers_beside_what_they_read(calls):
         assert rc == 0 and launches, (fine, text)
     for bad, word in [(dict(x_stride=23, out=at(X, 8), out_stride=23), "out overlaps x"), (dict(x_stride=24, out=at(X, 7), out_stride=24), "out overlaps x"),
                       (dict(x_stride=24, out=at(X, 9), out_stride=24), "out overlaps x"), (dict(x_stride=24, out=at(X, 8), out_stride=25), "out overlaps x"),
-                      (dict(out_stride=32, pre=at(OUT, 15), pre_stride=32), "pre overlaps out"), (dict(rows=1, x_stride=999, out=at(X, 7)), "out overlaps x"),
+                      (dict(out_stride=32, pre=at(OUT, 15), pre_stride=32), "pre overlaps out"), (dict(residual=at(OUT, 1)), "out overlaps residual"),
+                      (dict(residual=OUT, residual_stride=17), "out overlaps residual"), (dict(bias=OUT), "out overlaps bias"), (dict(pre=PRE, bias=PRE), "pre overlaps bias"),
+                      (dict(rows=1, bias=at(OUT, 1)), "out overlaps bias"), (dict(rows=1, x_stride=999, out=at(X, 7)), "out overlaps x"),
                       (dict(out=at(X, 99 * 24 + 7), x_stride=24), "out overlaps x"),
                       (dict(x_stride=48, out=at(X, 24), out_stride=24), "out overlaps x")]:  # out's second row lies on x's
         name, *args = layer(**bad)
@@ -174,7 +176,9 @@ def test_gradients_beside_what_they_read(calls):
         rc, text, launches = calls.call(name, *args)
         assert rc == 0 and launches, (fine, text)
     for bad, word in [(dict(grad_x=OUT), "grad_x overlaps grad_out"), (dict(grad_x=X, grad_w=PRE), "grad_x overlaps x"), (dict(grad_w=W, grad_x=PRE), "grad_weight overlaps weight"),
-                      (dict(act=1, pre=PRE, grad_x=PRE), "grad_x overlaps pre"),
+                      (dict(act=1, pre=PRE, grad_x=PRE), "grad_x overlaps pre"), (dict(grad_b=at(OUT, 1599)), "grad_bias overlaps grad_out"),
+                      (dict(grad_b=X, grad_w=PRE), "grad_bias overlaps x"), (dict(grad_b=W, grad_x=PRE), "grad_bias overlaps weight"),
+                      (dict(act=1, pre=PRE, grad_b=PRE), "grad_bias overlaps pre"), (dict(grad_w=PRE, grad_b=at(PRE, 127)), "grad_bias overlaps grad_weight"),
                       (dict(grad_w=PRE, grad_x=at(PRE, 8), grad_x_stride=15), "grad_x overlaps grad_weight")]:
         name, *args = gradients(**bad)
         rc, text, launches = calls.call(name, *args)
@@ -196,5 +200,8 @@ def test_rows_by_index_beside_what_they_read(calls):
                                lookup(index=eight, index_type=I64, index_stride=9, type=I64, out_stride=9),
                                backward(grad_stride=16, out=at(X, 8), out_stride=16), backward(out_stride=9, index=at(OUT, 8), index_stride=9)):
         assert rc == 0 and launches, text
-    for (rc, text, launches), word in ((lookup(table_stride=16, out=at(X, 7), out_stride=16), "overlaps the table"), (backward(grad_stride=16, out=at(X, 9), out_stride=16), "overlaps grad")):
+    for (rc, text, launches), word in ((lookup(table_stride=16, out=at(X, 7), out_stride=16), "overlaps the table"), (lookup(out_stride=9, index=at(OUT, 7), index_stride=9), "overlaps index"),
+                                       (lookup(index=OUT, index_type=I64, cols=1, type=I64, out_stride=2), "overlaps index"), (lookup(index=OUT, cols=1), "overlaps index"),
+                                       (lookup(index=OUT, index_stride=0), "overlaps index"), (backward(grad_stride=16, out=at(X, 9), out_stride=16), "overlaps grad"),
+                                       (backward(index=OUT), "overlaps index")):
         assert rc == EINVAL and word in text and not launches, text
