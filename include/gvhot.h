@@ -458,7 +458,8 @@ int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t inde
 
 /* A layer: z = x weight^T + bias, out = residual + act(z); x has cols columns, weight outs rows of cols, bias outs values, and residual,
  * pre and out have outs columns, all of `type` (GV_F32, GV_BF16, GV_F16).  bias, residual and pre may be NULL; pre receives z, which
- * the backward pass takes.  GV_ACT_GELU is z (1 + erf(z / sqrt 2)) / 2, its second factor to within 4e-7, GV_ACT_SILU z / (1 + exp(-z)).
+ * the backward pass takes.  GV_ACT_GELU is z (1 + erf(z / sqrt 2)) / 2, GV_ACT_SILU z / (1 + exp(-z)); gelu's
+ * second factor is within 4e-7 for the 16-bit types, and for GV_F32 within 12 2^-24 of itself (z > -13; it ends there).
  * Sums are fp32 in an order that sizes, type, strides and alignment decide, act is taken of the sum, and a result is rounded once.
  * out may be residual itself, and of one row out or pre may be bias; else neither out nor pre may overlap what the call reads, or
  * each other.  1 <= outs <= GV_MAX_ROW_COLS.  dev_workspace points to workspace_bytes bytes (at least those of

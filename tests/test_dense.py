@@ -408,3 +408,27 @@ def test_slices_of_one_buffer(gv, kind, rows, cols, outs):
     assert torch.equal(gv.gv_lookup_rows(x, index, out=grad_x), before[:, :cols].flip(0))
     back = gv.gv_lookup_rows_backward(g, index, rows, out=out)
     assert torch.equal(back, before[:, 2 * cols + outs:].flip(0)) and torch.equal(x, before[:, :cols])
+
+
+@gpu
+@pytest.mark.parametrize("rows", [60, 2000, 70_000])
+def test_gelu_in_full_precision(gv, rows):
+    """Of one column and a weight of 1 z is x itself, so what is off is gelu.  Below |z| = 1/4 its second factor is 1/2 and a small part, a
+    sum rounded once (u of it) whose part is off by some units, 6 u of a fifth of it; the product is rounded once more: 3.2 u.  Elsewhere the
+    factor's tail passes through a power of 2 (2 u and the rounding of what makes it exact, u), a reciprocal (2 u, which the
+    polynomial passes on) and three products and sums with coefficients of both signs (6 u): 12 u, with the last rounding 13.  The
+    slope, at most 1.13, adds up the factor and z times the bell curve, at most 0.25: 4 u."""
+    import torch
+
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    z = torch.cat([s * torch.randn(rows // 4 + 1, 1, device="cuda", generator=gen) for s in (0.05, 0.5, 2.0, 5.0)])[:rows]
+    z.clamp_(min=-13.0)
+    z[:7, 0] = torch.tensor([0.0, -0.0, 1.0, -1.0, 0.99999994, 1e-30, -13.0])
+    z[7:10, 0] = torch.tensor([20.0, 1e30, -12.999])
+    one, z64 = torch.ones(1, 1, device="cuda"), z.double()
+    got, want = gv.gv_dense_rows(z, one, act=gv.GV_ACT_GELU).out, act_of(torch, z64, "gelu")
+    within(got, want, want.abs() * torch.where(z64.abs() <= 0.25, 3.2, 13.0) * U + 2.0 ** -126)
+    grads = gv.gv_dense_rows_backward(torch.ones_like(z), z, one, z, act=gv.GV_ACT_GELU, keep_weight=False)
+    within(grads.x, slope_of(torch, z64, "gelu"), torch.full_like(z64, 4 * U))
+    wild = torch.tensor([[float("inf")], [float("nan")], [-1e30], [-40.0]], device="cuda")
+    assert torch.equal(gv.gv_dense_rows(wild, one, act=gv.GV_ACT_GELU).out.nan_to_num(nan=5.0, posinf=7.0).abs(), torch.tensor([[7.0], [5.0], [0.0], [0.0]], device="cuda"))
