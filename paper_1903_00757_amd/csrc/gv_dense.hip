@@ -219,15 +219,21 @@ struct Share {
             }
         }
     }
+    // kAgain: its places are taken anew in every step, which is a few instructions and leaves the sums their registers.  One operand along
+    // k and the other turned needs that at tiles of 256 (five were spilled: 8192 x 4095 x 4097 in bfloat16 672 us, 627 without);
+    // the others are a few per cent longer by it.
+    template <bool kAgain>
     __device__ __forceinline__ void put(char *tile) const {
+        uint32_t thread = threadIdx.x;
+        if constexpr (kAgain) asm volatile("" : "+v"(thread));
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             uint32_t row, piece;
             if constexpr (kAlong) {
-                const uint32_t id = q * 2 * kTile + threadIdx.x;
+                const uint32_t id = q * 2 * kTile + thread;
                 row = id / 8, piece = id % 8;
             } else {
-                row = 4 * (threadIdx.x % (kTile / 4)) + q, piece = threadIdx.x / (kTile / 4);
+                row = 4 * (thread % (kTile / 4)) + q, piece = thread / (kTile / 4);
             }
             *(uint4 *)(tile + place_of(row, piece)) = pieces[q];
         }
@@ -238,6 +244,7 @@ template <class T, int kTile, bool kAAlong, bool kBAlong>
 __global__ __launch_bounds__(2 * kTile) void k_product(DenseArgs a, uint32_t tiles_m, uint32_t tiles_n) {
     // waves: kTile / 64 x 2 of 64 x kTile / 2 (m x n)
     constexpr int kMs = 4, kNs = kTile / 32;
+    constexpr bool kAgain = kAAlong != kBAlong;
     __shared__ __attribute__((aligned(16))) char tiles[2][2][kTile * kStep];
     const uint32_t all = tiles_m * tiles_n, split = blockIdx.x / all;
     uint32_t id = blockIdx.x % all;
@@ -259,8 +266,8 @@ __global__ __launch_bounds__(2 * kTile) void k_product(DenseArgs a, uint32_t til
     if (k_first < k_last) {
         share_a.load(pa, a.x_stride, m0, a.rows, k_first, k_last);
         share_b.load(pb, a.weight_stride, n0, a.outs, k_first, k_last);
-        share_a.put(tiles[0][0]);
-        share_b.put(tiles[0][1]);
+        share_a.template put<kAgain>(tiles[0][0]);
+        share_b.template put<kAgain>(tiles[0][1]);
     }
     __syncthreads();
     uint32_t half = 0;
@@ -284,18 +291,21 @@ __global__ __launch_bounds__(2 * kTile) void k_product(DenseArgs a, uint32_t til
                 for (int j = 0; j < kNs; ++j) multiply(nb[j], ma[i], sums[i][j], (T *)nullptr);
         }
         if (more) {
-            share_a.put(tiles[half ^ 1][0]);
-            share_b.put(tiles[half ^ 1][1]);
+            share_a.template put<kAgain>(tiles[half ^ 1][0]);
+            share_b.template put<kAgain>(tiles[half ^ 1][1]);
         }
         __syncthreads();
     }
     // a lane has four columns in a row of one row
+    uint32_t thread = threadIdx.x;
+    if constexpr (kAgain) asm volatile("" : "+v"(thread));
+    const uint32_t m = m0 + thread / 128 * 64 + thread % 16, n = n0 + thread / 64 % 2 * (kTile / 2) + thread % 64 / 16 * 4;
 #pragma unroll
     for (int i = 0; i < kMs; ++i)
 #pragma unroll
         for (int j = 0; j < kNs; ++j) {
             float z[4] = {sums[i][j][0], sums[i][j][1], sums[i][j][2], sums[i][j][3]};
-            finish<T>(a, m0 + wm + 16 * i + lane % 16, n0 + wn + 16 * j + 4 * (lane / 16), split, z);
+            finish<T>(a, m + 16 * i, n + 16 * j, split, z);
         }
 }
 

@@ -432,3 +432,16 @@ def test_gelu_in_full_precision(gv, rows):
     within(grads.x, slope_of(torch, z64, "gelu"), torch.full_like(z64, 4 * U))
     wild = torch.tensor([[float("inf")], [float("nan")], [-1e30], [-40.0]], device="cuda")
     assert torch.equal(gv.gv_dense_rows(wild, one, act=gv.GV_ACT_GELU).out.nan_to_num(nan=5.0, posinf=7.0).abs(), torch.tensor([[7.0], [5.0], [0.0], [0.0]], device="cuda"))
+
+
+def test_no_kernel_of_these_operators_spills(gv):
+    """Those whose operands pass through registers (k_product) included: every kernel of a layer, of rows by index and of the selection."""
+    from test_kernel_registers import code_objects, kernels_of
+
+    with open(gv.LIB_PATH, "rb") as f:
+        data = f.read()
+    of = ("k_product", "k_join_product", "k_slope", "k_join_bias", "k_lookup", "k_copy_rows", "k_grad_few", "k_rank", "_digits", "k_sum_runs", "k_join_runs", "k_select")
+    found = {k[".name"]: k for elf in code_objects(data) for k in kernels_of(elf) if any(name in k[".name"] for name in of)}
+    assert sum("9k_productI" in name for name in found) == 3 * 2 * 3  # along or turned operands, tiles of 256 and 128, three types
+    for name, k in found.items():
+        assert k[".vgpr_spill_count"] == 0 and k[".private_segment_fixed_size"] == 0, name
