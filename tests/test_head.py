@@ -143,3 +143,86 @@ def test_calls_on_two_streams_at_once(gv):
         torch.cuda.synchronize()
         for got, want in zip(together, alone):
             assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def moves_of_training(torch, places, nodes, cols, hidden, device_step=None, without=None, steps=3):
+    """(moves, moves in 64 bits, bounds of the rounding) of the parameters over the steps of test_steps_of_training's model: a table, two layers
+    and a norm's gain.  Without device_step the moves are those of 64 bits themselves, of all parameters but `without`."""
+    rng = np.random.default_rng(places)
+    start = [rng.standard_normal((nodes, cols)), rng.standard_normal((hidden, cols)) / np.sqrt(cols), 0.1 * rng.standard_normal(hidden),
+             rng.standard_normal((cols, hidden)) / np.sqrt(hidden), np.ones(cols)]
+    start = [torch.tensor(np.float32(a)).double() for a in start]
+    host = [a.clone().requires_grad_() for a in start]
+    other = [a.clone().requires_grad_() for a in start] if device_step is None else [a.float().cuda() for a in start]
+    scale, rate = 1.5, 0.5
+
+    def in_64_bits(params, index, grad, leave):
+        t, a, b, c, g = params
+        x = torch.where((index >= 0).unsqueeze(1), t[index.clamp_min(0)] * scale, 0.0)
+        h = torch.nn.functional.gelu(x @ a.t() + b)
+        y = x + h @ c.t()
+        n = y / torch.sqrt((y * y).mean(1, keepdim=True) + 1e-6) * g
+        wrt = torch.autograd.grad((n * grad).sum(), params)
+        with torch.no_grad():
+            for k, (p, q) in enumerate(zip(params, wrt)):
+                if k != leave:
+                    p -= rate * q
+
+    for _ in range(steps):
+        index = torch.tensor(rng.integers(-1, nodes, places))
+        grad = torch.tensor(np.float32(rng.standard_normal((places, cols)) / np.sqrt(places)))
+        in_64_bits(host, index, grad.double(), None)
+        if device_step is None:
+            in_64_bits(other, index, grad.double(), without)
+        else:
+            device_step(other, index.cuda(), grad.cuda(), scale, rate)
+    moved = [p.detach().double().cpu() - s for p, s in zip(other, start)]
+    want = [p.detach() - s for p, s in zip(host, start)]
+    return moved, want, [steps * 2.0 ** -24 * p.detach().norm() for p in host]
+
+
+STEPS = [(5, 40, 24, 16), (700, 300, 64, 96), (5000, 900, 33, 50), (20_000, 900, 33, 50)]
+# Of the move: a gradient is a chain of eight sums of at most 100 terms, or of `places` terms in an order of its own, and each element is off by
+# a random walk of its roundings, some tens of units of 2^-24 of the size of its terms; the terms have both signs, so their sum is smaller by up
+# to the root of their number, 141 for 20 000 places: 64 * 141 * 2^-24 = 2^-10.9.
+NEAR = 2.0 ** -10
+
+
+@pytest.mark.parametrize("places,nodes,cols,hidden", STEPS)
+def test_what_the_moves_of_training_tell(places, nodes, cols, hidden):
+    """The oracle against itself: a parameter that is left out moves by nothing, which is a thousand times the gate of the next test off, and the
+    rounding that is allowed beside it is far below the move."""
+    import torch
+
+    for without in range(5):
+        moved, want, rounding = moves_of_training(torch, places, nodes, cols, hidden, without=without)
+        assert rounding[without] < want[without].norm() / 1000
+        assert (moved[without] - want[without]).norm() == want[without].norm()
+        assert NEAR * want[without].norm() + rounding[without] < 0.002 * want[without].norm()
+
+
+@gpu
+@pytest.mark.parametrize("places,nodes,cols,hidden", STEPS)
+def test_moves_of_training(gv, places, nodes, cols, hidden):
+    """What three steps add to each parameter, against 64 bits, by the size of what they add: a gradient that is left out, or half a per cent
+    off, is seen."""
+    import torch
+
+    def step(params, index, grad, scale, rate):
+        t, a, b, c, g = params
+        x = gv.gv_lookup_rows(t, index, scale=scale)
+        first = gv.gv_dense_rows(x, a, b, act=gv.GV_ACT_GELU, keep_pre=True)
+        second = gv.gv_dense_rows(first.out, c, residual=x)
+        normed = gv.gv_norm_rows(second.out, g, keep_rstd=True)
+        gn = gv.gv_norm_rows_backward(grad, second.out, g, normed.rstd)
+        g2 = gv.gv_dense_rows_backward(gn.x, first.out, c)
+        g1 = gv.gv_dense_rows_backward(g2.x, x, a, first.pre, act=gv.GV_ACT_GELU, keep_bias=True)
+        a -= rate * g1.weight
+        b -= rate * g1.bias
+        c -= rate * g2.weight
+        g -= rate * gn.gain
+        gv.gv_lookup_rows_backward(g1.x + gn.x, index, nodes, scale=-rate * scale, out=t, add=True)
+
+    moved, want, rounding = moves_of_training(torch, places, nodes, cols, hidden, step)
+    for k, (got, expected, off) in enumerate(zip(moved, want, rounding)):
+        assert (got - expected).norm() <= NEAR * expected.norm() + off, (k, ((got - expected).norm() / expected.norm()).item())
