@@ -87,7 +87,7 @@ def scores_of(vertex, context, gain, table, nodes):
 
 
 def shortlist(vertex, context, gain, table, nodes, length):
-    """The `length` likeliest nodes for each of `nodes`, by 8-bit queries against the 4-bit table."""
+    """The `length` likeliest nodes for each of `nodes`, by 8-bit queries against the 4-bit table; -1 where there are fewer."""
     return gv.gv_select_rows(scores_of(vertex, context, gain, table, nodes), length, log_softmax=False).row
 
 
@@ -95,7 +95,7 @@ def answer(vertex, context, gain, table, nodes, best, length):
     """The `best` nodes for each of `nodes`: the shortlist, ranked in full precision."""
     some = shortlist(vertex, context, gain, table, nodes, length)
     q = gv.gv_norm_rows(context[nodes], gain, vertex[nodes]).out
-    score = (vertex[some] * q.unsqueeze(1)).sum(2)
+    score = (vertex[some] * q.unsqueeze(1)).sum(2).masked_fill(some < 0, -math.inf)
     return some.gather(1, torch.topk(score, best, dim=1).indices)
 
 

@@ -226,3 +226,19 @@ def test_moves_of_training(gv, places, nodes, cols, hidden):
     moved, want, rounding = moves_of_training(torch, places, nodes, cols, hidden, step)
     for k, (got, expected, off) in enumerate(zip(moved, want, rounding)):
         assert (got - expected).norm() <= NEAR * expected.norm() + off, (k, ((got - expected).norm() / expected.norm()).item())
+
+
+@gpu
+@pytest.mark.parametrize("nodes,length", [(60, 100), (100, 100), (7, 8)])
+def test_a_shortlist_longer_than_the_nodes(gv, example, nodes, length):
+    """Its empty places are no answers: with every node on it, the answer is the ranking in full precision."""
+    import torch
+
+    gen = torch.Generator(device="cuda").manual_seed(nodes)
+    vertex, context = (torch.randn(nodes, 32, device="cuda", generator=gen) for _ in range(2))
+    gain, some = torch.ones(32, device="cuda"), torch.arange(nodes, device="cuda")
+    got = example.answer(vertex, context, gain, gv.gv_quantize_rows(vertex, group=32), some, 5, length)
+    score = (vertex.unsqueeze(0) * gv.gv_norm_rows(context, gain, vertex).out.unsqueeze(1)).sum(2)
+    assert torch.equal(got, torch.topk(score, 5, dim=1).indices)
+    few = example.answer(vertex[:3], context[:3], gain, gv.gv_quantize_rows(vertex[:3], group=32), some[:3], 5, length)
+    assert (few[:, 3:] == -1).all() and (few[:, :3].sort(1).values == some[:3]).all()
