@@ -840,7 +840,6 @@ hipError_t by_type(int type, Run &&run) {
 struct Cut {
     uint32_t tile, tiles_m, tiles_n, splits, split_k;
 };
-constexpr uint32_t kFewRows = 64;
 
 Cut cut_of(uint64_t rows, uint64_t cols, uint64_t outs, int type, bool wide) {
     const uint64_t step = kStep / (type == GV_F32 ? 4 : 2), steps = std::max<uint64_t>(1, (cols + step - 1) / step);
@@ -877,6 +876,17 @@ uint64_t most_partial_of(uint64_t rows, uint64_t cols, uint64_t outs, int type) 
     uint64_t most = 0;
     for (int i = 0; i < 2; ++i) most = std::max(most, partial_of(cut_of(rows, cols, outs, type, i), rows, outs));
     return most;
+}
+
+// Whether a layer goes by k_product_few: up to 16 rows, and up to 64 where a workgroup has little of x to read for its 16 columns.  us by
+// it and by tiles, of 4096 x 4096 in bfloat16: 16 rows 10 and 12, 24 rows 12.5 and 12.3, 32 rows 13.4 and 12.7, 64 rows 20.5 and 14;
+// 2048 x 2048: 32 rows 8.2 and 12.2, 64 rows 11.4 and 12.3; 32 x 4096 x 16384 45 and 28; in fp32 of 4096 x 4096 24 rows 22 and 26, 64 rows 39
+// and 32; 64 x 1024 x 4096 12.6 and 14.5, 64 x 2048 x 2048 21 and 16.  Rows that do not begin at whole pieces (`whole`) of 16-bit types 64 x
+// 4095 x 4097 118 and 24, of floats 40 and 28 at 32 rows.
+bool few_rows(uint64_t rows, uint32_t cols, uint32_t outs, int type, bool whole) {
+    if (rows <= 16) return true;
+    if (rows > 64 || outs > 4096 || (type != GV_F32 && !whole)) return false;
+    return cols <= (rows > 32 ? (type == GV_F32 ? 1024u : 2048u) : whole ? 4096u : 2048u);
 }
 
 template <class T, bool kAAlong, bool kBAlong>
@@ -945,13 +955,15 @@ GradPlan grad_plan_of(uint64_t rows, uint32_t cols, uint32_t outs, int type, int
 }  // namespace
 
 uint64_t dense_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type) {
-    return rows <= kFewRows ? 0 : most_partial_of(rows, cols, outs, type);
+    return few_rows(rows, cols, outs, type, false) ? 0 : most_partial_of(rows, cols, outs, type);
 }
 
 hipError_t launch_dense(const DenseArgs &a, void *workspace, hipStream_t stream) {
     return by_type(a.type, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        if (a.rows > kFewRows) return product<T, true, true>(a, workspace, stream);
+        const auto whole = [](const void *p, uint64_t stride) { return ((uintptr_t)p | stride * sizeof(T)) % 16 == 0; };
+        if (!few_rows(a.rows, a.cols, a.outs, a.type, whole(a.x, a.x_stride) && whole(a.weight, a.weight_stride)))
+            return product<T, true, true>(a, workspace, stream);
         const uint32_t blocks = (a.outs + 15) / 16;
         if (a.rows <= 16) return launch(k_product_few<T, 1>, blocks, kFewThreads, 0, stream, a);
         if (a.rows <= 32) return launch(k_product_few<T, 2>, blocks, kFewThreads, 0, stream, a);

@@ -205,3 +205,23 @@ def test_rows_by_index_beside_what_they_read(calls):
                                        (lookup(index=OUT, index_stride=0), "overlaps index"), (backward(grad_stride=16, out=at(X, 9), out_stride=16), "overlaps grad"),
                                        (backward(index=OUT), "overlaps index")):
         assert rc == EINVAL and word in text and not launches, text
+
+
+@pytest.mark.parametrize("type", [F32, BF16])
+def test_the_way_of_few_rows(calls, type):
+    """Layers of up to 64 rows: the way goes by the rule beside few_rows, and the workspace is enough for each of them, whatever the alignment."""
+    for rows in (1, 15, 16, 17, 32, 33, 64, 65):
+        for cols in (8, 1024, 1025, 2048, 2056, 4096, 4104, 16384):
+            for outs in (1, 512, 4096, 4104, 16384):
+                for apart in (0, 1):
+                    space = calls.bytes("gv_dense_rows_workspace", rows, cols, outs, type)
+                    stride = cols + apart + (-cols % 4 if apart == 0 else 0)
+                    rc, text, launches = calls.call("gv_dense_rows", rows, cols, outs, type, X, stride, W, stride, None, 0, None, 0, None, 0, OUT, outs,
+                                                    SPACE if space else None, space, None)
+                    assert rc == 0, text
+                    few = b"k_product_few" in launches[0]["kernel"]
+                    whole = stride * SIZE[type] % 16 == 0
+                    most = 4096 // SIZE[type] if rows > 32 else 4096 if whole else 2048
+                    assert few == (rows <= 16 or rows <= 64 and outs <= 4096 and (whole or type == F32) and cols <= most), (rows, cols, outs, apart)
+                    assert space or not any(l["cut"] for l in launches)
+                    assert len(launches) == (1 if few or not launches[0]["cut"] else 2)
