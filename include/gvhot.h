@@ -458,8 +458,8 @@ int gv_lookup_rows_backward(uint64_t count, const void *dev_index, uint64_t inde
 
 /* A layer: z = x weight^T + bias, out = residual + act(z); x has cols columns, weight outs rows of cols, bias outs values, and residual,
  * pre and out have outs columns, all of `type` (GV_F32, GV_BF16, GV_F16).  bias, residual and pre may be NULL; pre receives z, which
- * the backward pass takes.  GV_ACT_GELU is z (1 + erf(z / sqrt 2)) / 2, GV_ACT_SILU z / (1 + exp(-z)); gelu's
- * second factor is within 4e-7 for the 16-bit types, and for GV_F32 within 12 2^-24 of itself (z > -13; it ends there).
+ * the backward pass takes.  GV_ACT_GELU is z (1 + erf(z / sqrt 2)) / 2, GV_ACT_SILU z / (1 + exp(-z)); gelu's second factor is
+ * within 4e-7 for the 16-bit types, and for GV_F32 within 12 2^-24 of itself (down to z = -13, where it ends).
  * Sums are fp32 in an order that sizes, type, strides and alignment decide, act is taken of the sum, and a result is rounded once.
  * out may be residual itself, and of one row out or pre may be bias; else neither out nor pre may overlap what the call reads, or
  * each other.  1 <= outs <= GV_MAX_ROW_COLS.  dev_workspace points to workspace_bytes bytes (at least those of
@@ -473,10 +473,11 @@ int gv_dense_rows(uint64_t rows, uint32_t cols, uint32_t outs, int type, const v
 /* Its gradients from grad_out (of out): with gz = grad_out * act'(pre) (relu: 0 where pre is 0),
  *   grad_x = gz weight,  grad_weight = gz^T x,  grad_bias = sum over the rows of gz,
  * each of `type` and each may be NULL (the residual's gradient is grad_out).  pre is what the forward pass left; without an activation
- * it is not read.  The products take gz rounded to `type`, as they take their other operand; grad_bias adds up what is not rounded.
+ * it is not read.  The products take gz rounded to `type`, as they take their other operand (of GV_F16, what exceeds 65504 is infinite
+ * there, and slopes reach 1.13); grad_bias adds up what is not rounded.
  * None of the three may overlap another of them or what the call reads: x where grad_weight is asked for, weight where grad_x is, pre
- * with an activation.  rows = 0 leaves grad_weight and grad_bias 0.  The workspace is that
- * of gv_dense_rows_backward_workspace, which is told which gradients are asked for.                                  */
+ * with an activation.  rows = 0 leaves grad_weight and grad_bias 0.  The workspace is that of gv_dense_rows_backward_workspace,
+ * which is told which gradients are asked for.                                                                       */
 int gv_dense_rows_backward_workspace(uint64_t rows, uint32_t cols, uint32_t outs, int type, int act, int grad_x, int grad_weight,
                                      int grad_bias, uint64_t *bytes);
 int gv_dense_rows_backward(uint64_t rows, uint32_t cols, uint32_t outs, int type, const void *dev_grad_out, uint64_t grad_out_stride,

@@ -415,8 +415,9 @@ __global__ __launch_bounds__(kSmallThreads) void k_product_small(DenseArgs a, ui
 // LDS, where an operand lies as it does in memory, and what lies with the values of a k together is turned by the loads that
 // transpose. A wave's values of half a step are read while those of the half before are multiplied; one barrier a step says
 // that the next step has arrived and that this one's place is free for the step after that.  8192 x 4096 x 4096 in bfloat16
-// with bias, gelu and residual 227 us, 1.21 PFLOP/s: the matrix units are busy for half of the compute units' cycles, LDS for a
-// fifth (a wave's 128 x 64 take 24 KB of reads a step for 2^20 products), and the epilogue goes on beside nothing.
+// with bias, gelu and residual 242 us, 1.14 PFLOP/s (229 where the same operands come again and again): the matrix units are busy for
+// half of the compute units' cycles, LDS for a fifth (a wave's 128 x 64 take 24 KB of reads a step for 2^20 products), and the
+// epilogue goes on beside nothing.
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s4v LdsFour;
 typedef __attribute__((address_space(3))) void LdsAny;
@@ -752,8 +753,8 @@ __global__ __launch_bounds__(kFewThreads) void k_product_few(DenseArgs a) {
 
 // ---------------------------------------------------------------------------
 // gz = grad * slope(pre), and the sums over its rows: a lane has eight columns, a wave 512, the waves of a workgroup take rows
-// in turn. 65536 x 2048 in bfloat16 with gelu: 185 us for 810 MB, 4.4 TB/s, the vector units busy for half of it; the bias'
-// gradient alone 98 us for 537.
+// in turn. 65536 x 2048 in bfloat16 with gelu: 190 us for 810 MB, 4.2 TB/s, the vector units busy for half of it; the bias'
+// gradient alone 126 us for 537.
 constexpr int kSlopeThreads = 256, kSlopeWaves = kSlopeThreads / 64;
 
 // Rows of eight columns and more (kWide) have no broken piece: the last one lies back so far that it is whole, and two lanes
@@ -769,7 +770,7 @@ __global__ __launch_bounds__(kSlopeThreads) void k_slope(DenseGradArgs a) {
     const bool used = 8 * lane < width && width * part + 8 * lane < a.outs;
     const uint32_t k = kWide ? std::min(width * part + 8 * lane, a.outs - 8) : width * part + 8 * lane, cols = kWide ? k + 8 : a.outs;
     const uint64_t first = (uint64_t)chunk * a.chunk, last = std::min<uint64_t>(a.rows, first + a.chunk);
-    constexpr int kAhead = 2;  // rows of a wave asked for at once (four: 112 us for 65536 x 2048 with the bias' gradient alone, 98 with two)
+    constexpr int kAhead = 2;  // rows of a wave asked for at once (four: the bias' gradient of 65536 x 2048 121 us, of 200000 x 96 88 instead of 81)
     float sums[8] = {};
     if (used) {
         for (uint64_t row = first + wave; row < last; row += kAhead * kSlopeWaves) {
@@ -833,10 +834,10 @@ hipError_t by_type(int type, Run &&run) {
 }
 
 // How a product of rows x outs over `cols` k's is cut: the way that is the shortest by what steps were measured to take.
-// Larger tiles ask for fewer values (8192 x 4096 x 4096 in bfloat16: 214 us by tiles of 256, 256 by 128; 65536 x 512 x 2048
-// 202, 227 and 413 by the small ones; with bias, gelu and pre 242 and 275), smaller ones are more workgroups (1000 x 1000 x
-// 1000: 32, 22 and 10 us), and a long k is cut where there are few (a weight's gradient of 65536 x 128 x 512: 50 us in 64 parts
-// of 128 tiles, 203 in 8).
+// Larger tiles ask for fewer values (8192 x 4096 x 4096 in bfloat16: 214 us by tiles of 256, 244 by 128, 607 by the small ones; 65536 x
+// 512 x 2048 156, 181 and 364; with bias, gelu and pre 230, 263 and 523), smaller ones are more workgroups (1021 x 357 x 500 floats:
+// 65, 26 and 10 us; 1000 x 1000 x 1000 in bfloat16 29, 15, which is taken, and 10), and a long k is cut where there are few (a
+// weight's gradient of 65536 x 128 x 512: 49 us in 64 parts of tiles of 128, 92 in 8; 103 and 180 by the small ones).
 struct Cut {
     uint32_t tile, tiles_m, tiles_n, splits, split_k;
 };

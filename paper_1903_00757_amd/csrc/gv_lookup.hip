@@ -198,8 +198,8 @@ __global__ __launch_bounds__(kGradThreads) void k_grad_few(LookupGradArgs a, uin
 // --- the order of the places by row: pairs of a row (`rows` for places without one, at the end) and a place, sorted.
 
 // Some thousand places: the place of each is how many go before it.  A workgroup of 16 waves takes 64 places, each wave a
-// sixteenth of those that they are compared with.  (4096 places added to rows of 128: 29 us; 16384 75, of which the ranks are
-// 50, and by digits 57: six launches, but few comparisons.)
+// sixteenth of those that they are compared with.  (Places added to 10^6 rows of 128 by ranks and by
+// digits, which are six launches but few comparisons, us: 2048 17 and 32, 4096 24 and 34, 8192 39 and 36, 16384 68 and 38.)
 constexpr int kRankThreads = 1024;
 constexpr uint32_t kRanked = 1 << 13;
 

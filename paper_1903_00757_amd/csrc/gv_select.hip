@@ -58,11 +58,11 @@ __device__ __forceinline__ float raised_above(float least, float x) {
     return next <= least ? least : next;
 }
 
-// exp(d), d <= 21, within 2^-34 of it, and 1 of 0: 2^n times 2^f, |f| <= 1/2, by a polynomial whose first number is 1 and whose
+// exp(d), d <= 700, within 2^-34 of it, and 1 of 0: 2^n times 2^f, |f| <= 1/2, by a polynomial whose first number is 1 and whose
 // others make the largest error the least.  What is below exp(-700) counts as that, which no sum that has a term of 1 notices.
 // Fifteen instructions, each as long as one in fp32.  __expf takes four, but is off by up to (|d| + 1) 2^-23 of a term, and the sum of equal
-// scores by as much of it: beams whose totals lie closer came in the wrong order (the call for 16 x 8 beams of 10^6 took 116 us by it, 151
-// by this).
+// scores by as much of it: beams whose totals lie closer came in the wrong order (the call for 16 x 8 beams of 10^6 took 116 us by it, 147
+// to 151 by this).
 __device__ __forceinline__ double exp_of(double d) {
     constexpr double kLog2E = 1.4426950408889634, kWhole = 0x1.8p52;  // added, it leaves a whole number in the low word
     d = fmax(d, -700.0);
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_select_parts(SelectArgs a) {
     }
 }
 
-// --- the beams of a group joined: one workgroup for each, as long as its few dependent loads and searches take (12 to 23 us)
+// --- the beams of a group joined: one workgroup for each, as long as its few dependent loads and searches take (11 to 24 us)
 constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / 64;
 constexpr uint32_t kJoinSlots = 2 * kJoinThreads, kMostLists = 2048, kMostBeams = GV_MAX_BEAMS;
 static_assert(GV_MAX_BEST + kJoinThreads <= kJoinSlots, "room for the best and a turn");
